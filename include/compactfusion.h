@@ -99,7 +99,8 @@ typedef enum {
     CF_ERR_DEVICE = 6       /* a HIP call failed; see cf_last_hip_error */
 } cf_status;
 
-typedef enum { CF_F32 = 0, CF_BF16 = 1 } cf_dtype;
+/* CF_F16 is a type of the attention entry points only: the codec refuses it (CF_ERR_UNSUPPORTED). */
+typedef enum { CF_F32 = 0, CF_BF16 = 1, CF_F16 = 2 } cf_dtype;
 
 /* What a scale spans.  CHANNEL: all N tokens of one channel (the paper's v_j
  * with u = 1).  GROUP: `group` consecutive channels of one token (4-bit only).
@@ -318,6 +319,123 @@ cf_status cf_profile_next_call(cf_ctx *ctx, void *const *events, int32_t n_pairs
  * (a static string; NULL if k is out of range). */
 int32_t cf_profile_launch_count(const cf_ctx *ctx);
 const char *cf_profile_kernel_name(const cf_ctx *ctx, int32_t k);
+
+/* ---------------------------------------------------------------- attention over keys and values
+ *
+ * What reads the keys and values that the codec brings: appending them to a paged cache (with the rotation of
+ * positions on the way), attention over whole prompts, attention of one new token per sequence over the cache,
+ * and the join of attentions over parts of the keys (the hops of ring attention, App. B Alg. 2).
+ *
+ * These calls have no context and keep nothing between calls.  They follow the rules above: device pointers of the
+ * caller's, work enqueued on `stream` without synchronising, arguments validated on the host before anything is
+ * enqueued, nothing allocated, nothing thrown.  They may be captured into a HIP graph.  Calls that share a workspace
+ * must not overlap in time; calls that do not may run from any threads and on any streams.
+ *
+ * Numbers held on the device cannot be refused.  Whatever they are, no call reads or writes outside the buffers it
+ * was given: starts and lengths are clamped to the tokens or pages there are, page numbers outside the cache are taken
+ * as its nearest page, tokens whose slot or position lies outside are left out.
+ *
+ * Arithmetic.  Scores, the running maximum and sum of the softmax and all accumulators are fp32; the weights
+ * exp(score - maximum) are rounded once to `dtype` for the product with the values on the matrix cores, and outputs are
+ * rounded once.  Results do not depend on timing: the same call on the same data gives the same bits.
+ * Keys that a row does not see (masked, past the end of a sequence, on a page beyond the context) do not
+ * reach its output or its log-sum-exp, whatever those places hold, NaN and infinities included.  A row that sees no
+ * key, or whose scores are all -infinity, gives zeros and a log-sum-exp of -infinity. */
+
+/* A head's row of a token: element i of head h of token t is data[t * token + h * head + i].  Strides are in elements,
+ * multiples of 8, not negative and below 2^24; data is 16-byte aligned.  Slices of a wider projection are such rows.
+ * The rows of an output must not overlap one another. */
+typedef struct {
+    void *data;
+    int64_t token;
+    int64_t head;
+} cf_rows;
+
+typedef struct {
+    int32_t dtype;    /* CF_BF16 or CF_F16: queries, keys, values, outputs */
+    int32_t q_heads;  /* a multiple of kv_heads, at most 65536; head h reads the keys of head h / (q_heads / kv_heads) */
+    int32_t kv_heads;
+    int32_t head_dim; /* 64, 128 or 256 */
+    float scale;      /* of the scores q . k; 0 = 1 / sqrt(head_dim) */
+} cf_attn_desc;
+
+/* Keys and values in pages: element i of head h of slot s is k[(s / page_size) * page_stride +
+ * (h * page_size + s % page_size) * head_dim + i], so that a head's keys of one page are one piece of memory. */
+typedef struct {
+    void *k, *v;         /* 16-byte aligned; they must not overlap, except that pages of one may lie between pages of the other */
+    int64_t n_pages;     /* 1 .. 2^31 - 1 */
+    int64_t page_stride; /* elements from page to page, a multiple of 8; 0 = kv_heads * page_size * head_dim (dense), less is refused */
+    int32_t page_size;   /* tokens of a page: a power of two, 16 .. 32768 */
+} cf_kv_cache;
+
+typedef struct {
+    int64_t n_tokens;         /* >= 0 */
+    cf_rows k, v;             /* [n_tokens][kv_heads][head_dim] */
+    const int64_t *slots;     /* device [n_tokens]: where token t goes in the cache; a token with a slot outside the cache
+                                 (negative: padding) does not go there.  Two tokens of one call in one slot: either. */
+    cf_rows q, q_out;         /* [n_tokens][q_heads][head_dim]: rotated queries; data null: none.  q_out may be q itself. */
+    const int32_t *positions; /* device [n_tokens]; a token whose position is not in [0, n_positions) is left out
+                                 altogether.  Not read with rotary_dim 0. */
+    const float *cos, *sin;   /* device [n_positions][rotary_dim / 2] each */
+    int64_t n_positions;      /* 1 .. 2^31 - 1 */
+    int32_t rotary_dim;       /* leading elements of a head that are rotated, a multiple of 16 up to head_dim; 0 = none */
+    int32_t interleaved;      /* pairs are (2i, 2i + 1) if set, (i, i + rotary_dim / 2) if not */
+} cf_append;
+
+/* Rotates the new tokens' keys (and queries) by their positions, (a, b) -> (a cos - b sin, b cos + a sin) in fp32 with one
+ * rounding at the end, and stores keys and values in the cache.  n_tokens 0 does nothing. */
+cf_status cf_kv_append(const cf_attn_desc *desc, const cf_kv_cache *cache, const cf_append *args, void *stream);
+
+typedef struct {
+    int32_t n_seqs;       /* >= 0: packed one after another */
+    int32_t causal;       /* if set, token i of a sequence sees its keys up to i + (keys - tokens): the last token sees all */
+    int64_t n_q, n_k;     /* rows that q and k / v have; n_q * q_heads and n_k are at most 2^30 */
+    int64_t max_k;        /* keys of the longest sequence as far as the caller knows, 0 = n_k: a hint for how the work is split */
+    const int32_t *cu_q;  /* device [n_seqs + 1]: sequence b has the rows cu_q[b] .. cu_q[b + 1] - 1 of q and out */
+    const int32_t *cu_k;  /* device [n_seqs + 1]: and these of k and v */
+    cf_rows q, k, v, out; /* [n_q][q_heads][head_dim], [n_k][kv_heads][head_dim] twice, [n_q][q_heads][head_dim]; the token
+                             strides of k and v are at least head_dim */
+    float *lse;           /* [n_q][q_heads], dense: natural log of the sum of exp(score) over a row's keys; may be null */
+} cf_prompt;
+
+/* Most that cf_attn_prompt and cf_attn_paged use of a workspace (256-byte aligned device memory; its contents need not be kept
+ * or set).  Where there are few rows and many keys the keys are split and the parts meet in the workspace; a smaller one,
+ * or none (null, 0), allows fewer parts.  The bits of a result depend on the split, and so on the size given. */
+#define CF_ATTN_WORKSPACE_BYTES ((size_t)64 << 20)
+
+/* out = softmax(scale q k^T) v, sequence by sequence.  Rows outside all sequences are not written. */
+cf_status cf_attn_prompt(const cf_attn_desc *desc, const cf_prompt *args, void *workspace, size_t workspace_bytes, void *stream);
+
+typedef struct {
+    int32_t n_seqs;       /* >= 0 */
+    int32_t max_pages;    /* >= 1: entries of a row of the table */
+    int64_t table_stride; /* entries from row to row, at least max_pages; 0 = max_pages */
+    int64_t max_len;      /* the longest context as far as the caller knows, 0 = max_pages * page_size: a hint, as max_k above */
+    const int32_t *table; /* device [n_seqs][max_pages]: pages of sequence b, in the order of its tokens; entries past its length are not read */
+    const int32_t *lens;  /* device [n_seqs]: tokens of the context, the new one among them if it has been appended; at most 2^30 */
+    cf_rows q, out;       /* [n_seqs][q_heads][head_dim]: one token of every sequence */
+    float *lse;           /* [n_seqs][q_heads], dense; may be null */
+} cf_paged;
+
+/* Attention of one new token per sequence over its cached context. */
+cf_status cf_attn_paged(const cf_attn_desc *desc, const cf_kv_cache *cache, const cf_paged *args, void *workspace,
+                        size_t workspace_bytes, void *stream);
+
+#define CF_JOIN_MAX_PARTS 64
+typedef struct {
+    int32_t n_parts;          /* 1 .. CF_JOIN_MAX_PARTS */
+    int32_t part_dtype;       /* of the parts' outputs: CF_F32 or the descriptor's dtype */
+    int64_t n_tokens;         /* >= 0 */
+    const void *const *parts; /* host array of device pointers: [n_tokens][q_heads][head_dim], dense, 16-byte aligned */
+    const float *const *lses; /* host array of device pointers: [n_tokens][q_heads], dense */
+    cf_rows out;              /* [n_tokens][q_heads][head_dim] */
+    float *lse;               /* [n_tokens][q_heads], dense; may be null */
+} cf_join;
+
+/* Attention over the union of disjoint sets of keys from the attention over each: lse = log sum_p exp(lse_p),
+ * out = sum_p exp(lse_p - lse) part_p, in fp32, parts in the order given.  A part whose log-sum-exp of a row is -infinity
+ * adds nothing to it, whatever its output there holds. */
+cf_status cf_attn_join(const cf_attn_desc *desc, const cf_join *args, void *stream);
 
 #ifdef __cplusplus
 }

@@ -20,7 +20,7 @@ LIB_PATH = os.environ.get("CF_LIBRARY") or os.path.join(_HERE, "libcompactfusion
 # cf_status
 CF_OK, CF_ERR_INVALID_ARG, CF_ERR_SHAPE, CF_ERR_UNSUPPORTED, CF_ERR_STATE, CF_ERR_WORKSPACE, CF_ERR_DEVICE = range(7)
 # cf_dtype
-CF_F32, CF_BF16 = 0, 1
+CF_F32, CF_BF16, CF_F16 = 0, 1, 2
 # cf_scale_kind
 CF_SCALE_CHANNEL, CF_SCALE_GROUP, CF_SCALE_RANK1, CF_SPARSE_NM, CF_LOWRANK = 0, 1, 2, 3, 4
 # cf_ef_mode
@@ -34,7 +34,7 @@ CF_FLAG_TEST_NO_WAIT = 0x100
 EXPORTS = ["cf_sizes", "cf_workspace_bytes", "cf_init", "cf_warmup", "cf_set_warm", "cf_compress",
            "cf_decompress", "cf_step_fused", "cf_destroy", "cf_status_string", "cf_last_hip_error",
            "cf_profile_next_call", "cf_profile_launch_count", "cf_profile_kernel_name", "cf_check_device",
-           "cf_step_fused_static", "cf_given_up_items"]
+           "cf_step_fused_static", "cf_given_up_items", "cf_kv_append", "cf_attn_prompt", "cf_attn_paged", "cf_attn_join"]
 
 
 class cf_tensor_desc(ctypes.Structure):
@@ -45,6 +45,41 @@ class cf_tensor_desc(ctypes.Structure):
 class cf_options(ctypes.Structure):
     _fields_ = [("ef", ctypes.c_int32), ("err_dtype", ctypes.c_int32), ("flags", ctypes.c_uint32),
                 ("tile_rows", ctypes.c_int32), ("encode_rows", ctypes.c_int32)]
+
+
+_vp, _i32, _i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
+
+
+class cf_rows(ctypes.Structure):
+    _fields_ = [("data", _vp), ("token", _i64), ("head", _i64)]
+
+
+class cf_attn_desc(ctypes.Structure):
+    _fields_ = [("dtype", _i32), ("q_heads", _i32), ("kv_heads", _i32), ("head_dim", _i32), ("scale", ctypes.c_float)]
+
+
+class cf_kv_cache(ctypes.Structure):
+    _fields_ = [("k", _vp), ("v", _vp), ("n_pages", _i64), ("page_stride", _i64), ("page_size", _i32)]
+
+
+class cf_append(ctypes.Structure):
+    _fields_ = [("n_tokens", _i64), ("k", cf_rows), ("v", cf_rows), ("slots", _vp), ("q", cf_rows), ("q_out", cf_rows),
+                ("positions", _vp), ("cos", _vp), ("sin", _vp), ("n_positions", _i64), ("rotary_dim", _i32), ("interleaved", _i32)]
+
+
+class cf_prompt(ctypes.Structure):
+    _fields_ = [("n_seqs", _i32), ("causal", _i32), ("n_q", _i64), ("n_k", _i64), ("max_k", _i64), ("cu_q", _vp), ("cu_k", _vp),
+                ("q", cf_rows), ("k", cf_rows), ("v", cf_rows), ("out", cf_rows), ("lse", _vp)]
+
+
+class cf_paged(ctypes.Structure):
+    _fields_ = [("n_seqs", _i32), ("max_pages", _i32), ("table_stride", _i64), ("max_len", _i64), ("table", _vp), ("lens", _vp),
+                ("q", cf_rows), ("out", cf_rows), ("lse", _vp)]
+
+
+class cf_join(ctypes.Structure):
+    _fields_ = [("n_parts", _i32), ("part_dtype", _i32), ("n_tokens", _i64), ("parts", ctypes.POINTER(_vp)), ("lses", ctypes.POINTER(_vp)),
+                ("out", cf_rows), ("lse", _vp)]
 
 
 class CFError(RuntimeError):
@@ -102,6 +137,16 @@ def lib() -> ctypes.CDLL:
         L.cf_profile_kernel_name.argtypes = [vp, i32]
         L.cf_given_up_items.restype = i32
         L.cf_given_up_items.argtypes = [vp, vp, ctypes.POINTER(ctypes.c_uint32)]
+        desc_p = ctypes.POINTER(cf_attn_desc)
+        cache_p = ctypes.POINTER(cf_kv_cache)
+        L.cf_kv_append.restype = i32
+        L.cf_kv_append.argtypes = [desc_p, cache_p, ctypes.POINTER(cf_append), vp]
+        L.cf_attn_prompt.restype = i32
+        L.cf_attn_prompt.argtypes = [desc_p, ctypes.POINTER(cf_prompt), vp, sz, vp]
+        L.cf_attn_paged.restype = i32
+        L.cf_attn_paged.argtypes = [desc_p, cache_p, ctypes.POINTER(cf_paged), vp, sz, vp]
+        L.cf_attn_join.restype = i32
+        L.cf_attn_join.argtypes = [desc_p, ctypes.POINTER(cf_join), vp]
         L.cf_step_fused_static.restype = i32
         L.cf_step_fused_static.argtypes = [dp, i32, op, pp, pp, pp, pp, pp, vp]
         _lib = L
@@ -250,3 +295,25 @@ def cf_given_up_items(ctx, stream=None) -> int:
     n = ctypes.c_uint32()
     _check(lib().cf_given_up_items(ctx, _addr(stream), ctypes.byref(n)), "cf_given_up_items", ctx)
     return int(n.value)
+
+
+# ---------------------------------------------------------------- attention over keys and values
+
+CF_ATTN_WORKSPACE_BYTES = 64 << 20
+CF_JOIN_MAX_PARTS = 64
+
+
+def cf_kv_append(desc: cf_attn_desc, cache: cf_kv_cache, args: cf_append, stream=None) -> None:
+    _check(lib().cf_kv_append(desc, cache, args, _addr(stream)), "cf_kv_append")
+
+
+def cf_attn_prompt(desc: cf_attn_desc, args: cf_prompt, workspace=None, workspace_bytes: int = 0, stream=None) -> None:
+    _check(lib().cf_attn_prompt(desc, args, _addr(workspace), workspace_bytes, _addr(stream)), "cf_attn_prompt")
+
+
+def cf_attn_paged(desc: cf_attn_desc, cache: cf_kv_cache, args: cf_paged, workspace=None, workspace_bytes: int = 0, stream=None) -> None:
+    _check(lib().cf_attn_paged(desc, cache, args, _addr(workspace), workspace_bytes, _addr(stream)), "cf_attn_paged")
+
+
+def cf_attn_join(desc: cf_attn_desc, args: cf_join, stream=None) -> None:
+    _check(lib().cf_attn_join(desc, args, _addr(stream)), "cf_attn_join")

@@ -1,0 +1,92 @@
+// Internal interface between the host half of the attention entry points (cf_attn_api.cpp) and their
+// kernels (cf_attn_prompt.hip, cf_attn_paged.hip, cf_attn_rows.hip).  Not installed; not part of the ABI.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace cf {
+namespace attn {
+
+// Strides in bytes from here on.
+struct Rows {
+    char *data;
+    int64_t token, head;
+};
+
+struct Heads {
+    int32_t dtype;                  // cf_dtype
+    int32_t q_heads, kv_heads, group, head_dim;
+    float scale_log2;               // scale * log2(e): the kernels' exponentials are powers of two
+};
+
+struct Cache {
+    char *k, *v;
+    int64_t page_bytes;             // from page to page
+    int32_t n_pages, page_size, page_shift;
+};
+
+// Parts of the keys that were attended apart: part s of row (t, h) is o[(s * n_rows + t * q_heads + h) * head_dim],
+// fp32 and normalised, with its natural log-sum-exp in lse[s * n_rows + ...].
+struct Parts {
+    float *o, *lse;
+    int64_t n_rows;                 // tokens * q_heads
+};
+
+constexpr int kPromptRows = 128;    // query rows (token, head of the group) of a workgroup
+constexpr int kPagedHeads = 16;     // query heads of a workgroup: the columns of a 16 x 16 product
+constexpr int kMaxParts = 64;       // CF_JOIN_MAX_PARTS
+
+struct PromptArgs {
+    Heads h;
+    Rows q, k, v, out;
+    float *lse;
+    const int32_t *cu_q, *cu_k;
+    int32_t n_seqs, n_q, n_k, causal;
+    int32_t n_splits, split_keys;   // split s has the keys [s * split_keys, (s + 1) * split_keys) of a sequence, the last one all the rest
+    Parts parts;                    // of n_splits > 1
+};
+
+struct PagedArgs {
+    Heads h;
+    Cache cache;
+    Rows q, out;
+    float *lse;
+    const int32_t *table, *lens;
+    int64_t table_stride;
+    int32_t n_seqs, max_pages;
+    int32_t n_splits, split_keys;
+    Parts parts;
+};
+
+struct JoinArgs {
+    Heads h;
+    Rows out;
+    float *lse;
+    int64_t n_rows;                 // tokens * q_heads
+    int32_t n_parts;
+    int32_t part_dtype;             // cf_dtype
+    const int32_t *cover;           // if set, only the tokens from cover[0] to cover[n_cover] are joined
+    int32_t n_cover;
+    const void *parts[kMaxParts];
+    const float *lses[kMaxParts];
+};
+
+struct AppendArgs {
+    Heads h;
+    Cache cache;
+    Rows k, v, q, q_out;            // q.data null: none
+    const int64_t *slots;
+    const int32_t *positions;
+    const float *cos, *sin;
+    int64_t n_tokens;
+    int32_t n_positions, rotary_dim, interleaved;
+};
+
+hipError_t launch_prompt(const PromptArgs &a, hipStream_t s);
+hipError_t launch_paged(const PagedArgs &a, hipStream_t s);
+hipError_t launch_join(const JoinArgs &a, hipStream_t s);
+hipError_t launch_append(const AppendArgs &a, hipStream_t s);
+
+}  // namespace attn
+}  // namespace cf

@@ -1,0 +1,311 @@
+// Host half of the attention entry points: arguments are checked here, and the work is split, before anything is enqueued.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "cf_attn.h"
+#include "compactfusion.h"
+
+using namespace cf::attn;
+
+namespace {
+
+constexpr int64_t kMostStride = (int64_t)1 << 24;       // elements: a tile's rows are addressed with 32 bits
+constexpr int64_t kMostRows = (int64_t)1 << 30;
+constexpr int64_t kMostGrid = ((int64_t)1 << 31) - 1;
+constexpr int64_t kCUs = 256;
+
+bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+cf_status check_desc(const cf_attn_desc *d, Heads &h)
+{
+    if (!d) return CF_ERR_INVALID_ARG;
+    if (d->dtype != CF_BF16 && d->dtype != CF_F16) return CF_ERR_UNSUPPORTED;
+    if (d->head_dim != 64 && d->head_dim != 128 && d->head_dim != 256) return CF_ERR_UNSUPPORTED;
+    if (d->kv_heads < 1 || d->q_heads < 1 || d->q_heads > 65536 || d->q_heads % d->kv_heads != 0) return CF_ERR_SHAPE;
+    if (!(d->scale >= 0.0f) || !(d->scale <= 3.0e38f)) return CF_ERR_INVALID_ARG;
+    h.dtype = d->dtype;
+    h.q_heads = d->q_heads;
+    h.kv_heads = d->kv_heads;
+    h.group = d->q_heads / d->kv_heads;
+    h.head_dim = d->head_dim;
+    const double scale = d->scale > 0.0f ? (double)d->scale : 1.0 / sqrt((double)d->head_dim);
+    h.scale_log2 = (float)(scale * 1.4426950408889634);
+    return CF_OK;
+}
+
+// A span of memory: per token, `width` bytes from `at`; tokens lie `step` bytes apart.
+struct Span {
+    uintptr_t at;
+    int64_t tokens, step, width;
+    uintptr_t end() const { return at + (uintptr_t)((tokens - 1) * step + width); }
+};
+
+// Whether two spans may share a byte.  Spans with the same step that lie side by side within it do not.
+bool meet(const Span &a, const Span &b)
+{
+    if (a.tokens < 1 || b.tokens < 1 || a.end() <= b.at || b.end() <= a.at) return false;
+    if (a.step == b.step && a.step > 0) {
+        const int64_t ahead = (int64_t)((b.at - a.at) % (uintptr_t)a.step), off = b.at >= a.at ? ahead : (a.step - (int64_t)((a.at - b.at) % (uintptr_t)a.step)) % a.step;
+        if (off >= a.width && off + b.width <= a.step) return false;
+    }
+    return true;
+}
+
+// Rows of `heads` heads of `tokens` tokens.  `least`: the least stride from token to token that the kernels take.
+cf_status check_rows(const cf_rows &in, int64_t tokens, int64_t heads, int64_t dim, bool output, int64_t least, Rows &out, Span &span)
+{
+    int64_t token = in.token, head = in.head;
+    if (heads == 1) head = dim;             // strides that no element goes by
+    if (tokens == 1) token = heads == 1 ? dim : (heads - 1) * head + dim;
+    if (tokens == 1 && head >= 0 && token > kMostStride) token = dim;
+    if (!in.data || !aligned(in.data, 16)) return CF_ERR_INVALID_ARG;
+    if (token < 0 || head < 0 || token % 8 != 0 || head % 8 != 0 || token >= kMostStride || head >= kMostStride) return CF_ERR_SHAPE;
+    if (tokens > 1 && token < least) return CF_ERR_SHAPE;
+    if (output) {
+        const bool by_token = head >= dim && (tokens == 1 || token >= (heads - 1) * head + dim);
+        const bool by_head = token >= dim && (heads == 1 || head >= (tokens - 1) * token + dim);
+        if (!by_token && !by_head) return CF_ERR_INVALID_ARG;
+    }
+    out.data = static_cast<char *>(in.data);
+    out.token = token * 2;
+    out.head = head * 2;
+    span = {reinterpret_cast<uintptr_t>(in.data), tokens, out.token, ((heads - 1) * head + dim) * 2};
+    return CF_OK;
+}
+
+cf_status check_cache(const cf_kv_cache *c, const Heads &h, Cache &out, Span &k, Span &v)
+{
+    if (!c) return CF_ERR_INVALID_ARG;
+    if (!c->k || !c->v || !aligned(c->k, 16) || !aligned(c->v, 16)) return CF_ERR_INVALID_ARG;
+    if (c->page_size < 16 || c->page_size > 32768 || (c->page_size & (c->page_size - 1)) != 0) return CF_ERR_SHAPE;
+    if (c->n_pages < 1 || c->n_pages > INT32_MAX) return CF_ERR_SHAPE;
+    const int64_t dense = (int64_t)h.kv_heads * c->page_size * h.head_dim;
+    const int64_t stride = c->page_stride ? c->page_stride : dense;
+    if (stride < dense || stride % 8 != 0 || stride > ((int64_t)1 << 40)) return CF_ERR_SHAPE;
+    out.k = static_cast<char *>(c->k);
+    out.v = static_cast<char *>(c->v);
+    out.page_bytes = stride * 2;
+    out.n_pages = (int32_t)c->n_pages;
+    out.page_size = c->page_size;
+    out.page_shift = __builtin_ctz((unsigned)c->page_size);
+    k = {reinterpret_cast<uintptr_t>(c->k), c->n_pages, stride * 2, dense * 2};
+    v = k;
+    v.at = reinterpret_cast<uintptr_t>(c->v);
+    return meet(k, v) ? CF_ERR_INVALID_ARG : CF_OK;
+}
+
+cf_status check_workspace(const void *workspace, size_t bytes)
+{
+    if (bytes > 0 && !workspace) return CF_ERR_WORKSPACE;
+    return aligned(workspace, 256) ? CF_OK : CF_ERR_WORKSPACE;
+}
+
+// How many parts of `rows` rows fit the workspace.
+int64_t parts_that_fit(size_t bytes, int64_t rows, int dim)
+{
+    if (bytes > CF_ATTN_WORKSPACE_BYTES) bytes = CF_ATTN_WORKSPACE_BYTES;
+    return (int64_t)bytes / (rows * (dim + 1) * (int64_t)sizeof(float));
+}
+
+void place_parts(Parts &p, void *workspace, int64_t rows, int64_t n, int dim)
+{
+    p.o = static_cast<float *>(workspace);
+    p.lse = p.o + n * rows * dim;
+    p.n_rows = rows;
+}
+
+cf_status status_of(hipError_t e) { return e == hipSuccess ? CF_OK : CF_ERR_DEVICE; }
+
+hipError_t join_parts(const Heads &h, const Parts &p, int n, const Rows &out, float *lse, const int32_t *cover, int32_t n_cover, hipStream_t s)
+{
+    JoinArgs j = {};
+    j.h = h;
+    j.out = out;
+    j.lse = lse;
+    j.n_rows = p.n_rows;
+    j.n_parts = n;
+    j.part_dtype = CF_F32;
+    j.cover = cover;
+    j.n_cover = n_cover;
+    for (int i = 0; i < n; ++i) {
+        j.parts[i] = p.o + i * p.n_rows * h.head_dim;
+        j.lses[i] = p.lse + i * p.n_rows;
+    }
+    return launch_join(j, s);
+}
+
+int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+}  // namespace
+
+extern "C" {
+
+cf_status cf_kv_append(const cf_attn_desc *desc, const cf_kv_cache *cache, const cf_append *args, void *stream)
+{
+    AppendArgs a = {};
+    Span ck, cv, sk, sv, sq, so;
+    cf_status st = check_desc(desc, a.h);
+    if (st != CF_OK) return st;
+    if (!args) return CF_ERR_INVALID_ARG;
+    if ((st = check_cache(cache, a.h, a.cache, ck, cv)) != CF_OK) return st;
+    if (args->n_tokens < 0 || args->n_tokens > kMostRows) return CF_ERR_SHAPE;
+    if (args->rotary_dim < 0 || args->rotary_dim > desc->head_dim || args->rotary_dim % 16 != 0) return CF_ERR_SHAPE;
+    if (args->n_tokens == 0) return CF_OK;
+    const int64_t n = args->n_tokens, d = desc->head_dim;
+    if ((st = check_rows(args->k, n, desc->kv_heads, d, false, 0, a.k, sk)) != CF_OK) return st;
+    if ((st = check_rows(args->v, n, desc->kv_heads, d, false, 0, a.v, sv)) != CF_OK) return st;
+    if (!args->slots || !aligned(args->slots, 8)) return CF_ERR_INVALID_ARG;
+    if (meet(sk, ck) || meet(sk, cv) || meet(sv, ck) || meet(sv, cv)) return CF_ERR_INVALID_ARG;
+    if (args->q.data || args->q_out.data) {
+        if ((st = check_rows(args->q, n, desc->q_heads, d, false, 0, a.q, sq)) != CF_OK) return st;
+        if ((st = check_rows(args->q_out, n, desc->q_heads, d, true, 0, a.q_out, so)) != CF_OK) return st;
+        const bool in_place = a.q.data == a.q_out.data && a.q.token == a.q_out.token && a.q.head == a.q_out.head;
+        if ((!in_place && meet(sq, so)) || meet(so, sk) || meet(so, sv) || meet(so, ck) || meet(so, cv) || meet(sq, ck) || meet(sq, cv)) return CF_ERR_INVALID_ARG;
+    }
+    if (args->rotary_dim > 0) {
+        if (!args->positions || !aligned(args->positions, 4) || !args->cos || !args->sin || !aligned(args->cos, 16) || !aligned(args->sin, 16)) return CF_ERR_INVALID_ARG;
+        if (args->n_positions < 1 || args->n_positions > INT32_MAX) return CF_ERR_SHAPE;
+        a.positions = args->positions;
+        a.cos = args->cos;
+        a.sin = args->sin;
+        a.n_positions = (int32_t)args->n_positions;
+    }
+    a.slots = args->slots;
+    a.n_tokens = n;
+    a.rotary_dim = args->rotary_dim;
+    a.interleaved = args->interleaved ? 1 : 0;
+    const int64_t rows = (a.q.data ? a.h.q_heads : 0) + 2 * (int64_t)a.h.kv_heads;
+    if (n * rows > kMostGrid) return CF_ERR_SHAPE;
+    return status_of(launch_append(a, static_cast<hipStream_t>(stream)));
+}
+
+cf_status cf_attn_prompt(const cf_attn_desc *desc, const cf_prompt *args, void *workspace, size_t workspace_bytes, void *stream)
+{
+    PromptArgs a = {};
+    Span sq, sk, sv, so;
+    cf_status st = check_desc(desc, a.h);
+    if (st != CF_OK) return st;
+    if (!args) return CF_ERR_INVALID_ARG;
+    if ((st = check_workspace(workspace, workspace_bytes)) != CF_OK) return st;
+    if (args->n_seqs < 0 || args->n_q < 0 || args->n_k < 0 || args->max_k < 0 || args->n_k > kMostRows || args->n_q > kMostRows / desc->q_heads || args->n_seqs > kMostRows) return CF_ERR_SHAPE;
+    if (args->n_seqs == 0 || args->n_q == 0) return CF_OK;
+    const int64_t d = desc->head_dim;
+    if ((st = check_rows(args->q, args->n_q, desc->q_heads, d, false, 0, a.q, sq)) != CF_OK) return st;
+    if ((st = check_rows(args->out, args->n_q, desc->q_heads, d, true, 0, a.out, so)) != CF_OK) return st;
+    if (meet(so, sq)) return CF_ERR_INVALID_ARG;
+    if (args->n_k > 0) {
+        if ((st = check_rows(args->k, args->n_k, desc->kv_heads, d, false, d, a.k, sk)) != CF_OK) return st;
+        if ((st = check_rows(args->v, args->n_k, desc->kv_heads, d, false, d, a.v, sv)) != CF_OK) return st;
+        if (meet(so, sk) || meet(so, sv)) return CF_ERR_INVALID_ARG;
+    }
+    if (!args->cu_q || !args->cu_k || !aligned(args->cu_q, 4) || !aligned(args->cu_k, 4) || !aligned(args->lse, 4)) return CF_ERR_INVALID_ARG;
+    a.lse = args->lse;
+    a.cu_q = args->cu_q;
+    a.cu_k = args->cu_k;
+    a.n_seqs = args->n_seqs;
+    a.n_q = (int32_t)args->n_q;
+    a.n_k = (int32_t)args->n_k;
+    a.causal = args->causal ? 1 : 0;
+
+    const int64_t longest = args->max_k > 0 && args->max_k < args->n_k ? args->max_k : args->n_k;
+    const int64_t tiles = (args->n_q * a.h.group + kPromptRows - 1) / kPromptRows + args->n_seqs;
+    const int64_t rows = args->n_q * a.h.q_heads;
+    const int64_t busy = (args->n_q * a.h.group + kPromptRows - 1) / kPromptRows * a.h.kv_heads;
+    int64_t splits = 2 * kCUs / busy;
+    const int64_t fit = parts_that_fit(workspace_bytes, rows, a.h.head_dim);
+    if (splits > fit) splits = fit;
+    if (splits > longest / 256) splits = longest / 256;
+    if (splits > kMaxParts) splits = kMaxParts;
+    a.n_splits = 1;
+    a.split_keys = (int32_t)kMostRows;
+    if (splits > 1) {
+        a.split_keys = (int32_t)round_up((longest + splits - 1) / splits, 64);
+        a.n_splits = (int32_t)((longest + a.split_keys - 1) / a.split_keys);
+    }
+    if (tiles * a.h.kv_heads * a.n_splits > kMostGrid) return CF_ERR_SHAPE;
+    if (a.n_splits > 1) place_parts(a.parts, workspace, rows, a.n_splits, a.h.head_dim);
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    hipError_t e = launch_prompt(a, s);
+    if (e == hipSuccess && a.n_splits > 1) e = join_parts(a.h, a.parts, a.n_splits, a.out, a.lse, a.cu_q, a.n_seqs, s);
+    return status_of(e);
+}
+
+cf_status cf_attn_paged(const cf_attn_desc *desc, const cf_kv_cache *cache, const cf_paged *args, void *workspace, size_t workspace_bytes,
+                        void *stream)
+{
+    PagedArgs a = {};
+    Span ck, cv, sq, so;
+    cf_status st = check_desc(desc, a.h);
+    if (st != CF_OK) return st;
+    if (!args) return CF_ERR_INVALID_ARG;
+    if ((st = check_cache(cache, a.h, a.cache, ck, cv)) != CF_OK) return st;
+    if ((st = check_workspace(workspace, workspace_bytes)) != CF_OK) return st;
+    const int64_t stride = args->table_stride ? args->table_stride : args->max_pages;
+    if (args->n_seqs < 0 || args->max_pages < 1 || stride < args->max_pages || stride > ((int64_t)1 << 40) || args->max_len < 0 || args->n_seqs > kMostRows / desc->q_heads) return CF_ERR_SHAPE;
+    if (args->n_seqs == 0) return CF_OK;
+    if ((st = check_rows(args->q, args->n_seqs, desc->q_heads, desc->head_dim, false, 0, a.q, sq)) != CF_OK) return st;
+    if ((st = check_rows(args->out, args->n_seqs, desc->q_heads, desc->head_dim, true, 0, a.out, so)) != CF_OK) return st;
+    if (meet(so, sq) || meet(so, ck) || meet(so, cv)) return CF_ERR_INVALID_ARG;
+    if (!args->table || !args->lens || !aligned(args->table, 4) || !aligned(args->lens, 4) || !aligned(args->lse, 4)) return CF_ERR_INVALID_ARG;
+    a.lse = args->lse;
+    a.table = args->table;
+    a.lens = args->lens;
+    a.table_stride = stride;
+    a.n_seqs = args->n_seqs;
+    a.max_pages = args->max_pages;
+
+    const int64_t capacity = (int64_t)args->max_pages * a.cache.page_size;
+    int64_t longest = args->max_len > 0 && args->max_len < capacity ? args->max_len : capacity;
+    if (longest > kMostRows) longest = kMostRows;
+    const int64_t units = args->n_seqs * (int64_t)a.h.kv_heads * ((a.h.group + kPagedHeads - 1) / kPagedHeads);
+    const int64_t rows = (int64_t)args->n_seqs * a.h.q_heads;
+    int64_t keys = round_up((longest * units + 8 * kCUs - 1) / (8 * kCUs), 128);
+    if (keys < 256) keys = 256;
+    if (keys > 2048) keys = 2048;
+    int64_t splits = (longest + keys - 1) / keys;
+    const int64_t fit = parts_that_fit(workspace_bytes, rows, a.h.head_dim);
+    if (splits > fit) splits = fit;
+    if (splits > kMaxParts) splits = kMaxParts;
+    a.n_splits = 1;
+    a.split_keys = (int32_t)kMostRows;
+    if (splits > 1) {
+        a.split_keys = (int32_t)round_up((longest + splits - 1) / splits, 128);
+        a.n_splits = (int32_t)((longest + a.split_keys - 1) / a.split_keys);
+    }
+    if (units * a.n_splits > kMostGrid) return CF_ERR_SHAPE;
+    if (a.n_splits > 1) place_parts(a.parts, workspace, rows, a.n_splits, a.h.head_dim);
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    hipError_t e = launch_paged(a, s);
+    if (e == hipSuccess && a.n_splits > 1) e = join_parts(a.h, a.parts, a.n_splits, a.out, a.lse, nullptr, 0, s);
+    return status_of(e);
+}
+
+cf_status cf_attn_join(const cf_attn_desc *desc, const cf_join *args, void *stream)
+{
+    JoinArgs a = {};
+    Span so;
+    cf_status st = check_desc(desc, a.h);
+    if (st != CF_OK) return st;
+    if (!args || !args->parts || !args->lses) return CF_ERR_INVALID_ARG;
+    if (args->part_dtype != CF_F32 && args->part_dtype != desc->dtype) return CF_ERR_UNSUPPORTED;
+    if (args->n_parts < 1 || args->n_parts > CF_JOIN_MAX_PARTS || args->n_tokens < 0 || args->n_tokens > kMostRows / desc->q_heads) return CF_ERR_SHAPE;
+    if (args->n_tokens == 0) return CF_OK;
+    if ((st = check_rows(args->out, args->n_tokens, desc->q_heads, desc->head_dim, true, 0, a.out, so)) != CF_OK) return st;
+    if (!aligned(args->lse, 4)) return CF_ERR_INVALID_ARG;
+    a.n_rows = args->n_tokens * desc->q_heads;
+    const int64_t width = (int64_t)desc->q_heads * desc->head_dim * (args->part_dtype == CF_F32 ? 4 : 2);
+    for (int i = 0; i < args->n_parts; ++i) {
+        if (!args->parts[i] || !aligned(args->parts[i], 16) || !args->lses[i] || !aligned(args->lses[i], 4)) return CF_ERR_INVALID_ARG;
+        if (meet(so, {reinterpret_cast<uintptr_t>(args->parts[i]), 1, 0, args->n_tokens * width})) return CF_ERR_INVALID_ARG;
+        if (args->lse && meet({reinterpret_cast<uintptr_t>(args->lse), 1, 0, a.n_rows * 4}, {reinterpret_cast<uintptr_t>(args->lses[i]), 1, 0, a.n_rows * 4})) return CF_ERR_INVALID_ARG;
+        a.parts[i] = args->parts[i];
+        a.lses[i] = args->lses[i];
+    }
+    a.lse = args->lse;
+    a.n_parts = args->n_parts;
+    a.part_dtype = args->part_dtype;
+    return status_of(launch_join(a, static_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"

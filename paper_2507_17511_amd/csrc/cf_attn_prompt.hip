@@ -1,0 +1,268 @@
+// Attention over whole prompts: out = softmax(scale q k^T) v per sequence, one pass over the keys with a running
+// maximum and sum.
+//
+// The rows of a workgroup are (token, head) pairs of the query heads that share one head of keys, token-major, so that
+// grouped heads fill a tile of few tokens and the tile's causal edge is short.  A wave has 32 rows.  Both products are
+// taken transposed: S^T = K Q^T gives a lane the scores of ONE row (its column) and 16 of 32 keys; in that layout the weights are
+// the right operand of O^T = V^T P^T, up to an order of the keys that the reads of V follow, so weights
+// never leave their lane, and the row's maximum, sum and scale are scalars of the lane.
+#include <type_traits>
+
+#include "cf_attn_device.h"
+
+namespace cf {
+namespace attn {
+namespace {
+
+constexpr int kWaves = 4;
+static_assert(kPromptRows == kWaves * 32, "a wave has 32 rows");
+
+// Where the 16-byte vectors of a staged tile's row lie: XORed so that neither the reads of K (16 rows, one vector each) nor the
+// transposing reads of V (4 rows, 4 neighbouring vectors each) meet in a bank.
+template <int D> __device__ __forceinline__ int k_turn(int row) { return D == 64 ? (row >> 1) & 7 : row & 15; }
+template <int D> __device__ __forceinline__ int v_turn(int row) { return D == 64 ? ((row >> 1) & 1) << 2 : (row & 3) << 2; }
+
+struct Tile {
+    int seq_q, len_q;           // the sequence's first row of q, and how many
+    int seq_k, len_k;
+    int index;                  // which row tile of the sequence; -1: none
+};
+
+__device__ __forceinline__ int clamped(int x, int most) { return min(max(x, 0), most); }
+
+// The n-th row tile, counted from the last sequence's last: every lane takes a sequence, a prefix sum over the wave
+// finds the one that has it.  Starts are clamped to the rows there are.
+__device__ __forceinline__ Tile find_tile(const PromptArgs &a, int n)
+{
+    Tile t = {0, 0, 0, 0, -1};
+    const int lane = threadIdx.x & 63;
+    for (int end = a.n_seqs; end > 0; end -= 64) {
+        const int b = end - 1 - lane;
+        int q0 = 0, len = 0, tiles = 0;
+        if (b >= 0) {
+            q0 = clamped(gconst<int32_t>(a.cu_q)[b], a.n_q);
+            len = max(clamped(gconst<int32_t>(a.cu_q)[b + 1], a.n_q) - q0, 0);
+            tiles = (int)(((int64_t)len * a.h.group + kPromptRows - 1) / kPromptRows);
+        }
+        int upto = tiles;
+        for (int d = 1; d < 64; d <<= 1) {
+            const int below = __shfl_up(upto, d);
+            if (lane >= d) upto += below;
+        }
+        const int total = __shfl(upto, 63);
+        if (n < total) {
+            const int who = __ffsll((unsigned long long)__ballot(n < upto)) - 1;
+            const int seq = end - 1 - who;
+            t.seq_q = __builtin_amdgcn_readfirstlane(__shfl(q0, who));
+            t.len_q = __builtin_amdgcn_readfirstlane(__shfl(len, who));
+            t.index = __builtin_amdgcn_readfirstlane(__shfl(upto, who) - 1 - n);
+            const int k0 = clamped(gconst<int32_t>(a.cu_k)[seq], a.n_k);
+            t.seq_k = __builtin_amdgcn_readfirstlane(k0);
+            t.len_k = __builtin_amdgcn_readfirstlane(max(clamped(gconst<int32_t>(a.cu_k)[seq + 1], a.n_k) - k0, 0));
+            return t;
+        }
+        n -= total;
+    }
+    return t;
+}
+
+// Brings 16 bytes from `base` + `from` to `to` + 16 * lane in LDS; those past `bytes` are zeros.
+__device__ __forceinline__ void stage(const char *base, uint32_t bytes, uint32_t from, char *to)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (int)bytes, 0x00020000), (CF_LDS void *)to, 16, from, 0, 0, 0);
+}
+
+template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, 2) void k_attn_prompt(PromptArgs a)
+{
+    using E = Elem<DT>;
+    constexpr int kKeys = D == 256 ? 32 : 64;               // keys of a staged tile
+    constexpr int kSteps = D / 16;                          // matrix instructions over the head dimension
+    constexpr int kBlocks = D / 32;                         // 32-row blocks of O^T
+    constexpr int kSub = kKeys / 32;
+    constexpr int kVecs = D / 8;                            // 16-byte vectors of a row
+    constexpr int kLoads = kKeys * kVecs / (kWaves * 64);   // vectors of a tile that a lane brings
+    __shared__ __align__(256) char lds_k[kKeys * D * 2], lds_v[kKeys * D * 2];
+
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
+    const int unit = blockIdx.x % (a.h.kv_heads * a.n_splits);
+    const int kv_head = unit % a.h.kv_heads, split = unit / a.h.kv_heads;
+    const Tile t = find_tile(a, blockIdx.x / (a.h.kv_heads * a.n_splits));
+    if (t.index < 0) return;
+
+    // this lane's row
+    const int row = t.index * kPromptRows + wave * 32 + col;
+    const int rows = t.len_q * a.h.group;
+    const bool live = row < rows;
+    const int token = (live ? row : rows - 1) / a.h.group, head = kv_head * a.h.group + (live ? row : rows - 1) % a.h.group;
+    const int shift = a.causal ? t.len_k - t.len_q + 1 : t.len_k;
+    const int seen = min(max(a.causal ? token + shift : t.len_k, 0), t.len_k);          // keys that the row sees
+    const int split_begin = split * a.split_keys;
+    const int split_end = split == a.n_splits - 1 ? t.len_k : min(split_begin + a.split_keys, t.len_k);
+    // the most that any row of the workgroup, and of the wave, sees; and the least of the wave
+    const int last_row = min((t.index + 1) * kPromptRows, rows) - 1;
+    const int end = min(split_end, a.causal ? min(max(last_row / a.h.group + shift, 0), t.len_k) : t.len_k);
+    int wave_least = seen;
+    const int wave_last = min(t.index * kPromptRows + wave * 32 + 31, rows - 1);
+    const int wave_most = a.causal ? min(max(wave_last / a.h.group + shift, 0), t.len_k) : t.len_k;
+    wave_least = __builtin_amdgcn_readfirstlane(wave_least);                             // column 0 has the wave's first row
+    const bool wave_live = t.index * kPromptRows + wave * 32 < rows;
+
+    u32x4 q[kSteps];
+    {
+        const char *src = a.q.data + (t.seq_q + (int64_t)token) * a.q.token + head * a.q.head + half * 16;
+        for (int i = 0; i < kSteps; ++i) q[i] = *gconst<u32x4>(src + i * 32);
+    }
+
+    f32x16 o[kBlocks];
+    for (int d = 0; d < kBlocks; ++d)
+        for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+    float m = kNoMax, l = 0.0f;
+    const float c = a.h.scale_log2;
+
+    // where this lane's vectors of a tile come from
+    uint32_t k_from[kLoads], v_from[kLoads];
+    for (int n = 0; n < kLoads; ++n) {
+        const int at = (n * kWaves + wave) * 64 + lane, r = at / kVecs, place = at % kVecs;
+        k_from[n] = (uint32_t)r * (uint32_t)a.k.token + (place ^ k_turn<D>(r)) * 16;
+        v_from[n] = (uint32_t)r * (uint32_t)a.v.token + (place ^ v_turn<D>(r)) * 16;
+    }
+    const char *k_base = a.k.data + t.seq_k * a.k.token + kv_head * a.k.head;
+    const char *v_base = a.v.data + t.seq_k * a.v.token + kv_head * a.v.head;
+
+    const CF_LDS char *k_read = (const CF_LDS char *)lds_k + col * (D * 2) + ((half ^ k_turn<D>(col)) << 4);
+    const int v_row = 4 * half + ((lane & 15) >> 2);
+    const int v_vec = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    const CF_LDS char *v_read = (const CF_LDS char *)lds_v + v_row * (D * 2) + ((v_vec ^ v_turn<D>(v_row)) << 4) + (lane & 1) * 8;
+
+    // One staged tile: scores, weights, outputs.  `masked`: not every row sees every key of it.
+    auto step = [&](int key0, auto masked, int edge, int limit) {
+        f32x16 s[kSub];
+        for (int b = 0; b < kSub; ++b) {
+            for (int i = 0; i < 16; ++i) s[b][i] = 0.0f;
+            for (int i = 0; i < kSteps; ++i) {
+                const u32x4 k = *(const CF_LDS u32x4 *)((const CF_LDS char *)((uintptr_t)k_read ^ (i << 5)) + b * 32 * D * 2);
+                s[b] = E::mfma32(k, q[i], s[b]);
+            }
+        }
+        const int most = min(seen, split_end) - key0 - 4 * half;
+        if constexpr (masked) {
+            for (int b = 0; b < kSub; ++b)
+                for (int i = 0; i < 16; ++i)
+                    if (b * 32 + 8 * (i >> 2) + (i & 3) >= most) s[b][i] = -__builtin_inff();
+        }
+        float top = s[0][0];
+        for (int b = 0; b < kSub; ++b)
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
+        top = max_halves(top) * c;
+        if (__any(top > m + kMaxSlack)) {
+            const float fresh = fmaxf(m, top), scale = exp2_fast(m - fresh);
+            for (int d = 0; d < kBlocks; ++d)
+                for (int i = 0; i < 16; ++i) o[d][i] *= scale;
+            l *= scale;
+            m = fresh;
+        }
+        u32x4 p[kSub * 2];
+        for (int b = 0; b < kSub; ++b)
+            for (int i = 0; i < 16; i += 2) {
+                const float p0 = exp2_fast(__builtin_fmaf(s[b][i], c, -m)), p1 = exp2_fast(__builtin_fmaf(s[b][i + 1], c, -m));
+                l += p0 + p1;
+                p[b * 2 + (i >> 3)][(i & 7) >> 1] = E::pack(p0, p1);
+            }
+        for (int g = 0; g < kSub * 2; ++g) {
+            auto values = [&](int d) {
+                const CF_LDS char *at = (const CF_LDS char *)((uintptr_t)v_read ^ (d << 6)) + g * 16 * D * 2;
+                const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((CF_LDS s16x4 *)at));
+                const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((CF_LDS s16x4 *)(at + 8 * D * 2)));
+                return (u32x4){x[0], x[1], y[0], y[1]};
+            };
+            if constexpr (masked) {
+                // A weight of zero does not keep an infinity or NaN out of a sum: 16 keys that no row sees are left out, and where some rows
+                // see some of 16 keys and a value among them is not finite, the keys are added one by one to the rows that see them.
+                if (key0 + g * 16 >= limit) break;
+                if (key0 + g * 16 + 16 > edge) {
+                    u32x4 v[kBlocks];
+                    bool odd = false;
+                    for (int d = 0; d < kBlocks; ++d) {
+                        v[d] = values(d);
+                        for (int w = 0; w < 4; ++w) odd |= E::any_not_finite(v[d][w]);
+                    }
+                    if (!__any(odd)) {
+                        for (int d = 0; d < kBlocks; ++d) o[d] = E::mfma32(v[d], p[g], o[d]);
+                    } else {
+#pragma unroll 1
+                        for (int n = 0; n < 16; ++n) {      // key 8 * (n >> 3) + (n & 7) of the 16; the lanes of half (n >> 2) & 1 have it
+                            const bool mine = half == ((n >> 2) & 1), sees = (n & 4) + g * 16 + 8 * (n >> 3) + (n & 3) - 4 * half < most;
+                            u32x4 keep;
+                            for (int w = 0; w < 4; ++w) keep[w] = mine && w == 2 * (n >> 3) + ((n & 3) >> 1) ? (n & 1 ? 0xffff0000u : 0x0000ffffu) : 0u;
+                            for (int d = 0; d < kBlocks; ++d) {
+                                const f32x16 more = E::mfma32(v[d] & keep, p[g], o[d]);
+                                for (int i = 0; i < 16; ++i) o[d][i] = sees ? more[i] : o[d][i];
+                            }
+                        }
+                    }
+                    continue;
+                }
+            }
+            for (int d = 0; d < kBlocks; ++d) o[d] = E::mfma32(values(d), p[g], o[d]);
+        }
+    };
+
+    for (int key0 = split_begin; key0 < end; key0 += kKeys) {
+        __syncthreads();
+        {
+            const int left = t.len_k - key0;                    // rows from here on; those past the sequence read as zeros
+            const int rows_here = min(left, kKeys);
+            const char *k_at = k_base + (int64_t)key0 * a.k.token, *v_at = v_base + (int64_t)key0 * a.v.token;
+            const uint32_t k_bytes = (uint32_t)(rows_here - 1) * (uint32_t)a.k.token + D * 2, v_bytes = (uint32_t)(rows_here - 1) * (uint32_t)a.v.token + D * 2;
+            for (int n = 0; n < kLoads; ++n) {
+                stage(k_at, k_bytes, k_from[n], lds_k + (n * kWaves + wave) * 1024);
+                stage(v_at, v_bytes, v_from[n], lds_v + (n * kWaves + wave) * 1024);
+            }
+        }
+        __builtin_amdgcn_s_waitcnt(0);
+        __syncthreads();
+        if (!wave_live || key0 >= wave_most) continue;
+
+        // Keys that some of the wave's rows see and others do not, or that lie in the next split, need a mask.
+        const int limit = min(wave_most, split_end), edge = min(wave_least, split_end);
+        if (key0 + kKeys <= edge) step(key0, std::false_type{}, edge, limit);
+        else step(key0, std::true_type{}, edge, limit);
+    }
+
+    l = sum_halves(l);
+    if (!live) return;
+    const float inv = inverse_of(l);
+    const int64_t at = (t.seq_q + (int64_t)token) * a.h.q_heads + head;
+    if (a.n_splits > 1) {
+        float *dst = a.parts.o + ((int64_t)split * a.parts.n_rows + at) * D;
+        for (int d = 0; d < kBlocks; ++d)
+            for (int i = 0; i < 16; i += 4)
+                *gmut<f32x4>(dst + d * 32 + 2 * i + 4 * half) = (f32x4){o[d][i] * inv, o[d][i + 1] * inv, o[d][i + 2] * inv, o[d][i + 3] * inv};
+        if (half == 0) gmut<float>(a.parts.lse)[(int64_t)split * a.parts.n_rows + at] = lse_of(m, l);
+    } else {
+        char *dst = a.out.data + (t.seq_q + (int64_t)token) * a.out.token + head * a.out.head;
+        for (int d = 0; d < kBlocks; ++d)
+            for (int i = 0; i < 16; i += 4)
+                *gmut<u32x2>(dst + (d * 32 + 2 * i + 4 * half) * 2) = (u32x2){E::pack(o[d][i] * inv, o[d][i + 1] * inv), E::pack(o[d][i + 2] * inv, o[d][i + 3] * inv)};
+        if (a.lse && half == 0) gmut<float>(a.lse)[at] = lse_of(m, l);
+    }
+}
+
+template <int DT> hipError_t prompt_typed(const PromptArgs &a, hipStream_t s)
+{
+    const int64_t tiles = ((int64_t)a.n_q * a.h.group + kPromptRows - 1) / kPromptRows + a.n_seqs;      // at most: a part of one for every sequence
+    const unsigned grid = (unsigned)(tiles * a.h.kv_heads * a.n_splits);
+    switch (a.h.head_dim) {
+    case 64: hipLaunchKernelGGL((k_attn_prompt<DT, 64>), dim3(grid), dim3(kWaves * 64), 0, s, a); break;
+    case 128: hipLaunchKernelGGL((k_attn_prompt<DT, 128>), dim3(grid), dim3(kWaves * 64), 0, s, a); break;
+    default: hipLaunchKernelGGL((k_attn_prompt<DT, 256>), dim3(grid), dim3(kWaves * 64), 0, s, a); break;
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_prompt(const PromptArgs &a, hipStream_t s) { return a.h.dtype == BF16 ? prompt_typed<BF16>(a, s) : prompt_typed<F16>(a, s); }
+
+}  // namespace attn
+}  // namespace cf
