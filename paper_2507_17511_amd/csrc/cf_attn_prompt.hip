@@ -6,8 +6,6 @@
 // taken transposed: S^T = K Q^T gives a lane the scores of ONE row (its column) and 16 of 32 keys; in that layout the weights are
 // the right operand of O^T = V^T P^T, up to an order of the keys that the reads of V follow, so weights
 // never leave their lane, and the row's maximum, sum and scale are scalars of the lane.
-#include <type_traits>
-
 #include "cf_attn_device.h"
 
 namespace cf {
@@ -19,8 +17,8 @@ static_assert(kPromptRows == kWaves * 32, "a wave has 32 rows");
 
 // Where the 16-byte vectors of a staged tile's row lie: XORed so that neither the reads of K (16 rows, one vector each) nor the
 // transposing reads of V (4 rows, 4 neighbouring vectors each) meet in a bank.
-template <int D> __device__ __forceinline__ int k_turn(int row) { return D == 64 ? (row >> 1) & 7 : row & 15; }
-template <int D> __device__ __forceinline__ int v_turn(int row) { return D == 64 ? ((row >> 1) & 1) << 2 : (row & 3) << 2; }
+template <int D> __device__ __forceinline__ constexpr int k_turn(int row) { return D == 64 ? (row >> 1) & 7 : D == 128 ? row & 15 : row & 7; }
+template <int D> __device__ __forceinline__ constexpr int v_turn(int row) { return D == 64 ? ((row >> 1) & 1) << 2 : (row & 3) << 2; }
 
 struct Tile {
     int seq_q, len_q;           // the sequence's first row of q, and how many
@@ -49,13 +47,13 @@ __device__ __forceinline__ Tile find_tile(const PromptArgs &a, int n)
             const int below = __shfl_up(upto, d);
             if (lane >= d) upto += below;
         }
-        const int total = __shfl(upto, 63);
+        const int total = __builtin_amdgcn_readlane(upto, 63);
         if (n < total) {
-            const int who = __ffsll((unsigned long long)__ballot(n < upto)) - 1;
+            const int who = __builtin_ctzll(__ballot(n < upto));
             const int seq = end - 1 - who;
-            t.seq_q = __builtin_amdgcn_readfirstlane(__shfl(q0, who));
-            t.len_q = __builtin_amdgcn_readfirstlane(__shfl(len, who));
-            t.index = __builtin_amdgcn_readfirstlane(__shfl(upto, who) - 1 - n);
+            t.seq_q = __builtin_amdgcn_readlane(q0, who);
+            t.len_q = __builtin_amdgcn_readlane(len, who);
+            t.index = __builtin_amdgcn_readlane(upto, who) - 1 - n;
             const int k0 = clamped(gconst<int32_t>(a.cu_k)[seq], a.n_k);
             t.seq_k = __builtin_amdgcn_readfirstlane(k0);
             t.len_k = __builtin_amdgcn_readfirstlane(max(clamped(gconst<int32_t>(a.cu_k)[seq + 1], a.n_k) - k0, 0));
@@ -72,18 +70,21 @@ __device__ __forceinline__ void stage(const char *base, uint32_t bytes, uint32_t
     __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (int)bytes, 0x00020000), (CF_LDS void *)to, 16, from, 0, 0, 0);
 }
 
-template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, 2) void k_attn_prompt(PromptArgs a)
+template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void k_attn_prompt(PromptArgs a)
 {
     using E = Elem<DT>;
-    constexpr int kKeys = D == 256 ? 32 : 64;               // keys of a staged tile
+    constexpr int kKeys = 64;               // keys of a staged tile
     constexpr int kSteps = D / 16;                          // matrix instructions over the head dimension
     constexpr int kBlocks = D / 32;                         // 32-row blocks of O^T
     constexpr int kSub = kKeys / 32;
     constexpr int kVecs = D / 8;                            // 16-byte vectors of a row
+    constexpr int kStepRows = kWaves * 64 / kVecs;          // rows that the workgroup brings with one load a lane
+    static_assert(k_turn<D>(kStepRows) == 0 && v_turn<D>(kStepRows) == 0, "every kStepRows rows are turned alike");
     constexpr int kLoads = kKeys * kVecs / (kWaves * 64);   // vectors of a tile that a lane brings
-    __shared__ __align__(256) char lds_k[kKeys * D * 2], lds_v[kKeys * D * 2];
+    constexpr int kTile = kKeys * D * 2;
+    __shared__ __align__(256) char lds_k[2 * kTile], lds_v[2 * kTile];
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
     const int unit = blockIdx.x % (a.h.kv_heads * a.n_splits);
     const int kv_head = unit % a.h.kv_heads, split = unit / a.h.kv_heads;
     const Tile t = find_tile(a, blockIdx.x / (a.h.kv_heads * a.n_splits));
@@ -110,123 +111,136 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, 2) void k_att
     u32x4 q[kSteps];
     {
         const char *src = a.q.data + (t.seq_q + (int64_t)token) * a.q.token + head * a.q.head + half * 16;
+#pragma unroll
         for (int i = 0; i < kSteps; ++i) q[i] = *gconst<u32x4>(src + i * 32);
     }
 
     f32x16 o[kBlocks];
+#pragma unroll
     for (int d = 0; d < kBlocks; ++d)
+#pragma unroll
         for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
     float m = kNoMax, l = 0.0f;
     const float c = a.h.scale_log2;
 
-    // where this lane's vectors of a tile come from
-    uint32_t k_from[kLoads], v_from[kLoads];
-    for (int n = 0; n < kLoads; ++n) {
-        const int at = (n * kWaves + wave) * 64 + lane, r = at / kVecs, place = at % kVecs;
-        k_from[n] = (uint32_t)r * (uint32_t)a.k.token + (place ^ k_turn<D>(r)) * 16;
-        v_from[n] = (uint32_t)r * (uint32_t)a.v.token + (place ^ v_turn<D>(r)) * 16;
-    }
+    // where this lane's vectors of a tile come from: the n-th is n * kStepRows rows further on, and turned alike
+    const int from_row = (wave * 64 + lane) / kVecs, place = lane % kVecs;
+    const uint32_t k_from = (uint32_t)from_row * (uint32_t)a.k.token + (place ^ k_turn<D>(from_row)) * 16;
+    const uint32_t v_from = (uint32_t)from_row * (uint32_t)a.v.token + (place ^ v_turn<D>(from_row)) * 16;
     const char *k_base = a.k.data + t.seq_k * a.k.token + kv_head * a.k.head;
     const char *v_base = a.v.data + t.seq_k * a.v.token + kv_head * a.v.head;
+    auto bring = [&](int key0, int buffer) {
+#pragma unroll
+        for (int n = 0; n < kLoads; ++n) {
+            const int at = key0 + n * kStepRows, left = t.len_k - at;      // rows past the sequence come as zeros
+            stage(k_base + at * a.k.token, left > 0 ? (uint32_t)(min(left, kStepRows) - 1) * (uint32_t)a.k.token + D * 2 : 0, k_from, lds_k + buffer + (n * kWaves + wave) * 1024);
+            stage(v_base + at * a.v.token, left > 0 ? (uint32_t)(min(left, kStepRows) - 1) * (uint32_t)a.v.token + D * 2 : 0, v_from, lds_v + buffer + (n * kWaves + wave) * 1024);
+        }
+    };
 
     const CF_LDS char *k_read = (const CF_LDS char *)lds_k + col * (D * 2) + ((half ^ k_turn<D>(col)) << 4);
     const int v_row = 4 * half + ((lane & 15) >> 2);
     const int v_vec = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
     const CF_LDS char *v_read = (const CF_LDS char *)lds_v + v_row * (D * 2) + ((v_vec ^ v_turn<D>(v_row)) << 4) + (lane & 1) * 8;
+    // elements d * 32 + col of keys 16 g + 4 half + {0 .. 3, 8 .. 11} of the tile
+    auto values = [&](int buffer, int g, int d) {
+        const CF_LDS char *at = (const CF_LDS char *)((uintptr_t)v_read ^ (d << 6)) + buffer + g * 16 * D * 2;
+        const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((CF_LDS s16x4 *)at));
+        const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((CF_LDS s16x4 *)(at + 8 * D * 2)));
+        return (u32x4){x[0], x[1], y[0], y[1]};
+    };
 
-    // One staged tile: scores, weights, outputs.  `masked`: not every row sees every key of it.
-    auto step = [&](int key0, auto masked, int edge, int limit) {
+    // keys that no row of the wave sees begin here, and keys that not all of its rows see
+    const int limit = min(wave_live ? wave_most : 0, split_end), edge = min(wave_least, split_end);
+    if (split_begin < end) bring(split_begin, 0);
+    int buffer = 0;
+    for (int key0 = split_begin; key0 < end; key0 += kKeys, buffer ^= kTile) {
+        // This tile has come, for all waves, and nobody reads the other buffer any more: the next one goes there.
+        __builtin_amdgcn_s_waitcnt(0x0f70);                     // vmcnt(0)
+        __builtin_amdgcn_s_barrier();
+        if (key0 + kKeys < end) bring(key0 + kKeys, buffer ^ kTile);
+        if (key0 >= limit) continue;
+
         f32x16 s[kSub];
+#pragma unroll
         for (int b = 0; b < kSub; ++b) {
+#pragma unroll
             for (int i = 0; i < 16; ++i) s[b][i] = 0.0f;
+#pragma unroll
             for (int i = 0; i < kSteps; ++i) {
-                const u32x4 k = *(const CF_LDS u32x4 *)((const CF_LDS char *)((uintptr_t)k_read ^ (i << 5)) + b * 32 * D * 2);
+                const u32x4 k = *(const CF_LDS u32x4 *)((const CF_LDS char *)((uintptr_t)k_read ^ (i << 5)) + buffer + b * 32 * D * 2);
                 s[b] = E::mfma32(k, q[i], s[b]);
             }
         }
-        const int most = min(seen, split_end) - key0 - 4 * half;
-        if constexpr (masked) {
+        bool odd = false;
+        if (key0 + kKeys > edge) {
+            const int most = min(seen, split_end) - key0 - 4 * half;
+#pragma unroll
             for (int b = 0; b < kSub; ++b)
+#pragma unroll
                 for (int i = 0; i < 16; ++i)
                     if (b * 32 + 8 * (i >> 2) + (i & 3) >= most) s[b][i] = -__builtin_inff();
+            // A weight of zero does not keep an infinity or NaN out of a sum: is there one among the values that not all rows see?
+#pragma unroll 1
+            for (int g = max(edge - key0, 0) >> 4; g < kSub * 2; ++g)
+#pragma unroll
+                for (int d = 0; d < kBlocks; ++d) {
+                    const u32x4 v = values(buffer, g, d);
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) odd |= E::any_not_finite(v[w]);
+                }
+            odd = __any(odd);
         }
         float top = s[0][0];
+#pragma unroll
         for (int b = 0; b < kSub; ++b)
+#pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
         top = max_halves(top) * c;
         if (__any(top > m + kMaxSlack)) {
             const float fresh = fmaxf(m, top), scale = exp2_fast(m - fresh);
+#pragma unroll
             for (int d = 0; d < kBlocks; ++d)
+#pragma unroll
                 for (int i = 0; i < 16; ++i) o[d][i] *= scale;
             l *= scale;
             m = fresh;
         }
         u32x4 p[kSub * 2];
+#pragma unroll
         for (int b = 0; b < kSub; ++b)
+#pragma unroll
             for (int i = 0; i < 16; i += 2) {
                 const float p0 = exp2_fast(__builtin_fmaf(s[b][i], c, -m)), p1 = exp2_fast(__builtin_fmaf(s[b][i + 1], c, -m));
                 l += p0 + p1;
                 p[b * 2 + (i >> 3)][(i & 7) >> 1] = E::pack(p0, p1);
             }
-        for (int g = 0; g < kSub * 2; ++g) {
-            auto values = [&](int d) {
-                const CF_LDS char *at = (const CF_LDS char *)((uintptr_t)v_read ^ (d << 6)) + g * 16 * D * 2;
-                const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((CF_LDS s16x4 *)at));
-                const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((CF_LDS s16x4 *)(at + 8 * D * 2)));
-                return (u32x4){x[0], x[1], y[0], y[1]};
-            };
-            if constexpr (masked) {
-                // A weight of zero does not keep an infinity or NaN out of a sum: 16 keys that no row sees are left out, and where some rows
-                // see some of 16 keys and a value among them is not finite, the keys are added one by one to the rows that see them.
-                if (key0 + g * 16 >= limit) break;
-                if (key0 + g * 16 + 16 > edge) {
-                    u32x4 v[kBlocks];
-                    bool odd = false;
-                    for (int d = 0; d < kBlocks; ++d) {
-                        v[d] = values(d);
-                        for (int w = 0; w < 4; ++w) odd |= E::any_not_finite(v[d][w]);
-                    }
-                    if (!__any(odd)) {
-                        for (int d = 0; d < kBlocks; ++d) o[d] = E::mfma32(v[d], p[g], o[d]);
-                    } else {
+        if (__builtin_expect(!odd, 1)) {
+#pragma unroll
+            for (int g = 0; g < kSub * 2; ++g)
+#pragma unroll
+                for (int d = 0; d < kBlocks; ++d) o[d] = E::mfma32(values(buffer, g, d), p[g], o[d]);
+        } else {
+            // The tile's keys one by one, to the rows that see them: the n-th of 16, which the lanes of half (n >> 2) & 1 have.
+            const int most = min(seen, split_end) - key0;
 #pragma unroll 1
-                        for (int n = 0; n < 16; ++n) {      // key 8 * (n >> 3) + (n & 7) of the 16; the lanes of half (n >> 2) & 1 have it
-                            const bool mine = half == ((n >> 2) & 1), sees = (n & 4) + g * 16 + 8 * (n >> 3) + (n & 3) - 4 * half < most;
-                            u32x4 keep;
-                            for (int w = 0; w < 4; ++w) keep[w] = mine && w == 2 * (n >> 3) + ((n & 3) >> 1) ? (n & 1 ? 0xffff0000u : 0x0000ffffu) : 0u;
-                            for (int d = 0; d < kBlocks; ++d) {
-                                const f32x16 more = E::mfma32(v[d] & keep, p[g], o[d]);
-                                for (int i = 0; i < 16; ++i) o[d][i] = sees ? more[i] : o[d][i];
-                            }
-                        }
-                    }
-                    continue;
+            for (int key = 0; key < kKeys; ++key) {
+                const int g = key >> 4, n = key & 15;
+                u32x4 weights = p[0];
+#pragma unroll
+                for (int i = 1; i < kSub * 2; ++i) weights = g == i ? p[i] : weights;
+#pragma unroll
+                for (int d = 0; d < kBlocks; ++d) {
+                    u32x4 v = values(buffer, g, d);
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) v[w] = half == ((n >> 2) & 1) && w == 2 * (n >> 3) + ((n & 3) >> 1) ? v[w] & (n & 1 ? 0xffff0000u : 0x0000ffffu) : 0u;
+                    const f32x16 more = E::mfma32(v, weights, o[d]);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[d][i] = key < most ? more[i] : o[d][i];
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             }
-            for (int d = 0; d < kBlocks; ++d) o[d] = E::mfma32(values(d), p[g], o[d]);
         }
-    };
-
-    for (int key0 = split_begin; key0 < end; key0 += kKeys) {
-        __syncthreads();
-        {
-            const int left = t.len_k - key0;                    // rows from here on; those past the sequence read as zeros
-            const int rows_here = min(left, kKeys);
-            const char *k_at = k_base + (int64_t)key0 * a.k.token, *v_at = v_base + (int64_t)key0 * a.v.token;
-            const uint32_t k_bytes = (uint32_t)(rows_here - 1) * (uint32_t)a.k.token + D * 2, v_bytes = (uint32_t)(rows_here - 1) * (uint32_t)a.v.token + D * 2;
-            for (int n = 0; n < kLoads; ++n) {
-                stage(k_at, k_bytes, k_from[n], lds_k + (n * kWaves + wave) * 1024);
-                stage(v_at, v_bytes, v_from[n], lds_v + (n * kWaves + wave) * 1024);
-            }
-        }
-        __builtin_amdgcn_s_waitcnt(0);
-        __syncthreads();
-        if (!wave_live || key0 >= wave_most) continue;
-
-        // Keys that some of the wave's rows see and others do not, or that lie in the next split, need a mask.
-        const int limit = min(wave_most, split_end), edge = min(wave_least, split_end);
-        if (key0 + kKeys <= edge) step(key0, std::false_type{}, edge, limit);
-        else step(key0, std::true_type{}, edge, limit);
     }
 
     l = sum_halves(l);
@@ -235,13 +249,17 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, 2) void k_att
     const int64_t at = (t.seq_q + (int64_t)token) * a.h.q_heads + head;
     if (a.n_splits > 1) {
         float *dst = a.parts.o + ((int64_t)split * a.parts.n_rows + at) * D;
+#pragma unroll
         for (int d = 0; d < kBlocks; ++d)
+#pragma unroll
             for (int i = 0; i < 16; i += 4)
                 *gmut<f32x4>(dst + d * 32 + 2 * i + 4 * half) = (f32x4){o[d][i] * inv, o[d][i + 1] * inv, o[d][i + 2] * inv, o[d][i + 3] * inv};
         if (half == 0) gmut<float>(a.parts.lse)[(int64_t)split * a.parts.n_rows + at] = lse_of(m, l);
     } else {
         char *dst = a.out.data + (t.seq_q + (int64_t)token) * a.out.token + head * a.out.head;
+#pragma unroll
         for (int d = 0; d < kBlocks; ++d)
+#pragma unroll
             for (int i = 0; i < 16; i += 4)
                 *gmut<u32x2>(dst + (d * 32 + 2 * i + 4 * half) * 2) = (u32x2){E::pack(o[d][i] * inv, o[d][i + 1] * inv), E::pack(o[d][i + 2] * inv, o[d][i + 3] * inv)};
         if (a.lse && half == 0) gmut<float>(a.lse)[at] = lse_of(m, l);
