@@ -64,10 +64,10 @@ __device__ __forceinline__ Tile find_tile(const PromptArgs &a, int n)
     return t;
 }
 
-// Brings 16 bytes from `base` + `from` to `to` + 16 * lane in LDS; those past `bytes` are zeros.
-__device__ __forceinline__ void stage(const char *base, uint32_t bytes, uint32_t from, char *to)
+// Brings 16 bytes from `base` + `from_all` + `from` to `to` + 16 * lane in LDS; those of which `from` is past `bytes` are zeros.
+__device__ __forceinline__ void stage(const char *base, uint32_t bytes, uint32_t from, uint32_t from_all, char *to)
 {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (int)bytes, 0x00020000), (CF_LDS void *)to, 16, from, 0, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (int)bytes, 0x00020000), (CF_LDS void *)to, 16, from, from_all, 0, 0);
 }
 
 template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : 2) void k_attn_prompt(PromptArgs a)
@@ -130,11 +130,20 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 
     const char *k_base = a.k.data + t.seq_k * a.k.token + kv_head * a.k.head;
     const char *v_base = a.v.data + t.seq_k * a.v.token + kv_head * a.v.head;
     auto bring = [&](int key0, int buffer) {
+        const char *k_at = k_base + key0 * a.k.token, *v_at = v_base + key0 * a.v.token;
+        if (key0 + kKeys <= t.len_k) {
 #pragma unroll
-        for (int n = 0; n < kLoads; ++n) {
-            const int at = key0 + n * kStepRows, left = t.len_k - at;      // rows past the sequence come as zeros
-            stage(k_base + at * a.k.token, left > 0 ? (uint32_t)(min(left, kStepRows) - 1) * (uint32_t)a.k.token + D * 2 : 0, k_from, lds_k + buffer + (n * kWaves + wave) * 1024);
-            stage(v_base + at * a.v.token, left > 0 ? (uint32_t)(min(left, kStepRows) - 1) * (uint32_t)a.v.token + D * 2 : 0, v_from, lds_v + buffer + (n * kWaves + wave) * 1024);
+            for (int n = 0; n < kLoads; ++n) {
+                stage(k_at, 0xffffffffu, k_from, n * (uint32_t)(kStepRows * a.k.token), lds_k + buffer + (n * kWaves + wave) * 1024);
+                stage(v_at, 0xffffffffu, v_from, n * (uint32_t)(kStepRows * a.v.token), lds_v + buffer + (n * kWaves + wave) * 1024);
+            }
+        } else {            // rows past the sequence come as zeros
+#pragma unroll 1
+            for (int n = 0; n < kLoads; ++n) {
+                const int rows_here = min(t.len_k - key0 - n * kStepRows, kStepRows);
+                stage(k_at + n * kStepRows * a.k.token, rows_here > 0 ? (uint32_t)(rows_here - 1) * (uint32_t)a.k.token + D * 2 : 0, k_from, 0, lds_k + buffer + (n * kWaves + wave) * 1024);
+                stage(v_at + n * kStepRows * a.v.token, rows_here > 0 ? (uint32_t)(rows_here - 1) * (uint32_t)a.v.token + D * 2 : 0, v_from, 0, lds_v + buffer + (n * kWaves + wave) * 1024);
+            }
         }
     };
 
@@ -151,17 +160,20 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 
     };
 
     // keys that no row of the wave sees begin here, and keys that not all of its rows see
-    const int limit = min(wave_live ? wave_most : 0, split_end), edge = min(wave_least, split_end);
-    if (split_begin < end) bring(split_begin, 0);
-    int buffer = 0;
-    for (int key0 = split_begin; key0 < end; key0 += kKeys, buffer ^= kTile) {
-        // This tile has come, for all waves, and nobody reads the other buffer any more: the next one goes there.
-        __builtin_amdgcn_s_waitcnt(0x0f70);                     // vmcnt(0)
-        __builtin_amdgcn_s_barrier();
-        if (key0 + kKeys < end) bring(key0 + kKeys, buffer ^ kTile);
-        if (key0 >= limit) continue;
+    const int limit = min(wave_live ? wave_most : 0, split_end), edge = min(wave_least, limit);
 
-        f32x16 s[kSub];
+    // Two buffers: while one is worked on the next tile comes into the other.  The waves of a workgroup meet here once a tile,
+    // wherever in the loops below they are.
+    int key0 = split_begin, buffer = 0;
+    auto advance = [&]() {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");      // the next tile has come, and this one's buffer is free
+        if (key0 + 2 * kKeys < end) bring(key0 + 2 * kKeys, buffer);
+        key0 += kKeys;
+        buffer ^= kTile;
+    };
+    f32x16 s[kSub];
+    u32x4 p[kSub * 2];
+    auto scores = [&]() {
 #pragma unroll
         for (int b = 0; b < kSub; ++b) {
 #pragma unroll
@@ -172,41 +184,25 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 
                 s[b] = E::mfma32(k, q[i], s[b]);
             }
         }
-        bool odd = false;
-        if (key0 + kKeys > edge) {
-            const int most = min(seen, split_end) - key0 - 4 * half;
-#pragma unroll
-            for (int b = 0; b < kSub; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (b * 32 + 8 * (i >> 2) + (i & 3) >= most) s[b][i] = -__builtin_inff();
-            // A weight of zero does not keep an infinity or NaN out of a sum: is there one among the values that not all rows see?
-#pragma unroll 1
-            for (int g = max(edge - key0, 0) >> 4; g < kSub * 2; ++g)
-#pragma unroll
-                for (int d = 0; d < kBlocks; ++d) {
-                    const u32x4 v = values(buffer, g, d);
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) odd |= E::any_not_finite(v[w]);
-                }
-            odd = __any(odd);
-        }
+    };
+    auto largest = [&]() {
         float top = s[0][0];
 #pragma unroll
         for (int b = 0; b < kSub; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
-        top = max_halves(top) * c;
-        if (__any(top > m + kMaxSlack)) {
-            const float fresh = fmaxf(m, top), scale = exp2_fast(m - fresh);
+        return max_halves(top) * c;
+    };
+    auto rescale = [&](float top) {
+        const float fresh = fmaxf(m, top), scale = exp2_fast(m - fresh);
 #pragma unroll
-            for (int d = 0; d < kBlocks; ++d)
+        for (int d = 0; d < kBlocks; ++d)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) o[d][i] *= scale;
-            l *= scale;
-            m = fresh;
-        }
-        u32x4 p[kSub * 2];
+            for (int i = 0; i < 16; ++i) o[d][i] *= scale;
+        l *= scale;
+        m = fresh;
+    };
+    auto weights = [&]() {
 #pragma unroll
         for (int b = 0; b < kSub; ++b)
 #pragma unroll
@@ -215,33 +211,79 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 
                 l += p0 + p1;
                 p[b * 2 + (i >> 3)][(i & 7) >> 1] = E::pack(p0, p1);
             }
-        if (__builtin_expect(!odd, 1)) {
+    };
+    auto products = [&]() {
 #pragma unroll
-            for (int g = 0; g < kSub * 2; ++g)
+        for (int g = 0; g < kSub * 2; ++g)
 #pragma unroll
-                for (int d = 0; d < kBlocks; ++d) o[d] = E::mfma32(values(buffer, g, d), p[g], o[d]);
-        } else {
-            // The tile's keys one by one, to the rows that see them: the n-th of 16, which the lanes of half (n >> 2) & 1 have.
-            const int most = min(seen, split_end) - key0;
+            for (int d = 0; d < kBlocks; ++d) o[d] = E::mfma32(values(buffer, g, d), p[g], o[d]);
+    };
+
+    if (key0 < end) {
+        bring(key0, 0);
+        asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+        if (key0 + kKeys < end) bring(key0 + kKeys, kTile);
+    }
+    // Tiles that all rows of the wave see.  The accumulators are scaled outside of the inner loop, where the compiler keeps them in place; a tile
+    // that asks for it, most often the first alone, has its scores computed again.
+    while (key0 + kKeys <= edge) {
+        float top;
+        for (; key0 + kKeys <= edge; advance()) {
+            scores();
+            top = largest();
+            if (__any(top > m + kMaxSlack)) break;
+            weights();
+            products();
+        }
+        if (key0 + kKeys <= edge) rescale(top);
+    }
+    // Tiles of which some rows see a part.
+    for (; key0 < limit; advance()) {
+        scores();
+        const int most = min(seen, split_end) - key0;
+#pragma unroll
+        for (int b = 0; b < kSub; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (b * 32 + 8 * (i >> 2) + (i & 3) >= most - 4 * half) s[b][i] = -__builtin_inff();
+        // A weight of zero does not keep an infinity or NaN out of a sum: is there one among the values that not all rows see?
+        bool odd = false;
 #pragma unroll 1
-            for (int key = 0; key < kKeys; ++key) {
-                const int g = key >> 4, n = key & 15;
-                u32x4 weights = p[0];
+        for (int g = max(edge - key0, 0) >> 4; g < kSub * 2; ++g)
 #pragma unroll
-                for (int i = 1; i < kSub * 2; ++i) weights = g == i ? p[i] : weights;
+            for (int d = 0; d < kBlocks; ++d) {
+                const u32x4 v = values(buffer, g, d);
 #pragma unroll
-                for (int d = 0; d < kBlocks; ++d) {
-                    u32x4 v = values(buffer, g, d);
+                for (int w = 0; w < 4; ++w) odd |= E::any_not_finite(v[w]);
+            }
+        const float top = largest();
+        if (__any(top > m + kMaxSlack)) rescale(top);
+        weights();
+        if (__builtin_expect(!__any(odd), 1)) {
+            products();
+            continue;
+        }
+        // The tile's keys one by one, to the rows that see them: the n-th of 16, which the lanes of half (n >> 2) & 1 have.
+#pragma unroll 1
+        for (int key = 0; key < kKeys; ++key) {
+            const int g = key >> 4, n = key & 15;
+            u32x4 of_key = p[0];
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) v[w] = half == ((n >> 2) & 1) && w == 2 * (n >> 3) + ((n & 3) >> 1) ? v[w] & (n & 1 ? 0xffff0000u : 0x0000ffffu) : 0u;
-                    const f32x16 more = E::mfma32(v, weights, o[d]);
+            for (int i = 1; i < kSub * 2; ++i) of_key = g == i ? p[i] : of_key;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) o[d][i] = key < most ? more[i] : o[d][i];
-                    __builtin_amdgcn_sched_barrier(0);
-                }
+            for (int d = 0; d < kBlocks; ++d) {
+                u32x4 v = values(buffer, g, d);
+#pragma unroll
+                for (int w = 0; w < 4; ++w) v[w] = half == ((n >> 2) & 1) && w == 2 * (n >> 3) + ((n & 3) >> 1) ? v[w] & (n & 1 ? 0xffff0000u : 0x0000ffffu) : 0u;
+                const f32x16 more = E::mfma32(v, of_key, o[d]);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[d][i] = key < most ? more[i] : o[d][i];
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
     }
+    // Tiles that only other waves see.
+    while (key0 < end) advance();
 
     l = sum_halves(l);
     if (!live) return;
