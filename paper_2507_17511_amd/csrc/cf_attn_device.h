@@ -32,6 +32,9 @@ constexpr float kNoMax = -3.0e38f;
 // A row's accumulators are scaled down when a score passes the maximum in use by so many powers of two.  Weights then reach 2^8 at
 // most: their rounding is relative, sums of 2^31 of them stay finite in fp32, and 2^8 is far from the largest fp16.
 constexpr float kMaxSlack = 8.0f;
+// Where the maximum is not looked for (see k_attn_prompt): the most that the weights of a lane's keys of one tile may sum up to.  No weight is
+// larger than that, so that all of them are finite in fp16.
+constexpr float kMostSum = 32768.0f;
 
 template <typename T> __device__ __forceinline__ const CF_GLOBAL T *gconst(const void *p) { return (const CF_GLOBAL T *)p; }
 template <typename T> __device__ __forceinline__ CF_GLOBAL T *gmut(void *p) { return (CF_GLOBAL T *)p; }

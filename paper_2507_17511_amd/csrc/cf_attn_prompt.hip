@@ -129,23 +129,21 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 
     const uint32_t v_from = (uint32_t)from_row * (uint32_t)a.v.token + (place ^ v_turn<D>(from_row)) * 16;
     const char *k_base = a.k.data + t.seq_k * a.k.token + kv_head * a.k.head;
     const char *v_base = a.v.data + t.seq_k * a.v.token + kv_head * a.v.head;
-    auto bring = [&](int key0, int buffer) {
-        const char *k_at = k_base + key0 * a.k.token, *v_at = v_base + key0 * a.v.token;
-        if (key0 + kKeys <= t.len_k) {
+    auto bring = [&](const char *base, int64_t stride, uint32_t from, char *to, int at) {
+        base += at * stride;
+        if (at + kKeys <= t.len_k) {
 #pragma unroll
-            for (int n = 0; n < kLoads; ++n) {
-                stage(k_at, 0xffffffffu, k_from, n * (uint32_t)(kStepRows * a.k.token), lds_k + buffer + (n * kWaves + wave) * 1024);
-                stage(v_at, 0xffffffffu, v_from, n * (uint32_t)(kStepRows * a.v.token), lds_v + buffer + (n * kWaves + wave) * 1024);
-            }
+            for (int n = 0; n < kLoads; ++n) stage(base, 0xffffffffu, from, n * (uint32_t)(kStepRows * stride), to + (n * kWaves + wave) * 1024);
         } else {            // rows past the sequence come as zeros
 #pragma unroll 1
             for (int n = 0; n < kLoads; ++n) {
-                const int rows_here = min(t.len_k - key0 - n * kStepRows, kStepRows);
-                stage(k_at + n * kStepRows * a.k.token, rows_here > 0 ? (uint32_t)(rows_here - 1) * (uint32_t)a.k.token + D * 2 : 0, k_from, 0, lds_k + buffer + (n * kWaves + wave) * 1024);
-                stage(v_at + n * kStepRows * a.v.token, rows_here > 0 ? (uint32_t)(rows_here - 1) * (uint32_t)a.v.token + D * 2 : 0, v_from, 0, lds_v + buffer + (n * kWaves + wave) * 1024);
+                const int rows_here = min(t.len_k - at - n * kStepRows, kStepRows);
+                stage(base + n * kStepRows * stride, rows_here > 0 ? (uint32_t)(rows_here - 1) * (uint32_t)stride + D * 2 : 0, from, 0, to + (n * kWaves + wave) * 1024);
             }
         }
     };
+    auto bring_k = [&](int at, int buffer) { bring(k_base, a.k.token, k_from, lds_k + buffer, at); };
+    auto bring_v = [&](int at, int buffer) { bring(v_base, a.v.token, v_from, lds_v + buffer, at); };
 
     const CF_LDS char *k_read = (const CF_LDS char *)lds_k + col * (D * 2) + ((half ^ k_turn<D>(col)) << 4);
     const int v_row = 4 * half + ((lane & 15) >> 2);
@@ -162,18 +160,20 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 
     // keys that no row of the wave sees begin here, and keys that not all of its rows see
     const int limit = min(wave_live ? wave_most : 0, split_end), edge = min(wave_least, limit);
 
-    // Two buffers: while one is worked on the next tile comes into the other.  The waves of a workgroup meet here once a tile,
-    // wherever in the loops below they are.
-    int key0 = split_begin, buffer = 0;
+    // A tile's scores are taken while the weights of the tile before are computed.  While V of tile n and K of tile n + 1 are read, V of tile
+    // n + 1 and K of tile n + 2 come, into the other buffers.  The waves of a workgroup meet here once a tile, wherever in the
+    // loops below they are.
+    int key0 = split_begin, buffer = 0;         // the tile in work, and where its V is; K of the next one is in the other buffer
     auto advance = [&]() {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");      // the next tile has come, and this one's buffer is free
-        if (key0 + 2 * kKeys < end) bring(key0 + 2 * kKeys, buffer);
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         key0 += kKeys;
         buffer ^= kTile;
+        if (key0 + kKeys < end) bring_v(key0 + kKeys, buffer ^ kTile);
+        if (key0 + 2 * kKeys < end) bring_k(key0 + 2 * kKeys, buffer);
     };
     f32x16 s[kSub];
     u32x4 p[kSub * 2];
-    auto scores = [&]() {
+    auto scores = [&](f32x16 (&s)[kSub], int buffer) {
 #pragma unroll
         for (int b = 0; b < kSub; ++b) {
 #pragma unroll
@@ -185,7 +185,7 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 
             }
         }
     };
-    auto largest = [&]() {
+    auto largest = [&](const f32x16 (&s)[kSub]) {
         float top = s[0][0];
 #pragma unroll
         for (int b = 0; b < kSub; ++b)
@@ -202,15 +202,17 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 
         l *= scale;
         m = fresh;
     };
-    auto weights = [&]() {
+    auto weights = [&]() {          // -> their sum
+        float sum = 0.0f;
 #pragma unroll
         for (int b = 0; b < kSub; ++b)
 #pragma unroll
             for (int i = 0; i < 16; i += 2) {
                 const float p0 = exp2_fast(__builtin_fmaf(s[b][i], c, -m)), p1 = exp2_fast(__builtin_fmaf(s[b][i + 1], c, -m));
-                l += p0 + p1;
+                sum += p0 + p1;
                 p[b * 2 + (i >> 3)][(i & 7) >> 1] = E::pack(p0, p1);
             }
+        return sum;
     };
     auto products = [&]() {
 #pragma unroll
@@ -220,67 +222,79 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 
     };
 
     if (key0 < end) {
-        bring(key0, 0);
+        bring_k(key0, 0);
+        bring_v(key0, 0);
+        if (key0 + kKeys < end) bring_k(key0 + kKeys, kTile);
         asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-        if (key0 + kKeys < end) bring(key0 + kKeys, kTile);
+        scores(s, 0);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");      // K's first buffer is free again
+        if (key0 + kKeys < end) bring_v(key0 + kKeys, kTile);
+        if (key0 + 2 * kKeys < end) bring_k(key0 + 2 * kKeys, 0);
     }
-    // Tiles that all rows of the wave see.  The accumulators are scaled outside of the inner loop, where the compiler keeps them in place; a tile
-    // that asks for it, most often the first alone, has its scores computed again.
-    while (key0 + kKeys <= edge) {
-        float top;
-        for (; key0 + kKeys <= edge; advance()) {
-            scores();
-            top = largest();
-            if (__any(top > m + kMaxSlack)) break;
-            weights();
+    // Tiles that all rows of the wave see, up to the last but one.  Their maximum is not looked for: weights are positive, so
+    // that none is larger than their sum.  Where that passes kMostSum, in any lane, the tile is done again after its maximum has been taken and the
+    // accumulators scaled; most often that is the first tile alone.  That happens outside of the inner loop, where the compiler keeps them in place.
+    while (key0 + 2 * kKeys <= edge) {
+        rescale(largest(s));
+        do {
+            f32x16 next[kSub];
+            scores(next, buffer ^ kTile);
+            const float sum = weights();
+            if (__any(sum > kMostSum)) break;
+            l += sum;
             products();
-        }
-        if (key0 + kKeys <= edge) rescale(top);
+#pragma unroll
+            for (int b = 0; b < kSub; ++b) s[b] = next[b];
+            advance();
+        } while (key0 + 2 * kKeys <= edge);
     }
-    // Tiles of which some rows see a part.
-    for (; key0 < limit; advance()) {
-        scores();
-        const int most = min(seen, split_end) - key0;
-#pragma unroll
-        for (int b = 0; b < kSub; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (b * 32 + 8 * (i >> 2) + (i & 3) >= most - 4 * half) s[b][i] = -__builtin_inff();
-        // A weight of zero does not keep an infinity or NaN out of a sum: is there one among the values that not all rows see?
+    // The last of them, and tiles of which some rows see a part.
+    while (key0 < limit) {
         bool odd = false;
+        const int most = min(seen, split_end) - key0;
+        if (key0 + kKeys > edge) {
+#pragma unroll
+            for (int b = 0; b < kSub; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (b * 32 + 8 * (i >> 2) + (i & 3) >= most - 4 * half) s[b][i] = -__builtin_inff();
+            // A weight of zero does not keep an infinity or NaN out of a sum: is there one among the values that not all rows see?
 #pragma unroll 1
-        for (int g = max(edge - key0, 0) >> 4; g < kSub * 2; ++g)
+            for (int g = max(edge - key0, 0) >> 4; g < kSub * 2; ++g)
 #pragma unroll
-            for (int d = 0; d < kBlocks; ++d) {
-                const u32x4 v = values(buffer, g, d);
+                for (int d = 0; d < kBlocks; ++d) {
+                    const u32x4 v = values(buffer, g, d);
 #pragma unroll
-                for (int w = 0; w < 4; ++w) odd |= E::any_not_finite(v[w]);
-            }
-        const float top = largest();
+                    for (int w = 0; w < 4; ++w) odd |= E::any_not_finite(v[w]);
+                }
+        }
+        const float top = largest(s);
         if (__any(top > m + kMaxSlack)) rescale(top);
-        weights();
+        l += weights();
         if (__builtin_expect(!__any(odd), 1)) {
             products();
-            continue;
-        }
-        // The tile's keys one by one, to the rows that see them: the n-th of 16, which the lanes of half (n >> 2) & 1 have.
+        } else {
+            // The tile's keys one by one, to the rows that see them: the n-th of 16, which the lanes of half (n >> 2) & 1 have.
 #pragma unroll 1
-        for (int key = 0; key < kKeys; ++key) {
-            const int g = key >> 4, n = key & 15;
-            u32x4 of_key = p[0];
+            for (int key = 0; key < kKeys; ++key) {
+                const int g = key >> 4, n = key & 15;
+                u32x4 of_key = p[0];
 #pragma unroll
-            for (int i = 1; i < kSub * 2; ++i) of_key = g == i ? p[i] : of_key;
+                for (int i = 1; i < kSub * 2; ++i) of_key = g == i ? p[i] : of_key;
 #pragma unroll
-            for (int d = 0; d < kBlocks; ++d) {
-                u32x4 v = values(buffer, g, d);
+                for (int d = 0; d < kBlocks; ++d) {
+                    u32x4 v = values(buffer, g, d);
 #pragma unroll
-                for (int w = 0; w < 4; ++w) v[w] = half == ((n >> 2) & 1) && w == 2 * (n >> 3) + ((n & 3) >> 1) ? v[w] & (n & 1 ? 0xffff0000u : 0x0000ffffu) : 0u;
-                const f32x16 more = E::mfma32(v, of_key, o[d]);
+                    for (int w = 0; w < 4; ++w) v[w] = half == ((n >> 2) & 1) && w == 2 * (n >> 3) + ((n & 3) >> 1) ? v[w] & (n & 1 ? 0xffff0000u : 0x0000ffffu) : 0u;
+                    const f32x16 more = E::mfma32(v, of_key, o[d]);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) o[d][i] = key < most ? more[i] : o[d][i];
-                __builtin_amdgcn_sched_barrier(0);
+                    for (int i = 0; i < 16; ++i) o[d][i] = key < most ? more[i] : o[d][i];
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
         }
+        if (key0 + kKeys < limit) scores(s, buffer ^ kTile);
+        advance();
     }
     // Tiles that only other waves see.
     while (key0 < end) advance();
