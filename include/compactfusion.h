@@ -398,10 +398,12 @@ typedef struct {
     float *lse;           /* [n_q][q_heads], dense: natural log of the sum of exp(score) over a row's keys; may be null */
 } cf_prompt;
 
-/* Most that cf_attn_prompt and cf_attn_paged use of a workspace (256-byte aligned device memory; its contents need not be kept
- * or set).  Where there are few rows and many keys the keys are split and the parts meet in the workspace; a smaller one,
- * or none (null, 0), allows fewer parts.  The bits of a result depend on the split, and so on the size given. */
+/* Most that cf_attn_prompt and cf_attn_paged use of a workspace: 256-byte aligned device memory whose first
+ * CF_ATTN_COUNTER_BYTES are zero before the first call that is given it; every call leaves them zero, and nothing else of it
+ * need be kept or set.  Where there are few rows and many keys the keys are split and the parts meet in the workspace; a smaller
+ * one, or none (null, 0), allows fewer parts.  The bits of a result depend on the split, and so on the size given. */
 #define CF_ATTN_WORKSPACE_BYTES ((size_t)64 << 20)
+#define CF_ATTN_COUNTER_BYTES ((size_t)256 << 10)
 
 /* out = softmax(scale q k^T) v, sequence by sequence.  Rows outside all sequences are not written. */
 cf_status cf_attn_prompt(const cf_attn_desc *desc, const cf_prompt *args, void *workspace, size_t workspace_bytes, void *stream);

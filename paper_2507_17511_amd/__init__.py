@@ -300,6 +300,7 @@ def cf_given_up_items(ctx, stream=None) -> int:
 # ---------------------------------------------------------------- attention over keys and values
 
 CF_ATTN_WORKSPACE_BYTES = 64 << 20
+CF_ATTN_COUNTER_BYTES = 256 << 10
 CF_JOIN_MAX_PARTS = 64
 
 

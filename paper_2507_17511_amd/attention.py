@@ -8,6 +8,7 @@ strided (slices of a wider projection).  Calls enqueue work on the session's str
 from __future__ import annotations
 
 import ctypes
+import struct
 from typing import Optional, Sequence
 
 import torch
@@ -15,6 +16,17 @@ import torch
 import paper_2507_17511_amd as cf
 
 _CF_DT = {torch.bfloat16: cf.CF_BF16, torch.float16: cf.CF_F16, torch.float32: cf.CF_F32}
+
+# The arguments of a call, as one struct.pack_into writes them: filling a ctypes structure field by field takes several times as long
+# as the call itself.  A cf_rows is "Pqq".
+_APPEND = struct.Struct("@q Pqq Pqq P Pqq Pqq PPP q ii")
+_PROMPT = struct.Struct("@ii qqq PP Pqq Pqq Pqq Pqq P")
+_PAGED = struct.Struct("@ii qq PP Pqq Pqq P")
+_JOIN = struct.Struct("@ii q PP Pqq P")
+for _layout, _args in ((_APPEND, cf.cf_append), (_PROMPT, cf.cf_prompt), (_PAGED, cf.cf_paged), (_JOIN, cf.cf_join)):
+    assert _layout.size == ctypes.sizeof(_args), _args
+
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # device index -> hipStream_t, without a Stream object
 
 
 def _require(ok: bool, what: str) -> None:
@@ -32,7 +44,7 @@ class PagedCache:
         for x in (k, v):
             _require(x.numel() > 0 and x[0].is_contiguous() and (pages == 1 or x.stride(0) == k.stride(0)), "pages are dense, and as far apart in k as in v")
         self.k, self.v = k, v
-        self.page_size = page
+        self.heads, self.page_size, self.head_dim, self.dtype, self.device = heads, page, dim, k.dtype, k.device
         self.struct = cf.cf_kv_cache(k.data_ptr(), v.data_ptr(), pages, k.stride(0) if pages > 1 else 0, page)
 
     @classmethod
@@ -55,31 +67,37 @@ class AttentionSession:
             self.device = torch.device("cuda", torch.cuda.current_device())
         self.desc = cf.cf_attn_desc(_CF_DT[dtype], q_heads, kv_heads, head_dim, scale)
         self.ws_bytes = workspace_bytes
-        self.workspace = torch.empty(workspace_bytes, dtype=torch.uint8, device=self.device) if workspace_bytes else None
+        self.workspace = torch.zeros(workspace_bytes, dtype=torch.uint8, device=self.device) if workspace_bytes else None
         self._ws = self.workspace.data_ptr() if workspace_bytes else None
         self._stream = stream
+        self._args = {x: x() for x in (cf.cf_append, cf.cf_prompt, cf.cf_paged, cf.cf_join)}
 
     def _on(self) -> int:
-        s = self._stream if self._stream is not None else torch.cuda.current_stream(self.device)
-        return s.cuda_stream
+        if self._stream is not None:
+            return self._stream.cuda_stream
+        if _raw_stream is not None:
+            return _raw_stream(self.device.index)
+        return torch.cuda.current_stream(self.device).cuda_stream
 
-    def _rows(self, x: torch.Tensor, heads: int, name: str) -> cf.cf_rows:
-        if x.dim() != 3 or x.shape[1] != heads or x.shape[2] != self.head_dim or x.dtype != self.dtype or x.device != self.device:
-            raise ValueError(f"{name} is [tokens, {heads}, {self.head_dim}] of {self.dtype} on {self.device}: got {tuple(x.shape)} of {x.dtype} on {x.device}")
-        token, head, last = x.stride()
-        if last != 1:
-            raise ValueError(f"{name}: the elements of a head lie next to one another")
-        return cf.cf_rows(x.data_ptr(), token, head)
+    def _rows(self, x: torch.Tensor, tokens: int, heads: int, name: str):
+        """-> data, token stride, head stride."""
+        if x.dim() == 3:
+            n, h, d = x.shape
+            token, head, last = x.stride()
+            if n == tokens and h == heads and d == self.head_dim and last == 1 and x.dtype is self.dtype and x.device == self.device:
+                return x.data_ptr(), token, head
+        raise ValueError(f"{name} is [{tokens}, {heads}, {self.head_dim}] of {self.dtype} on {self.device}, the elements of a head next to one another: "
+                         f"got {tuple(x.shape)} of {x.dtype} on {x.device}, strides {x.stride()}")
 
     def _plain(self, x: torch.Tensor, dtype: torch.dtype, shape, name: str) -> int:
-        if x.dtype != dtype or x.device != self.device or tuple(x.shape) != tuple(shape) or not x.is_contiguous():
+        if x.dtype is not dtype or x.shape != shape or not x.is_contiguous() or x.device != self.device:
             raise ValueError(f"{name} is dense {tuple(shape)} of {dtype} on {self.device}: got {tuple(x.shape)} of {x.dtype} on {x.device}")
         return x.data_ptr()
 
-    def _cache(self, cache: PagedCache) -> cf.cf_kv_cache:
-        k = cache.k
-        if k.shape[1] != self.kv_heads or k.shape[3] != self.head_dim or k.dtype != self.dtype or k.device != self.device:
-            raise ValueError(f"the cache has {self.kv_heads} heads of {self.head_dim} of {self.dtype} on {self.device}: got {tuple(k.shape)} of {k.dtype} on {k.device}")
+    def _cache(self, cache: "PagedCache") -> cf.cf_kv_cache:
+        if cache.heads != self.kv_heads or cache.head_dim != self.head_dim or cache.dtype is not self.dtype or cache.device != self.device:
+            raise ValueError(f"the cache has {self.kv_heads} heads of {self.head_dim} of {self.dtype} on {self.device}: got {cache.heads} of "
+                             f"{cache.head_dim} of {cache.dtype} on {cache.device}")
         return cache.struct
 
     def append(self, cache: PagedCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, positions: Optional[torch.Tensor] = None,
@@ -89,21 +107,24 @@ class AttentionSession:
         [n_positions, rotary_dim / 2] (fp32); without positions nothing is rotated.  Returns the rotated queries, if any: in q_out,
         which may be q."""
         n = k.shape[0]
-        a = cf.cf_append(n_tokens=n, k=self._rows(k, self.kv_heads, "k"), v=self._rows(v, self.kv_heads, "v"),
-                         slots=self._plain(slots, torch.int64, (n,), "slots"))
-        _require(v.shape[0] == n, "k and v have as many tokens")
+        rows_q = rows_out = (0, 0, 0)
         if q is not None:
             if q_out is None:
                 q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-            a.q, a.q_out = self._rows(q, self.q_heads, "q"), self._rows(q_out, self.q_heads, "q_out")
-            _require(q.shape[0] == n and q_out.shape[0] == n, "q and q_out have as many tokens as k")
-        else:
-            _require(q_out is None, "q_out goes with q")
+            rows_q = self._rows(q, n, self.q_heads, "q")
+            rows_out = rows_q if q_out is q else self._rows(q_out, n, self.q_heads, "q_out")
+        elif q_out is not None:
+            raise ValueError("q_out goes with q")
+        at = table = (0, 0, 0)
         if positions is not None:
             _require(cos is not None and sin is not None and cos.dim() == 2, "positions go with cos and sin [n_positions, rotary_dim / 2]")
-            a.positions = self._plain(positions, torch.int32, (n,), "positions")
-            a.cos, a.sin = self._plain(cos, torch.float32, cos.shape, "cos"), self._plain(sin, torch.float32, cos.shape, "sin")
-            a.n_positions, a.rotary_dim, a.interleaved = cos.shape[0], 2 * cos.shape[1], int(interleaved)
+            shape = cos.shape
+            at = (self._plain(positions, torch.int32, (n,), "positions"), self._plain(cos, torch.float32, shape, "cos"),
+                  self._plain(sin, torch.float32, shape, "sin"))
+            table = (shape[0], 2 * shape[1], interleaved)
+        a = self._args[cf.cf_append]
+        _APPEND.pack_into(a, 0, n, *self._rows(k, n, self.kv_heads, "k"), *self._rows(v, n, self.kv_heads, "v"),
+                          self._plain(slots, torch.int64, (n,), "slots"), *rows_q, *rows_out, *at, *table)
         cf.cf_kv_append(self.desc, self._cache(cache), a, self._on())
         return q_out
 
@@ -112,16 +133,14 @@ class AttentionSession:
         """Attention of packed sequences: sequence b has rows cu_q[b] .. cu_q[b + 1] of q and cu_k[b] .. of k and v (int32; cu_k is
         cu_q if not given).  `lse`: fp32 [tokens, q_heads], filled with the rows' log-sum-exps.  max_k: keys of the longest sequence, a hint."""
         cu_k = cu_q if cu_k is None else cu_k
-        n = cu_q.shape[0] - 1
-        _require(n >= 0 and v.shape[0] == k.shape[0], "cu_q has an entry more than there are sequences; k and v have as many tokens")
+        n, n_q, n_k = cu_q.shape[0] - 1, q.shape[0], k.shape[0]
+        _require(n >= 0, "cu_q has an entry more than there are sequences")
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        _require(out.shape[0] == q.shape[0], "out has as many tokens as q")
-        a = cf.cf_prompt(n, int(causal), q.shape[0], k.shape[0], max_k, self._plain(cu_q, torch.int32, (n + 1,), "cu_q"),
-                         self._plain(cu_k, torch.int32, (n + 1,), "cu_k"), self._rows(q, self.q_heads, "q"), self._rows(k, self.kv_heads, "k"),
-                         self._rows(v, self.kv_heads, "v"), self._rows(out, self.q_heads, "out"))
-        if lse is not None:
-            a.lse = self._plain(lse, torch.float32, (q.shape[0], self.q_heads), "lse")
+        a = self._args[cf.cf_prompt]
+        _PROMPT.pack_into(a, 0, n, causal, n_q, n_k, max_k, self._plain(cu_q, torch.int32, (n + 1,), "cu_q"), self._plain(cu_k, torch.int32, (n + 1,), "cu_k"),
+                          *self._rows(q, n_q, self.q_heads, "q"), *self._rows(k, n_k, self.kv_heads, "k"), *self._rows(v, n_k, self.kv_heads, "v"),
+                          *self._rows(out, n_q, self.q_heads, "out"), 0 if lse is None else self._plain(lse, torch.float32, (n_q, self.q_heads), "lse"))
         cf.cf_attn_prompt(self.desc, a, self._ws, self.ws_bytes, self._on())
         return out
 
@@ -132,12 +151,14 @@ class AttentionSession:
         n = q.shape[0]
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        _require(out.shape[0] == n and table.dim() == 2 and table.shape[0] == n and table.dtype == torch.int32 and table.device == self.device
-                 and (table.shape[1] == 1 or table.stride(1) == 1), "out is as q; table is [sequences, pages] int32, its rows dense")
-        a = cf.cf_paged(n, table.shape[1], table.stride(0) if n > 1 else 0, max_len, table.data_ptr(), self._plain(lens, torch.int32, (n,), "lens"),
-                        self._rows(q, self.q_heads, "q"), self._rows(out, self.q_heads, "out"))
-        if lse is not None:
-            a.lse = self._plain(lse, torch.float32, (n, self.q_heads), "lse")
+        _require(table.dim() == 2 and table.shape[0] == n and table.dtype is torch.int32 and table.device == self.device, "table is [sequences, pages] int32")
+        row, entry = table.stride()
+        cols = table.shape[1]
+        _require(cols == 1 or entry == 1, "the rows of table are dense")
+        a = self._args[cf.cf_paged]
+        _PAGED.pack_into(a, 0, n, cols, row if n > 1 else 0, max_len, table.data_ptr(), self._plain(lens, torch.int32, (n,), "lens"),
+                         *self._rows(q, n, self.q_heads, "q"), *self._rows(out, n, self.q_heads, "out"),
+                         0 if lse is None else self._plain(lse, torch.float32, (n, self.q_heads), "lse"))
         cf.cf_attn_paged(self.desc, self._cache(cache), a, self._ws, self.ws_bytes, self._on())
         return out
 
@@ -145,17 +166,18 @@ class AttentionSession:
              lse: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Attention over the union of disjoint sets of keys: parts [tokens, q_heads, head_dim], all of the session's dtype or all fp32,
         and their log-sum-exps."""
-        _require(len(parts) > 0 and len(parts) == len(lses), "a log-sum-exp for every part, and one part at least")
+        n = len(parts)
+        _require(n > 0 and n == len(lses), "a log-sum-exp for every part, and one part at least")
         shape, pdt = parts[0].shape, parts[0].dtype
-        _require(len(shape) == 3 and shape[1] == self.q_heads and shape[2] == self.head_dim and pdt in (self.dtype, torch.float32),
+        _require(len(shape) == 3 and shape[1] == self.q_heads and shape[2] == self.head_dim and (pdt is self.dtype or pdt is torch.float32),
                  f"parts are [tokens, {self.q_heads}, {self.head_dim}] of {self.dtype} or torch.float32")
+        tokens = shape[0]
         if out is None:
             out = torch.empty(shape, dtype=self.dtype, device=self.device)
-        _require(out.shape[0] == shape[0], "out has as many tokens as the parts")
-        p = (ctypes.c_void_p * len(parts))(*[self._plain(x, pdt, shape, "a part") for x in parts])
-        s = (ctypes.c_void_p * len(parts))(*[self._plain(x, torch.float32, shape[:2], "a log-sum-exp") for x in lses])
-        a = cf.cf_join(len(parts), _CF_DT[pdt], shape[0], p, s, self._rows(out, self.q_heads, "out"))
-        if lse is not None:
-            a.lse = self._plain(lse, torch.float32, shape[:2], "lse")
+        p = (ctypes.c_void_p * n)(*[self._plain(x, pdt, shape, "a part") for x in parts])
+        s = (ctypes.c_void_p * n)(*[self._plain(x, torch.float32, shape[:2], "a log-sum-exp") for x in lses])
+        a = self._args[cf.cf_join]
+        _JOIN.pack_into(a, 0, n, _CF_DT[pdt], tokens, ctypes.addressof(p), ctypes.addressof(s), *self._rows(out, tokens, self.q_heads, "out"),
+                        0 if lse is None else self._plain(lse, torch.float32, shape[:2], "lse"))
         cf.cf_attn_join(self.desc, a, self._on())
         return out

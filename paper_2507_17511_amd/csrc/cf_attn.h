@@ -56,7 +56,9 @@ struct PagedArgs {
     int64_t table_stride;
     int32_t n_seqs, max_pages;
     int32_t n_splits, split_keys;
-    Parts parts;
+    int32_t join_after;             // the parts are joined by a kernel of its own, which reads parts.lse of all splits, in natural logarithms
+    uint32_t *counters;             // one for every (sequence, unit of heads): parts that have landed; zero between calls
+    Parts parts;                    // without join_after its log-sum-exps are of powers of two
 };
 
 struct JoinArgs {

@@ -8,12 +8,26 @@
 
 using namespace cf::attn;
 
+#ifndef PAGED_WGS
+#define PAGED_WGS 2
+#endif
+#ifndef PAGED_MOST
+#define PAGED_MOST 1024
+#endif
+#ifndef PAGED_AFTER
+#define PAGED_AFTER 4
+#endif
+#ifndef PAGED_LEAST
+#define PAGED_LEAST 128
+#endif
+
 namespace {
 
 constexpr int64_t kMostStride = (int64_t)1 << 24;       // elements: a tile's rows are addressed with 32 bits
 constexpr int64_t kMostRows = (int64_t)1 << 30;
 constexpr int64_t kMostGrid = ((int64_t)1 << 31) - 1;
 constexpr int64_t kCUs = 256;
+constexpr int64_t kCounters = CF_ATTN_COUNTER_BYTES / sizeof(uint32_t);
 
 bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
@@ -101,16 +115,16 @@ cf_status check_workspace(const void *workspace, size_t bytes)
     return aligned(workspace, 256) ? CF_OK : CF_ERR_WORKSPACE;
 }
 
-// How many parts of `rows` rows fit the workspace.
+// How many parts of `rows` rows fit the workspace, behind the counters.
 int64_t parts_that_fit(size_t bytes, int64_t rows, int dim)
 {
     if (bytes > CF_ATTN_WORKSPACE_BYTES) bytes = CF_ATTN_WORKSPACE_BYTES;
-    return (int64_t)bytes / (rows * (dim + 1) * (int64_t)sizeof(float));
+    return bytes > CF_ATTN_COUNTER_BYTES ? (int64_t)(bytes - CF_ATTN_COUNTER_BYTES) / (rows * (dim + 1) * (int64_t)sizeof(float)) : 0;
 }
 
 void place_parts(Parts &p, void *workspace, int64_t rows, int64_t n, int dim)
 {
-    p.o = static_cast<float *>(workspace);
+    p.o = reinterpret_cast<float *>(static_cast<char *>(workspace) + CF_ATTN_COUNTER_BYTES);
     p.lse = p.o + n * rows * dim;
     p.n_rows = rows;
 }
@@ -260,12 +274,13 @@ cf_status cf_attn_paged(const cf_attn_desc *desc, const cf_kv_cache *cache, cons
     if (longest > kMostRows) longest = kMostRows;
     const int64_t units = args->n_seqs * (int64_t)a.h.kv_heads * ((a.h.group + kPagedHeads - 1) / kPagedHeads);
     const int64_t rows = (int64_t)args->n_seqs * a.h.q_heads;
-    int64_t keys = round_up((longest * units + 8 * kCUs - 1) / (8 * kCUs), 128);
-    if (keys < 256) keys = 256;
-    if (keys > 2048) keys = 2048;
+    int64_t keys = round_up((longest * units + PAGED_WGS * kCUs - 1) / (PAGED_WGS * kCUs), 128);
+    if (keys < PAGED_LEAST) keys = PAGED_LEAST;
+    if (units >= 8 && keys < longest / 32) keys = round_up(longest / 32, 128);
+    if (keys > PAGED_MOST) keys = PAGED_MOST;
     int64_t splits = (longest + keys - 1) / keys;
     const int64_t fit = parts_that_fit(workspace_bytes, rows, a.h.head_dim);
-    if (splits > fit) splits = fit;
+    if (splits > fit || units > kCounters) splits = units > kCounters ? 1 : fit;
     if (splits > kMaxParts) splits = kMaxParts;
     a.n_splits = 1;
     a.split_keys = (int32_t)kMostRows;
@@ -275,9 +290,11 @@ cf_status cf_attn_paged(const cf_attn_desc *desc, const cf_kv_cache *cache, cons
     }
     if (units * a.n_splits > kMostGrid) return CF_ERR_SHAPE;
     if (a.n_splits > 1) place_parts(a.parts, workspace, rows, a.n_splits, a.h.head_dim);
+    a.counters = static_cast<uint32_t *>(workspace);
+    a.join_after = a.n_splits > 1 && units * a.n_splits > PAGED_AFTER * kCUs;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     hipError_t e = launch_paged(a, s);
-    if (e == hipSuccess && a.n_splits > 1) e = join_parts(a.h, a.parts, a.n_splits, a.out, a.lse, nullptr, 0, s);
+    if (e == hipSuccess && a.join_after) e = join_parts(a.h, a.parts, a.n_splits, a.out, a.lse, nullptr, 0, s);
     return status_of(e);
 }
 

@@ -302,6 +302,11 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 
     l = sum_halves(l);
     if (!live) return;
     const float inv = inverse_of(l);
+    if (l == 0.0f)              // no key, or none with a score above -infinity: 0 times an infinite value is none of the row's
+#pragma unroll
+        for (int d = 0; d < kBlocks; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
     const int64_t at = (t.seq_q + (int64_t)token) * a.h.q_heads + head;
     if (a.n_splits > 1) {
         float *dst = a.parts.o + ((int64_t)split * a.parts.n_rows + at) * D;

@@ -81,41 +81,85 @@ template <int DT, int D> __global__ __launch_bounds__(256) void k_kv_append(Appe
 
 // ---------------------------------------------------------------- join
 //
-// A lane has 8 elements of a row and computes that row's weights for itself: the log-sum-exps of a row are read by the
-// lanes of that row together, and from the cache after the first.
-template <int DT, int PT, int D> __global__ __launch_bounds__(256) void k_attn_join(JoinArgs a)
+// A lane has 8 elements of a row of every SPREAD-th part, and computes the weights of these parts for itself: the log-sum-exps of a row are
+// read by the lanes of that row together, and from the cache after the first.  Where there are many parts of few rows, SPREAD lanes
+// share an element, and their sums meet in LDS.
+constexpr int kFewParts = 4;
+
+template <int DT, int PT, int D, int SPREAD> __global__ __launch_bounds__(256) void k_attn_join(JoinArgs a)
 {
-    constexpr int kLanes = D / 8;
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t row = id / kLanes;
-    if (row >= a.n_rows) return;
-    const int lane = (int)(id % kLanes);
-    const int64_t token = row / a.h.q_heads;
-    if (a.cover && (token < gconst<int32_t>(a.cover)[0] || token >= gconst<int32_t>(a.cover)[a.n_cover])) return;
-    float top = -__builtin_inff();
-    for (int p = 0; p < a.n_parts; ++p) top = fmaxf(top, gconst<float>(a.lses[p])[row]);
-    const float base = top == -__builtin_inff() ? 0.0f : top;
-    float total = 0.0f, o[8] = {};
-    for (int p = 0; p < a.n_parts; ++p) {
-        const float lse = gconst<float>(a.lses[p])[row];
-        if (lse == -__builtin_inff()) continue;
-        const float w = exp2_fast((lse - base) * 1.44269504088896341f);
-        total += w;
+    constexpr int kLanes = D / 8;                       // of a row
+    constexpr int kRows = 256 / (kLanes * SPREAD);      // of a workgroup
+    static_assert(kRows >= 1, "a workgroup has a row at least");
+    const int row_here = threadIdx.x / (kLanes * SPREAD), share = threadIdx.x / kLanes % SPREAD, lane = threadIdx.x % kLanes;
+    const int64_t row = (int64_t)blockIdx.x * kRows + row_here;
+    const bool there = row < a.n_rows;
+    const int64_t token = (there ? row : 0) / a.h.q_heads;
+    float top = -__builtin_inff(), total = 0.0f, o[8] = {}, base = 0.0f;
+    auto weight = [&](float lse) { return exp2_fast((lse - base) * 1.44269504088896341f); };
+    auto load = [&](int p, f32x4 &x, f32x4 &y) {
         if constexpr (PT == 0) {
             const CF_GLOBAL f32x4 *src = gconst<f32x4>(static_cast<const float *>(a.parts[p]) + row * D + lane * 8);
-            const f32x4 x = src[0], y = src[1];
-            for (int k = 0; k < 4; ++k) {
-                o[k] = __builtin_fmaf(w, x[k], o[k]);
-                o[4 + k] = __builtin_fmaf(w, y[k], o[4 + k]);
-            }
+            x = src[0], y = src[1];
         } else {
-            const u32x4 x = *gconst<u32x4>(static_cast<const uint16_t *>(a.parts[p]) + row * D + lane * 8);
-            for (int k = 0; k < 4; ++k) {
-                o[2 * k] = __builtin_fmaf(w, Elem<DT>::lo(x[k]), o[2 * k]);
-                o[2 * k + 1] = __builtin_fmaf(w, Elem<DT>::hi(x[k]), o[2 * k + 1]);
+            const u32x4 v = *gconst<u32x4>(static_cast<const uint16_t *>(a.parts[p]) + row * D + lane * 8);
+            x = (f32x4){Elem<DT>::lo(v[0]), Elem<DT>::hi(v[0]), Elem<DT>::lo(v[1]), Elem<DT>::hi(v[1])};
+            y = (f32x4){Elem<DT>::lo(v[2]), Elem<DT>::hi(v[2]), Elem<DT>::lo(v[3]), Elem<DT>::hi(v[3])};
+        }
+    };
+    auto add = [&](float lse, const f32x4 &x, const f32x4 &y) {
+        const float w = lse == -__builtin_inff() ? 0.0f : weight(lse);
+        total += w;
+        for (int k = 0; k < 4; ++k) {
+            o[k] = lse == -__builtin_inff() ? o[k] : __builtin_fmaf(w, x[k], o[k]);
+            o[4 + k] = lse == -__builtin_inff() ? o[4 + k] : __builtin_fmaf(w, y[k], o[4 + k]);
+        }
+    };
+    if constexpr (SPREAD == 1) {                        // all loads at once
+        float lse[kFewParts];
+        f32x4 x[kFewParts], y[kFewParts];
+        if (there) {
+#pragma unroll
+            for (int p = 0; p < kFewParts; ++p) {
+                lse[p] = -__builtin_inff();
+                if (p < a.n_parts) {
+                    lse[p] = gconst<float>(a.lses[p])[row];
+                    load(p, x[p], y[p]);
+                }
             }
+#pragma unroll
+            for (int p = 0; p < kFewParts; ++p) top = fmaxf(top, lse[p]);
+            base = top == -__builtin_inff() ? 0.0f : top;
+#pragma unroll
+            for (int p = 0; p < kFewParts; ++p)
+                if (p < a.n_parts) add(lse[p], x[p], y[p]);
+        }
+    } else if (there) {
+        for (int p = 0; p < a.n_parts; ++p) top = fmaxf(top, gconst<float>(a.lses[p])[row]);
+        base = top == -__builtin_inff() ? 0.0f : top;
+        for (int p = share; p < a.n_parts; p += SPREAD) {
+            const float lse = gconst<float>(a.lses[p])[row];
+            if (lse == -__builtin_inff()) continue;     // its output is not read
+            f32x4 x, y;
+            load(p, x, y);
+            add(lse, x, y);
         }
     }
+    if constexpr (SPREAD > 1) {
+        __shared__ float sums[256][9];
+        for (int k = 0; k < 8; ++k) sums[threadIdx.x][k] = o[k];
+        sums[threadIdx.x][8] = total;
+        for (int w = SPREAD / 2; w > 0; w >>= 1) {
+            __syncthreads();
+            if (share < w) {
+                for (int k = 0; k < 8; ++k) sums[threadIdx.x][k] = o[k] += sums[threadIdx.x + w * kLanes][k];
+                sums[threadIdx.x][8] = total += sums[threadIdx.x + w * kLanes][8];
+            }
+        }
+        if (share > 0) return;
+    }
+    if (!there) return;
+    if (a.cover && (token < gconst<int32_t>(a.cover)[0] || token >= gconst<int32_t>(a.cover)[a.n_cover])) return;
     const float inv = inverse_of(total);
     u32x4 r;
     for (int k = 0; k < 4; ++k) r[k] = Elem<DT>::pack(o[2 * k] * inv, o[2 * k + 1] * inv);
@@ -124,15 +168,26 @@ template <int DT, int PT, int D> __global__ __launch_bounds__(256) void k_attn_j
     if (a.lse && lane == 0) gmut<float>(a.lse)[row] = total > 0.0f || total != total ? base + __log2f(total) * kLn2 : -__builtin_inff();
 }
 
+template <int DT, int PT, int D, int SPREAD> hipError_t join_spread(const JoinArgs &a, hipStream_t s)
+{
+    constexpr int kRows = 256 / (D / 8 * SPREAD);
+    hipLaunchKernelGGL((k_attn_join<DT, PT, D, SPREAD>), dim3((unsigned)((a.n_rows + kRows - 1) / kRows)), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
+template <int DT, int PT, int D> hipError_t join_dim(const JoinArgs &a, hipStream_t s)
+{
+    if (a.n_parts > kFewParts) return join_spread<DT, PT, D, 256 / (D / 8)>(a, s);
+    return join_spread<DT, PT, D, 1>(a, s);
+}
+
 template <int DT, int PT> hipError_t join_typed(const JoinArgs &a, hipStream_t s)
 {
-    const unsigned grid = (unsigned)((a.n_rows * (a.h.head_dim / 8) + 255) / 256);
     switch (a.h.head_dim) {
-    case 64: hipLaunchKernelGGL((k_attn_join<DT, PT, 64>), dim3(grid), dim3(256), 0, s, a); break;
-    case 128: hipLaunchKernelGGL((k_attn_join<DT, PT, 128>), dim3(grid), dim3(256), 0, s, a); break;
-    default: hipLaunchKernelGGL((k_attn_join<DT, PT, 256>), dim3(grid), dim3(256), 0, s, a); break;
+    case 64: return join_dim<DT, PT, 64>(a, s);
+    case 128: return join_dim<DT, PT, 128>(a, s);
+    default: return join_dim<DT, PT, 256>(a, s);
     }
-    return hipGetLastError();
 }
 
 template <int DT> hipError_t append_typed(const AppendArgs &a, hipStream_t s)
