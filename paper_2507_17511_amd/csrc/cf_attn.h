@@ -35,6 +35,7 @@ struct Parts {
 
 constexpr int kPromptRows = 128;    // query rows (token, head of the group) of a workgroup
 constexpr int kPagedHeads = 16;     // query heads of a workgroup: the columns of a 16 x 16 product
+constexpr int kMostListed = 2048;   // sequences whose parts a workgroup lists
 constexpr int kMaxParts = 64;       // CF_JOIN_MAX_PARTS
 
 struct PromptArgs {
@@ -56,9 +57,9 @@ struct PagedArgs {
     int64_t table_stride;
     int32_t n_seqs, max_pages;
     int32_t n_splits, split_keys;
-    int32_t join_after;             // the parts are joined by a kernel of its own, which reads parts.lse of all splits, in natural logarithms
+    int32_t many;                   // more parts than workgroups; they are joined by a kernel of its own
     uint32_t *counters;             // one for every (sequence, unit of heads): parts that have landed; zero between calls
-    Parts parts;                    // without join_after its log-sum-exps are of powers of two
+    Parts parts;                    // its log-sum-exps are of powers of two unless `many`
 };
 
 struct JoinArgs {
@@ -70,6 +71,8 @@ struct JoinArgs {
     int32_t part_dtype;             // cf_dtype
     const int32_t *cover;           // if set, only the tokens from cover[0] to cover[n_cover] are joined
     int32_t n_cover;
+    const int32_t *lens;            // if set, token t has max(1, min(ceil(lens[t] / split_keys), n_parts)) parts, and one of one part is done already
+    int32_t split_keys;
     const void *parts[kMaxParts];
     const float *lses[kMaxParts];
 };

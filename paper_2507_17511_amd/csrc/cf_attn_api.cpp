@@ -8,19 +8,6 @@
 
 using namespace cf::attn;
 
-#ifndef PAGED_WGS
-#define PAGED_WGS 2
-#endif
-#ifndef PAGED_MOST
-#define PAGED_MOST 1024
-#endif
-#ifndef PAGED_AFTER
-#define PAGED_AFTER 4
-#endif
-#ifndef PAGED_LEAST
-#define PAGED_LEAST 128
-#endif
-
 namespace {
 
 constexpr int64_t kMostStride = (int64_t)1 << 24;       // elements: a tile's rows are addressed with 32 bits
@@ -131,7 +118,7 @@ void place_parts(Parts &p, void *workspace, int64_t rows, int64_t n, int dim)
 
 cf_status status_of(hipError_t e) { return e == hipSuccess ? CF_OK : CF_ERR_DEVICE; }
 
-hipError_t join_parts(const Heads &h, const Parts &p, int n, const Rows &out, float *lse, const int32_t *cover, int32_t n_cover, hipStream_t s)
+JoinArgs parts_to_join(const Heads &h, const Parts &p, int n, const Rows &out, float *lse)
 {
     JoinArgs j = {};
     j.h = h;
@@ -140,13 +127,11 @@ hipError_t join_parts(const Heads &h, const Parts &p, int n, const Rows &out, fl
     j.n_rows = p.n_rows;
     j.n_parts = n;
     j.part_dtype = CF_F32;
-    j.cover = cover;
-    j.n_cover = n_cover;
     for (int i = 0; i < n; ++i) {
         j.parts[i] = p.o + i * p.n_rows * h.head_dim;
         j.lses[i] = p.lse + i * p.n_rows;
     }
-    return launch_join(j, s);
+    return j;
 }
 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
@@ -241,7 +226,12 @@ cf_status cf_attn_prompt(const cf_attn_desc *desc, const cf_prompt *args, void *
     if (a.n_splits > 1) place_parts(a.parts, workspace, rows, a.n_splits, a.h.head_dim);
     const hipStream_t s = static_cast<hipStream_t>(stream);
     hipError_t e = launch_prompt(a, s);
-    if (e == hipSuccess && a.n_splits > 1) e = join_parts(a.h, a.parts, a.n_splits, a.out, a.lse, a.cu_q, a.n_seqs, s);
+    if (e == hipSuccess && a.n_splits > 1) {
+        JoinArgs j = parts_to_join(a.h, a.parts, a.n_splits, a.out, a.lse);
+        j.cover = a.cu_q;
+        j.n_cover = a.n_seqs;
+        e = launch_join(j, s);
+    }
     return status_of(e);
 }
 
@@ -274,13 +264,17 @@ cf_status cf_attn_paged(const cf_attn_desc *desc, const cf_kv_cache *cache, cons
     if (longest > kMostRows) longest = kMostRows;
     const int64_t units = args->n_seqs * (int64_t)a.h.kv_heads * ((a.h.group + kPagedHeads - 1) / kPagedHeads);
     const int64_t rows = (int64_t)args->n_seqs * a.h.q_heads;
-    int64_t keys = round_up((longest * units + PAGED_WGS * kCUs - 1) / (PAGED_WGS * kCUs), 128);
-    if (keys < PAGED_LEAST) keys = PAGED_LEAST;
-    if (units >= 8 && keys < longest / 32) keys = round_up(longest / 32, 128);
-    if (keys > PAGED_MOST) keys = PAGED_MOST;
+    // Two workgroups a CU, of 128 to 2048 keys each, and 32 parts at most where that gives every CU one: a part costs its join about 0.1 us, 128
+    // keys a workgroup 1.2 us.  us, on one card: 1 x 901 keys, 2 heads of keys: parts of 128 / 256 / 512 keys 8.2 / 9.6 / 11.4; 1 x 8192, 8 heads: 128 / 256
+    // / 512 16.7 / 13.0 / 13.6; 8 x 8192, 8 heads: two / three / six workgroups a CU 45 / 49 / 53; 64 x 7 to 700: 14.5 / 18.1 / 16.1; 96 x 160 to
+    // 16000, 8 heads: parts of 512 / 1024 / 2048 keys 287 / 281 / 276, 96 x 3540 273 / 255 / 247.
+    int64_t keys = round_up((longest * units + 2 * kCUs - 1) / (2 * kCUs), 128);
+    if (units * 32 >= kCUs && keys < longest / 32) keys = round_up(longest / 32, 128);
+    if (keys > 2048) keys = 2048;
     int64_t splits = (longest + keys - 1) / keys;
     const int64_t fit = parts_that_fit(workspace_bytes, rows, a.h.head_dim);
-    if (splits > fit || units > kCounters) splits = units > kCounters ? 1 : fit;
+    if (splits > fit) splits = fit;
+    if (units > kCounters || args->n_seqs > kMostListed) splits = 1;
     if (splits > kMaxParts) splits = kMaxParts;
     a.n_splits = 1;
     a.split_keys = (int32_t)kMostRows;
@@ -291,10 +285,15 @@ cf_status cf_attn_paged(const cf_attn_desc *desc, const cf_kv_cache *cache, cons
     if (units * a.n_splits > kMostGrid) return CF_ERR_SHAPE;
     if (a.n_splits > 1) place_parts(a.parts, workspace, rows, a.n_splits, a.h.head_dim);
     a.counters = static_cast<uint32_t *>(workspace);
-    a.join_after = a.n_splits > 1 && units * a.n_splits > PAGED_AFTER * kCUs;
+    a.many = a.n_splits > 1 && units * a.n_splits > 4 * kCUs;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     hipError_t e = launch_paged(a, s);
-    if (e == hipSuccess && a.join_after) e = join_parts(a.h, a.parts, a.n_splits, a.out, a.lse, nullptr, 0, s);
+    if (e == hipSuccess && a.many) {
+        JoinArgs j = parts_to_join(a.h, a.parts, a.n_splits, a.out, a.lse);
+        j.lens = a.lens;
+        j.split_keys = a.split_keys;
+        e = launch_join(j, s);
+    }
     return status_of(e);
 }
 

@@ -93,8 +93,9 @@ template <int DT, int PT, int D, int SPREAD> __global__ __launch_bounds__(256) v
     static_assert(kRows >= 1, "a workgroup has a row at least");
     const int row_here = threadIdx.x / (kLanes * SPREAD), share = threadIdx.x / kLanes % SPREAD, lane = threadIdx.x % kLanes;
     const int64_t row = (int64_t)blockIdx.x * kRows + row_here;
-    const bool there = row < a.n_rows;
-    const int64_t token = (there ? row : 0) / a.h.q_heads;
+    const int64_t token = (row < a.n_rows ? row : 0) / a.h.q_heads;
+    const int n_parts = a.lens ? (int)max(min((gconst<int32_t>(a.lens)[token] + (int64_t)a.split_keys - 1) / a.split_keys, (int64_t)a.n_parts), (int64_t)1) : a.n_parts;
+    const bool there = row < a.n_rows && !(a.lens && n_parts == 1);
     float top = -__builtin_inff(), total = 0.0f, o[8] = {}, base = 0.0f;
     auto weight = [&](float lse) { return exp2_fast((lse - base) * 1.44269504088896341f); };
     auto load = [&](int p, f32x4 &x, f32x4 &y) {
@@ -122,7 +123,7 @@ template <int DT, int PT, int D, int SPREAD> __global__ __launch_bounds__(256) v
 #pragma unroll
             for (int p = 0; p < kFewParts; ++p) {
                 lse[p] = -__builtin_inff();
-                if (p < a.n_parts) {
+                if (p < n_parts) {
                     lse[p] = gconst<float>(a.lses[p])[row];
                     load(p, x[p], y[p]);
                 }
@@ -132,12 +133,12 @@ template <int DT, int PT, int D, int SPREAD> __global__ __launch_bounds__(256) v
             base = top == -__builtin_inff() ? 0.0f : top;
 #pragma unroll
             for (int p = 0; p < kFewParts; ++p)
-                if (p < a.n_parts) add(lse[p], x[p], y[p]);
+                if (p < n_parts) add(lse[p], x[p], y[p]);
         }
     } else if (there) {
-        for (int p = 0; p < a.n_parts; ++p) top = fmaxf(top, gconst<float>(a.lses[p])[row]);
+        for (int p = 0; p < n_parts; ++p) top = fmaxf(top, gconst<float>(a.lses[p])[row]);
         base = top == -__builtin_inff() ? 0.0f : top;
-        for (int p = share; p < a.n_parts; p += SPREAD) {
+        for (int p = share; p < n_parts; p += SPREAD) {
             const float lse = gconst<float>(a.lses[p])[row];
             if (lse == -__builtin_inff()) continue;     // its output is not read
             f32x4 x, y;
