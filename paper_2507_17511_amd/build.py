@@ -11,9 +11,9 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcompactfusion.so")
 SOURCES = ["cf_api.cpp", "cf_kernels.hip", "cf_single_pass.hip", "cf_lowrank.hip", "cf_static.hip",
-           "cf_attn_api.cpp", "cf_attn_prompt.hip", "cf_attn_paged.hip", "cf_attn_rows.hip"]
+           "cf_attn_api.cpp", "cf_attn_prompt.hip", "cf_attn_prompt256.hip", "cf_attn_paged.hip", "cf_attn_rows.hip"]
 HEADERS = [os.path.join(CSRC, "cf_internal.h"), os.path.join(CSRC, "cf_device.h"), os.path.join(CSRC, "cf_attn.h"),
-           os.path.join(CSRC, "cf_attn_device.h"), os.path.join(ROOT, "include", "compactfusion.h")]
+           os.path.join(CSRC, "cf_attn_device.h"), os.path.join(CSRC, "cf_attn_prompt.h"), os.path.join(ROOT, "include", "compactfusion.h")]
 
 # -ffp-contract=off: one rounding per fp32 operation (results must match a plain
 # CPU evaluation bit for bit).  Packed-fp32 instructions are switched off.
@@ -24,6 +24,9 @@ HIPCC_FLAGS = [
     "-Wall", "-Wno-unused-function",
     "-x", "hip",
 ]
+
+# Flags of single files, on top: results of matrix instructions in vector registers, where a kernel keeps all it has there.
+FILE_FLAGS = {"cf_attn_prompt.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 def build(force: bool = True, verbose: bool = False) -> str:
@@ -37,7 +40,7 @@ def build(force: bool = True, verbose: bool = False) -> str:
     with tempfile.TemporaryDirectory(prefix="cf_build_") as tmpdir:
         def compile_one(src: str) -> str:
             obj = os.path.join(tmpdir, os.path.basename(src) + ".o")
-            cmd = [hipcc, *compile_flags, "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-c", src, "-o", obj]
+            cmd = [hipcc, *compile_flags, *FILE_FLAGS.get(os.path.basename(src), []), "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-c", src, "-o", obj]
             if verbose:
                 print(" ".join(cmd))
             subprocess.check_call(cmd)
