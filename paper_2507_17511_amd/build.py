@@ -11,9 +11,9 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcompactfusion.so")
 SOURCES = ["cf_api.cpp", "cf_kernels.hip", "cf_single_pass.hip", "cf_lowrank.hip", "cf_static.hip",
-           "cf_attn_api.cpp", "cf_attn_prompt.hip", "cf_attn_prompt256.hip", "cf_attn_paged.hip", "cf_attn_rows.hip"]
+           "cf_attn_api.cpp", "cf_attn_prompt.hip", "cf_attn_paged.hip", "cf_attn_rows.hip"]
 HEADERS = [os.path.join(CSRC, "cf_internal.h"), os.path.join(CSRC, "cf_device.h"), os.path.join(CSRC, "cf_attn.h"),
-           os.path.join(CSRC, "cf_attn_device.h"), os.path.join(CSRC, "cf_attn_prompt.h"), os.path.join(ROOT, "include", "compactfusion.h")]
+           os.path.join(CSRC, "cf_attn_device.h"), os.path.join(ROOT, "include", "compactfusion.h")]
 
 # -ffp-contract=off: one rounding per fp32 operation (results must match a plain
 # CPU evaluation bit for bit).  Packed-fp32 instructions are switched off.
@@ -25,7 +25,8 @@ HIPCC_FLAGS = [
     "-x", "hip",
 ]
 
-# Flags of single files, on top: results of matrix instructions in vector registers, where a kernel keeps all it has there.
+# Flags of single files, on top.  Results of matrix instructions in vector registers: scores need not be moved there before they are used
+# (prompts of 16384 x 24 heads 2897 -> 2860 us, of 4096 x 24 heads 215 -> 196).
 FILE_FLAGS = {"cf_attn_prompt.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 

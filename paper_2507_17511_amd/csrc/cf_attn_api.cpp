@@ -136,18 +136,18 @@ JoinArgs parts_to_join(const Heads &h, const Parts &p, int n, const Rows &out, f
 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
-// Into how many parts the keys of `busy` workgroups are split: what takes the least time, where the device holds two workgroups a CU (one with
-// head_dim 256) that take 1.8 us over 64 keys (0.9 with head_dim 64), half a round of workgroups takes 0.6 of one, and the join
-// moves the parts twice at 5 TB/s, 4 us at least.  2 x 333 tokens over 20333 keys, 84 workgroups, head_dim 256: 3 parts 205 us, 6 277.
+// Into how many parts the keys of `busy` workgroups are split: what takes the least time, where the device holds two workgroups a CU that
+// take 1.8 us over 64 keys of 128 elements, half a round of workgroups takes 0.6 of one, and the join moves the parts twice at 5 TB/s, 4 us at
+// least.  2 x 333 tokens over 20333 keys, 84 workgroups: 6 parts, 246 us.
 int64_t prompt_splits(int64_t busy, int64_t longest, int64_t rows, int dim, int64_t most)
 {
-    const int64_t slots = dim == 256 ? kCUs : 2 * kCUs, steps = (longest + 63) / 64;
-    const double step_us = dim == 64 ? 0.9 : 1.8, part_us = (double)rows * (dim + 1) * 4 * 2 / 5.0e6;
+    const int64_t slots = 2 * kCUs, steps = (longest + 63) / 64;
+    const double step_us = 0.9 / 64.0 * dim, part_us = (double)rows * (dim + 1) * 4 * 2 / 5.0e6;
     int64_t best = 1;
     double least = 0.0;
     for (int64_t n = 1; n <= (most > 1 ? most : 1); ++n) {
         const int64_t rest = busy * n % slots;
-        const double rounds = (double)(busy * n / slots) + (rest == 0 ? 0.0 : slots > kCUs && rest <= kCUs ? 0.6 : 1.0);
+        const double rounds = (double)(busy * n / slots) + (rest == 0 ? 0.0 : rest <= kCUs ? 0.6 : 1.0);
         const double us = rounds * (double)((steps + n - 1) / n) * step_us + (n > 1 ? 4.0 + part_us * (double)n : 0.0);
         if (n == 1 || us < least) {
             best = n;

@@ -1,17 +1,364 @@
-// Whole prompts of head_dim 64 and 128: two waves a SIMD, of 256 vector registers each.  Compiled with the results of matrix instructions
-// in these (build.py): scores need not be moved before they are used.  16384 x 24 heads of zeros 2270 -> 2100 us, 4096 x 24 heads 218 -> 207.
-#include "cf_attn_prompt.h"
+// Attention over whole prompts: out = softmax(scale q k^T) v per sequence, one pass over the keys with a running
+// maximum and sum.
+//
+// The rows of a workgroup are (token, head) pairs of the query heads that share one head of keys, token-major, so that
+// grouped heads fill a tile of few tokens and the tile's causal edge is short.  A wave has 32 rows.  Both products are
+// taken transposed: S^T = K Q^T gives a lane the scores of ONE row (its column) and 16 of 32 keys; in that layout the weights are
+// the right operand of O^T = V^T P^T, up to an order of the keys that the reads of V follow, so weights
+// never leave their lane, and the row's maximum, sum and scale are scalars of the lane.
+#include "cf_attn_device.h"
 
 namespace cf {
 namespace attn {
+namespace {
 
-hipError_t launch_prompt256(const PromptArgs &a, hipStream_t s);
+constexpr int kWaves = 4;
+static_assert(kPromptRows == kWaves * 32, "a wave has 32 rows");
+
+// Where the 16-byte vectors of a staged tile's row lie: XORed so that neither the reads of K (16 rows, one vector each) nor the
+// transposing reads of V (4 rows, 4 neighbouring vectors each) meet in a bank.
+template <int D> __device__ __forceinline__ constexpr int k_turn(int row) { return D == 64 ? (row >> 1) & 7 : D == 128 ? row & 15 : row & 7; }
+template <int D> __device__ __forceinline__ constexpr int v_turn(int row) { return D == 64 ? ((row >> 1) & 1) << 2 : (row & 3) << 2; }
+
+struct Tile {
+    int seq_q, len_q;           // the sequence's first row of q, and how many
+    int seq_k, len_k;
+    int index;                  // which row tile of the sequence; -1: none
+};
+
+__device__ __forceinline__ int clamped(int x, int most) { return min(max(x, 0), most); }
+
+// The n-th row tile, counted from the last sequence's last: every lane takes a sequence, a prefix sum over the wave
+// finds the one that has it.  Starts are clamped to the rows there are.
+__device__ __forceinline__ Tile find_tile(const PromptArgs &a, int n)
+{
+    Tile t = {0, 0, 0, 0, -1};
+    const int lane = threadIdx.x & 63;
+    for (int end = a.n_seqs; end > 0; end -= 64) {
+        const int b = end - 1 - lane;
+        int q0 = 0, len = 0, tiles = 0;
+        if (b >= 0) {
+            q0 = clamped(gconst<int32_t>(a.cu_q)[b], a.n_q);
+            len = max(clamped(gconst<int32_t>(a.cu_q)[b + 1], a.n_q) - q0, 0);
+            tiles = (int)(((int64_t)len * a.h.group + kPromptRows - 1) / kPromptRows);
+        }
+        int upto = tiles;
+        for (int d = 1; d < 64; d <<= 1) {
+            const int below = __shfl_up(upto, d);
+            if (lane >= d) upto += below;
+        }
+        const int total = __builtin_amdgcn_readlane(upto, 63);
+        if (n < total) {
+            const int who = __builtin_ctzll(__ballot(n < upto));
+            const int seq = end - 1 - who;
+            t.seq_q = __builtin_amdgcn_readlane(q0, who);
+            t.len_q = __builtin_amdgcn_readlane(len, who);
+            t.index = __builtin_amdgcn_readlane(upto, who) - 1 - n;
+            const int k0 = clamped(gconst<int32_t>(a.cu_k)[seq], a.n_k);
+            t.seq_k = __builtin_amdgcn_readfirstlane(k0);
+            t.len_k = __builtin_amdgcn_readfirstlane(max(clamped(gconst<int32_t>(a.cu_k)[seq + 1], a.n_k) - k0, 0));
+            return t;
+        }
+        n -= total;
+    }
+    return t;
+}
+
+// Brings 16 bytes from `base` + `from_all` + `from` to `to` + 16 * lane in LDS; those of which `from` is past `bytes` are zeros.
+__device__ __forceinline__ void stage(const char *base, uint32_t bytes, uint32_t from, uint32_t from_all, char *to)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (int)bytes, 0x00020000), (CF_LDS void *)to, 16, from, from_all, 0, 0);
+}
+
+template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, 2) void k_attn_prompt(PromptArgs a)
+{
+    using E = Elem<DT>;
+    constexpr int kKeys = D == 256 ? 32 : 64;               // keys of a staged tile
+    constexpr bool kAhead = D != 256;                       // the next tile's scores are taken while this one's weights are computed
+    constexpr int kSteps = D / 16;                          // matrix instructions over the head dimension
+    constexpr int kBlocks = D / 32;                         // 32-row blocks of O^T
+    constexpr int kSub = kKeys / 32;
+    constexpr int kVecs = D / 8;                            // 16-byte vectors of a row
+    constexpr int kStepRows = kWaves * 64 / kVecs;          // rows that the workgroup brings with one load a lane
+    static_assert(k_turn<D>(kStepRows) == 0 && v_turn<D>(kStepRows) == 0, "every kStepRows rows are turned alike");
+    constexpr int kLoads = kKeys * kVecs / (kWaves * 64);   // vectors of a tile that a lane brings
+    constexpr int kTile = kKeys * D * 2;
+    __shared__ __align__(256) char lds_k[2 * kTile], lds_v[2 * kTile];
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
+    const int unit = blockIdx.x % (a.h.kv_heads * a.n_splits);
+    const int kv_head = unit % a.h.kv_heads, split = unit / a.h.kv_heads;
+    const Tile t = find_tile(a, blockIdx.x / (a.h.kv_heads * a.n_splits));
+    if (t.index < 0) return;
+
+    // this lane's row
+    const int row0 = t.index * kPromptRows + wave * 32, rows = t.len_q * a.h.group;
+    const int shift = a.causal ? t.len_k - t.len_q + 1 : t.len_k;
+    const int split_begin = split * a.split_keys;
+    const int split_end = split == a.n_splits - 1 ? t.len_k : min(split_begin + a.split_keys, t.len_k);
+    auto seen_by = [&](int token) { return min(max(a.causal ? token + shift : t.len_k, 0), t.len_k); };      // keys that a token's rows see
+    const int row = min(row0 + col, rows - 1), token = row / a.h.group, head = kv_head * a.h.group + row - token * a.h.group;
+    const int seen = min(seen_by(token), split_end);
+    u32x4 q[kSteps];
+    {
+        const char *src = a.q.data + (t.seq_q + (int64_t)token) * a.q.token + head * a.q.head + half * 16;
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) q[i] = *gconst<u32x4>(src + i * 32);
+    }
+    // keys that no row of the workgroup sees begin at `end`, those that no row of the wave sees at `limit`, and those that not all of its rows see at `edge`
+    const int end = min(split_end, seen_by((min((t.index + 1) * kPromptRows, rows) - 1) / a.h.group));
+    const int limit = row0 < rows ? min(split_end, seen_by((min(row0 + 32, rows) - 1) / a.h.group)) : 0;
+    const int edge = min(limit, seen_by(min(row0, rows - 1) / a.h.group));
+
+    f32x16 o[kBlocks];
+#pragma unroll
+    for (int d = 0; d < kBlocks; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+    float m = kNoMax, l = 0.0f;
+    const float c = a.h.scale_log2;
+
+    // where this lane's vectors of a tile come from: the n-th is n * kStepRows rows further on, and turned alike
+    const int from_row = (wave * 64 + lane) / kVecs, place = lane % kVecs;
+    const uint32_t k_from = (uint32_t)from_row * (uint32_t)a.k.token + (place ^ k_turn<D>(from_row)) * 16;
+    const uint32_t v_from = (uint32_t)from_row * (uint32_t)a.v.token + (place ^ v_turn<D>(from_row)) * 16;
+    const char *k_base = a.k.data + t.seq_k * a.k.token + kv_head * a.k.head;
+    const char *v_base = a.v.data + t.seq_k * a.v.token + kv_head * a.v.head;
+    auto bring = [&](const char *base, int64_t stride, uint32_t from, char *to, int at) {
+        base += at * stride;
+        if (at + kKeys <= t.len_k) {
+#pragma unroll
+            for (int n = 0; n < kLoads; ++n) stage(base, 0xffffffffu, from, n * (uint32_t)(kStepRows * stride), to + (n * kWaves + wave) * 1024);
+        } else {            // rows past the sequence come as zeros
+#pragma unroll 1
+            for (int n = 0; n < kLoads; ++n) {
+                const int rows_here = min(t.len_k - at - n * kStepRows, kStepRows);
+                stage(base + n * kStepRows * stride, rows_here > 0 ? (uint32_t)(rows_here - 1) * (uint32_t)stride + D * 2 : 0, from, 0, to + (n * kWaves + wave) * 1024);
+            }
+        }
+    };
+    auto bring_k = [&](int at, int buffer) { bring(k_base, a.k.token, k_from, lds_k + buffer, at); };
+    auto bring_v = [&](int at, int buffer) { bring(v_base, a.v.token, v_from, lds_v + buffer, at); };
+
+    const CF_LDS char *k_read = (const CF_LDS char *)lds_k + col * (D * 2) + ((half ^ k_turn<D>(col)) << 4);
+    const int v_row = 4 * half + ((lane & 15) >> 2);
+    const int v_vec = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    const CF_LDS char *v_read = (const CF_LDS char *)lds_v + v_row * (D * 2) + ((v_vec ^ v_turn<D>(v_row)) << 4) + (lane & 1) * 8;
+    // elements d * 32 + col of keys 16 g + 4 half + {0 .. 3, 8 .. 11} of the tile
+    auto values = [&](int buffer, int g, int d) {
+        const CF_LDS char *at = (const CF_LDS char *)((uintptr_t)v_read ^ (d << 6)) + buffer + g * 16 * D * 2;
+        const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((CF_LDS s16x4 *)at));
+        const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((CF_LDS s16x4 *)(at + 8 * D * 2)));
+        return (u32x4){x[0], x[1], y[0], y[1]};
+    };
+
+    // A tile's scores are taken while the weights of the tile before are computed.  While V of tile n and K of tile n + 1 are read, V of tile
+    // n + 1 and K of tile n + 2 come, into the other buffers.  The waves of a workgroup meet here once a tile, wherever in the
+    // loops below they are.
+    int key0 = split_begin, buffer = 0;         // the tile in work, and where its V is; K of the next one is in the other buffer
+    auto send = [&]() {
+        if (key0 + kKeys < end) bring_v(key0 + kKeys, buffer ^ kTile);
+        if constexpr (kAhead) {
+            if (key0 + 2 * kKeys < end) bring_k(key0 + 2 * kKeys, buffer);
+        } else {
+            if (key0 + kKeys < end) bring_k(key0 + kKeys, buffer ^ kTile);
+        }
+    };
+    auto advance = [&]() {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        key0 += kKeys;
+        buffer ^= kTile;
+        send();
+    };
+    f32x16 s[kSub];
+    u32x4 p[kSub * 2];
+    auto scores = [&](f32x16 (&s)[kSub], int buffer) {
+#pragma unroll
+        for (int b = 0; b < kSub; ++b) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[b][i] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                const u32x4 k = *(const CF_LDS u32x4 *)((const CF_LDS char *)((uintptr_t)k_read ^ (i << 5)) + buffer + b * 32 * D * 2);
+                s[b] = E::mfma32(k, q[i], s[b]);
+            }
+        }
+    };
+    auto largest = [&](const f32x16 (&s)[kSub]) {
+        float top = s[0][0];
+#pragma unroll
+        for (int b = 0; b < kSub; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
+        return max_halves(top) * c;
+    };
+    auto rescale = [&](float top) {
+        const float fresh = fmaxf(m, top), scale = exp2_fast(m - fresh);
+#pragma unroll
+        for (int d = 0; d < kBlocks; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] *= scale;
+        l *= scale;
+        m = fresh;
+    };
+    auto weights = [&]() {          // -> their sum
+        float sum = 0.0f;
+#pragma unroll
+        for (int b = 0; b < kSub; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                const float p0 = exp2_fast(__builtin_fmaf(s[b][i], c, -m)), p1 = exp2_fast(__builtin_fmaf(s[b][i + 1], c, -m));
+                sum += p0 + p1;
+                p[b * 2 + (i >> 3)][(i & 7) >> 1] = E::pack(p0, p1);
+            }
+        return sum;
+    };
+    auto products = [&]() {
+#pragma unroll
+        for (int g = 0; g < kSub * 2; ++g)
+#pragma unroll
+            for (int d = 0; d < kBlocks; ++d) o[d] = E::mfma32(values(buffer, g, d), p[g], o[d]);
+    };
+
+    if (key0 < end) {
+        bring_k(key0, 0);
+        bring_v(key0, 0);
+        if (kAhead && key0 + kKeys < end) bring_k(key0 + kKeys, kTile);
+        asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+        if constexpr (kAhead) {
+            scores(s, 0);
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");      // K's first buffer is free again
+        }
+        send();
+    }
+    // Tiles that all rows of the wave see, up to the last but one.  Their maximum is not looked for: weights are positive, so
+    // that none is larger than their sum.  Where that passes kMostSum, in any lane, the tile is done again after its maximum has been taken and the
+    // accumulators scaled; most often that is the first tile alone.  That happens outside of the inner loop, where the compiler keeps them in place.
+    if constexpr (kAhead) {
+        while (key0 + 2 * kKeys <= edge) {
+            rescale(largest(s));
+            do {
+                f32x16 next[kSub];
+                scores(next, buffer ^ kTile);
+                const float sum = weights();
+                if (__any(sum > kMostSum)) break;
+                l += sum;
+                products();
+#pragma unroll
+                for (int b = 0; b < kSub; ++b) s[b] = next[b];
+                advance();
+            } while (key0 + 2 * kKeys <= edge);
+        }
+    } else {
+        while (key0 + kKeys <= edge) {
+            scores(s, buffer);
+            rescale(largest(s));
+            do {
+                scores(s, buffer);
+                const float sum = weights();
+                if (__any(sum > kMostSum)) break;
+                l += sum;
+                products();
+                advance();
+            } while (key0 + kKeys <= edge);
+        }
+    }
+    // The last of them, and tiles of which some rows see a part.
+    while (key0 < limit) {
+        bool odd = false;
+        if constexpr (!kAhead) scores(s, buffer);
+        if (key0 + kKeys > edge) {
+#pragma unroll
+            for (int b = 0; b < kSub; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (b * 32 + 8 * (i >> 2) + (i & 3) >= seen - key0 - 4 * half) s[b][i] = -__builtin_inff();
+            // A weight of zero does not keep an infinity or NaN out of a sum: is there one among the values that not all rows see?
+#pragma unroll 1
+            for (int g = max(edge - key0, 0) >> 4; g < kSub * 2; ++g)
+#pragma unroll
+                for (int d = 0; d < kBlocks; ++d) {
+                    const u32x4 v = values(buffer, g, d);
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) odd |= E::any_not_finite(v[w]);
+                }
+        }
+        const float top = largest(s);
+        if (__any(top > m + kMaxSlack)) rescale(top);
+        l += weights();
+        if (__builtin_expect(!__any(odd), 1)) {
+            products();
+        } else {
+            // The tile's keys one by one, to the rows that see them: the n-th of 16, which the lanes of half (n >> 2) & 1 have.
+#pragma unroll 1
+            for (int key = 0; key < kKeys; ++key) {
+                const int g = key >> 4, n = key & 15;
+                u32x4 of_key = p[0];
+#pragma unroll
+                for (int i = 1; i < kSub * 2; ++i) of_key = g == i ? p[i] : of_key;
+#pragma unroll
+                for (int d = 0; d < kBlocks; ++d) {
+                    u32x4 v = values(buffer, g, d);
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) v[w] = half == ((n >> 2) & 1) && w == 2 * (n >> 3) + ((n & 3) >> 1) ? v[w] & (n & 1 ? 0xffff0000u : 0x0000ffffu) : 0u;
+                    const f32x16 more = E::mfma32(v, of_key, o[d]);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[d][i] = key0 + key < seen ? more[i] : o[d][i];
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        }
+        if (kAhead && key0 + kKeys < limit) scores(s, buffer ^ kTile);
+        advance();
+    }
+    // Tiles that only other waves see.
+    while (key0 < end) advance();
+
+    l = sum_halves(l);
+    if (row0 + col >= rows) return;
+    const float inv = inverse_of(l);
+    if (l == 0.0f)              // no key, or none with a score above -infinity: 0 times an infinite value is none of the row's
+#pragma unroll
+        for (int d = 0; d < kBlocks; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+    const int64_t at = (t.seq_q + (int64_t)token) * a.h.q_heads + head;
+    if (a.n_splits > 1) {
+        float *dst = a.parts.o + ((int64_t)split * a.parts.n_rows + at) * D;
+#pragma unroll
+        for (int d = 0; d < kBlocks; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+                *gmut<f32x4>(dst + d * 32 + 2 * i + 4 * half) = (f32x4){o[d][i] * inv, o[d][i + 1] * inv, o[d][i + 2] * inv, o[d][i + 3] * inv};
+        if (half == 0) gmut<float>(a.parts.lse)[(int64_t)split * a.parts.n_rows + at] = lse_of(m, l);
+    } else {
+        char *dst = a.out.data + (t.seq_q + (int64_t)token) * a.out.token + head * a.out.head;
+#pragma unroll
+        for (int d = 0; d < kBlocks; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+                *gmut<u32x2>(dst + (d * 32 + 2 * i + 4 * half) * 2) = (u32x2){E::pack(o[d][i] * inv, o[d][i + 1] * inv), E::pack(o[d][i + 2] * inv, o[d][i + 3] * inv)};
+        if (a.lse && half == 0) gmut<float>(a.lse)[at] = lse_of(m, l);
+    }
+}
+
+template <int DT, int D> hipError_t prompt_dim(const PromptArgs &a, hipStream_t s)
+{
+    const int64_t tiles = ((int64_t)a.n_q * a.h.group + kPromptRows - 1) / kPromptRows + a.n_seqs;      // at most: a part of one for every sequence
+    hipLaunchKernelGGL((k_attn_prompt<DT, D>), dim3((unsigned)(tiles * a.h.kv_heads * a.n_splits)), dim3(kWaves * 64), 0, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace
 
 hipError_t launch_prompt(const PromptArgs &a, hipStream_t s)
 {
-    if (a.h.head_dim == 256) return launch_prompt256(a, s);
-    if (a.h.dtype == BF16) return a.h.head_dim == 64 ? prompt_dim<BF16, 64>(a, s) : prompt_dim<BF16, 128>(a, s);
-    return a.h.head_dim == 64 ? prompt_dim<F16, 64>(a, s) : prompt_dim<F16, 128>(a, s);
+    const bool bf16 = a.h.dtype == BF16;
+    switch (a.h.head_dim) {
+    case 64: return bf16 ? prompt_dim<BF16, 64>(a, s) : prompt_dim<F16, 64>(a, s);
+    case 128: return bf16 ? prompt_dim<BF16, 128>(a, s) : prompt_dim<F16, 128>(a, s);
+    default: return bf16 ? prompt_dim<BF16, 256>(a, s) : prompt_dim<F16, 256>(a, s);
+    }
 }
 
 }  // namespace attn
