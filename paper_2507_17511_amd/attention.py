@@ -44,8 +44,9 @@ class PagedCache:
         for x in (k, v):
             _require(x.numel() > 0 and x[0].is_contiguous() and (pages == 1 or x.stride(0) == k.stride(0)), "pages are dense, and as far apart in k as in v")
         self.k, self.v = k, v
-        self.heads, self.page_size, self.head_dim, self.dtype, self.device = heads, page, dim, k.dtype, k.device
+        self.heads, self.page_size, self.head_dim, self.dtype, self.index = heads, page, dim, k.dtype, k.get_device()
         self.struct = cf.cf_kv_cache(k.data_ptr(), v.data_ptr(), pages, k.stride(0) if pages > 1 else 0, page)
+        self.ref = ctypes.byref(self.struct)
 
     @classmethod
     def empty(cls, pages: int, kv_heads: int, head_dim: int, page_size: int = 64, dtype: torch.dtype = torch.bfloat16,
@@ -65,40 +66,50 @@ class AttentionSession:
         self.device = torch.device(device)
         if self.device.type == "cuda" and self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
+        self._index = self.device.index if self.device.type == "cuda" else -1
         self.desc = cf.cf_attn_desc(_CF_DT[dtype], q_heads, kv_heads, head_dim, scale)
+        self._lib = cf.lib()
+        self._desc = ctypes.byref(self.desc)
         self.ws_bytes = workspace_bytes
         self.workspace = torch.zeros(workspace_bytes, dtype=torch.uint8, device=self.device) if workspace_bytes else None
         self._ws = self.workspace.data_ptr() if workspace_bytes else None
         self._stream = stream
-        self._args = {x: x() for x in (cf.cf_append, cf.cf_prompt, cf.cf_paged, cf.cf_join)}
+        # the arguments of the call in hand, and how the library is handed them
+        self._append, self._prompt, self._paged, self._join = cf.cf_append(), cf.cf_prompt(), cf.cf_paged(), cf.cf_join()
+        self._refs = [ctypes.byref(x) for x in (self._append, self._prompt, self._paged, self._join)]
 
     def _on(self) -> int:
         if self._stream is not None:
             return self._stream.cuda_stream
         if _raw_stream is not None:
-            return _raw_stream(self.device.index)
+            return _raw_stream(self._index)
         return torch.cuda.current_stream(self.device).cuda_stream
 
+    # What a call reads of its tensors is most of its time on the host: each attribute once, and those that tell a wrong tensor.
     def _rows(self, x: torch.Tensor, tokens: int, heads: int, name: str):
         """-> data, token stride, head stride."""
-        if x.dim() == 3:
-            n, h, d = x.shape
+        if x.shape == (tokens, heads, self.head_dim) and x.dtype is self.dtype and x.get_device() == self._index:
             token, head, last = x.stride()
-            if n == tokens and h == heads and d == self.head_dim and last == 1 and x.dtype is self.dtype and x.device == self.device:
+            if last == 1:
                 return x.data_ptr(), token, head
         raise ValueError(f"{name} is [{tokens}, {heads}, {self.head_dim}] of {self.dtype} on {self.device}, the elements of a head next to one another: "
                          f"got {tuple(x.shape)} of {x.dtype} on {x.device}, strides {x.stride()}")
 
+    def _list(self, x: torch.Tensor, dtype: torch.dtype, n: int, name: str) -> int:
+        if x.numel() != n or x.dtype is not dtype or x.get_device() != self._index or not x.is_contiguous():
+            raise ValueError(f"{name} is {n} dense values of {dtype} on {self.device}: got {tuple(x.shape)} of {x.dtype} on {x.device}")
+        return x.data_ptr()
+
     def _plain(self, x: torch.Tensor, dtype: torch.dtype, shape, name: str) -> int:
-        if x.dtype is not dtype or x.shape != shape or not x.is_contiguous() or x.device != self.device:
+        if x.shape != shape or x.dtype is not dtype or x.get_device() != self._index or not x.is_contiguous():
             raise ValueError(f"{name} is dense {tuple(shape)} of {dtype} on {self.device}: got {tuple(x.shape)} of {x.dtype} on {x.device}")
         return x.data_ptr()
 
-    def _cache(self, cache: "PagedCache") -> cf.cf_kv_cache:
-        if cache.heads != self.kv_heads or cache.head_dim != self.head_dim or cache.dtype is not self.dtype or cache.device != self.device:
+    def _cache(self, cache: PagedCache):
+        if cache.heads != self.kv_heads or cache.head_dim != self.head_dim or cache.dtype is not self.dtype or cache.index != self._index:
             raise ValueError(f"the cache has {self.kv_heads} heads of {self.head_dim} of {self.dtype} on {self.device}: got {cache.heads} of "
-                             f"{cache.head_dim} of {cache.dtype} on {cache.device}")
-        return cache.struct
+                             f"{cache.head_dim} of {cache.dtype} on {cache.k.device}")
+        return cache.ref
 
     def append(self, cache: PagedCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, positions: Optional[torch.Tensor] = None,
                cos: Optional[torch.Tensor] = None, sin: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None,
@@ -119,13 +130,14 @@ class AttentionSession:
         if positions is not None:
             _require(cos is not None and sin is not None and cos.dim() == 2, "positions go with cos and sin [n_positions, rotary_dim / 2]")
             shape = cos.shape
-            at = (self._plain(positions, torch.int32, (n,), "positions"), self._plain(cos, torch.float32, shape, "cos"),
+            at = (self._list(positions, torch.int32, n, "positions"), self._plain(cos, torch.float32, shape, "cos"),
                   self._plain(sin, torch.float32, shape, "sin"))
             table = (shape[0], 2 * shape[1], interleaved)
-        a = self._args[cf.cf_append]
-        _APPEND.pack_into(a, 0, n, *self._rows(k, n, self.kv_heads, "k"), *self._rows(v, n, self.kv_heads, "v"),
-                          self._plain(slots, torch.int64, (n,), "slots"), *rows_q, *rows_out, *at, *table)
-        cf.cf_kv_append(self.desc, self._cache(cache), a, self._on())
+        _APPEND.pack_into(self._append, 0, n, *self._rows(k, n, self.kv_heads, "k"), *self._rows(v, n, self.kv_heads, "v"),
+                          self._list(slots, torch.int64, n, "slots"), *rows_q, *rows_out, *at, *table)
+        status = self._lib.cf_kv_append(self._desc, self._cache(cache), self._refs[0], self._on())
+        if status:
+            raise cf.CFError(status, "cf_kv_append")
         return q_out
 
     def prompt(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor, cu_k: Optional[torch.Tensor] = None,
@@ -137,11 +149,12 @@ class AttentionSession:
         _require(n >= 0, "cu_q has an entry more than there are sequences")
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        a = self._args[cf.cf_prompt]
-        _PROMPT.pack_into(a, 0, n, causal, n_q, n_k, max_k, self._plain(cu_q, torch.int32, (n + 1,), "cu_q"), self._plain(cu_k, torch.int32, (n + 1,), "cu_k"),
+        _PROMPT.pack_into(self._prompt, 0, n, causal, n_q, n_k, max_k, self._list(cu_q, torch.int32, n + 1, "cu_q"), self._list(cu_k, torch.int32, n + 1, "cu_k"),
                           *self._rows(q, n_q, self.q_heads, "q"), *self._rows(k, n_k, self.kv_heads, "k"), *self._rows(v, n_k, self.kv_heads, "v"),
                           *self._rows(out, n_q, self.q_heads, "out"), 0 if lse is None else self._plain(lse, torch.float32, (n_q, self.q_heads), "lse"))
-        cf.cf_attn_prompt(self.desc, a, self._ws, self.ws_bytes, self._on())
+        status = self._lib.cf_attn_prompt(self._desc, self._refs[1], self._ws, self.ws_bytes, self._on())
+        if status:
+            raise cf.CFError(status, "cf_attn_prompt")
         return out
 
     def paged(self, cache: PagedCache, q: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, out: Optional[torch.Tensor] = None,
@@ -151,15 +164,16 @@ class AttentionSession:
         n = q.shape[0]
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        _require(table.dim() == 2 and table.shape[0] == n and table.dtype is torch.int32 and table.device == self.device, "table is [sequences, pages] int32")
+        _require(table.dim() == 2 and table.shape[0] == n and table.dtype is torch.int32 and table.get_device() == self._index, "table is [sequences, pages] int32")
         row, entry = table.stride()
         cols = table.shape[1]
         _require(cols == 1 or entry == 1, "the rows of table are dense")
-        a = self._args[cf.cf_paged]
-        _PAGED.pack_into(a, 0, n, cols, row if n > 1 else 0, max_len, table.data_ptr(), self._plain(lens, torch.int32, (n,), "lens"),
+        _PAGED.pack_into(self._paged, 0, n, cols, row if n > 1 else 0, max_len, table.data_ptr(), self._list(lens, torch.int32, n, "lens"),
                          *self._rows(q, n, self.q_heads, "q"), *self._rows(out, n, self.q_heads, "out"),
                          0 if lse is None else self._plain(lse, torch.float32, (n, self.q_heads), "lse"))
-        cf.cf_attn_paged(self.desc, self._cache(cache), a, self._ws, self.ws_bytes, self._on())
+        status = self._lib.cf_attn_paged(self._desc, self._cache(cache), self._refs[2], self._ws, self.ws_bytes, self._on())
+        if status:
+            raise cf.CFError(status, "cf_attn_paged")
         return out
 
     def join(self, parts: Sequence[torch.Tensor], lses: Sequence[torch.Tensor], out: Optional[torch.Tensor] = None,
@@ -176,8 +190,9 @@ class AttentionSession:
             out = torch.empty(shape, dtype=self.dtype, device=self.device)
         p = (ctypes.c_void_p * n)(*[self._plain(x, pdt, shape, "a part") for x in parts])
         s = (ctypes.c_void_p * n)(*[self._plain(x, torch.float32, shape[:2], "a log-sum-exp") for x in lses])
-        a = self._args[cf.cf_join]
-        _JOIN.pack_into(a, 0, n, _CF_DT[pdt], tokens, ctypes.addressof(p), ctypes.addressof(s), *self._rows(out, tokens, self.q_heads, "out"),
+        _JOIN.pack_into(self._join, 0, n, _CF_DT[pdt], tokens, ctypes.addressof(p), ctypes.addressof(s), *self._rows(out, tokens, self.q_heads, "out"),
                         0 if lse is None else self._plain(lse, torch.float32, shape[:2], "lse"))
-        cf.cf_attn_join(self.desc, a, self._on())
+        status = self._lib.cf_attn_join(self._desc, self._refs[3], self._on())
+        if status:
+            raise cf.CFError(status, "cf_attn_join")
         return out
