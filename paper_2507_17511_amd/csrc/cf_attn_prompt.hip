@@ -6,6 +6,8 @@
 // taken transposed: S^T = K Q^T gives a lane the scores of ONE row (its column) and 16 of 32 keys; in that layout the weights are
 // the right operand of O^T = V^T P^T, up to an order of the keys that the reads of V follow, so weights
 // never leave their lane, and the row's maximum, sum and scale are scalars of the lane.
+#include <type_traits>
+
 #include "cf_attn_device.h"
 
 namespace cf {
@@ -36,10 +38,12 @@ __device__ __forceinline__ Tile find_tile(const PromptArgs &a, int n)
     const int lane = threadIdx.x & 63;
     for (int end = a.n_seqs; end > 0; end -= 64) {
         const int b = end - 1 - lane;
-        int q0 = 0, len = 0, tiles = 0;
+        int q0 = 0, len = 0, k0 = 0, len_k = 0, tiles = 0;
         if (b >= 0) {
             q0 = clamped(gconst<int32_t>(a.cu_q)[b], a.n_q);
             len = max(clamped(gconst<int32_t>(a.cu_q)[b + 1], a.n_q) - q0, 0);
+            k0 = clamped(gconst<int32_t>(a.cu_k)[b], a.n_k);
+            len_k = max(clamped(gconst<int32_t>(a.cu_k)[b + 1], a.n_k) - k0, 0);
             tiles = (int)(((int64_t)len * a.h.group + kPromptRows - 1) / kPromptRows);
         }
         int upto = tiles;
@@ -50,13 +54,11 @@ __device__ __forceinline__ Tile find_tile(const PromptArgs &a, int n)
         const int total = __builtin_amdgcn_readlane(upto, 63);
         if (n < total) {
             const int who = __builtin_ctzll(__ballot(n < upto));
-            const int seq = end - 1 - who;
             t.seq_q = __builtin_amdgcn_readlane(q0, who);
             t.len_q = __builtin_amdgcn_readlane(len, who);
+            t.seq_k = __builtin_amdgcn_readlane(k0, who);
+            t.len_k = __builtin_amdgcn_readlane(len_k, who);
             t.index = __builtin_amdgcn_readlane(upto, who) - 1 - n;
-            const int k0 = clamped(gconst<int32_t>(a.cu_k)[seq], a.n_k);
-            t.seq_k = __builtin_amdgcn_readfirstlane(k0);
-            t.len_k = __builtin_amdgcn_readfirstlane(max(clamped(gconst<int32_t>(a.cu_k)[seq + 1], a.n_k) - k0, 0));
             return t;
         }
         n -= total;
@@ -83,7 +85,9 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, 2) void k_att
     static_assert(k_turn<D>(kStepRows) == 0 && v_turn<D>(kStepRows) == 0, "every kStepRows rows are turned alike");
     constexpr int kLoads = kKeys * kVecs / (kWaves * 64);   // vectors of a tile that a lane brings
     constexpr int kTile = kKeys * D * 2;
-    __shared__ __align__(256) char lds_k[2 * kTile], lds_v[2 * kTile];
+    __shared__ __align__(256) char lds[4 * kTile];          // two tiles of K, two of V
+    char *const lds_k = lds, *const lds_v = lds + 2 * kTile;
+    __shared__ int64_t lds_dst[kWaves][32];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
     const int unit = blockIdx.x % (a.h.kv_heads * a.n_splits);
@@ -314,8 +318,10 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, 2) void k_att
     // Tiles that only other waves see.
     while (key0 < end) advance();
 
+    // All waves have left the tiles behind.  A wave turns its rows in LDS, 128 columns at a time, so that it stores whole lines.
     l = sum_halves(l);
-    if (row0 + col >= rows) return;
+    if (row0 >= rows) return;
+    const bool live = row0 + col < rows;
     const float inv = inverse_of(l);
     if (l == 0.0f)              // no key, or none with a score above -infinity: 0 times an infinite value is none of the row's
 #pragma unroll
@@ -323,22 +329,39 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, 2) void k_att
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
     const int64_t at = (t.seq_q + (int64_t)token) * a.h.q_heads + head;
+    float *lse = a.n_splits > 1 ? a.parts.lse + (int64_t)split * a.parts.n_rows : a.lse;
+    if (lse && live && half == 0) gmut<float>(lse)[at] = lse_of(m, l);
+    constexpr int kPass = D < 128 ? D / 32 : 4;             // blocks of 32 columns of a pass
+    CF_LDS char *const mine = (CF_LDS char *)lds + wave * (kTile * 4 / kWaves);
+    auto store = [&](char *base, auto wide) {
+        constexpr int kSize = decltype(wide)::value ? 4 : 2, kRow = kPass * 32 * kSize, kLine = kRow / 16;
+        static_assert(32 * kRow <= kTile * 4 / kWaves, "a wave's rows fit its share of LDS");
+#pragma unroll
+        for (int d0 = 0; d0 < kBlocks; d0 += kPass) {
+#pragma unroll
+            for (int d = 0; d < kPass; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    const f32x16 &x = o[d0 + d];
+                    if constexpr (kSize == 4) *(CF_LDS f32x4 *)(mine + col * kRow + (((d * 8 + i / 2 + half) ^ (col & (kLine - 1))) << 4)) = (f32x4){x[i] * inv, x[i + 1] * inv, x[i + 2] * inv, x[i + 3] * inv};
+                    else *(CF_LDS u32x2 *)(mine + col * kRow + (((d * 4 + i / 4) ^ (col & (kLine - 1))) << 4) + half * 8) = (u32x2){E::pack(x[i] * inv, x[i + 1] * inv), E::pack(x[i + 2] * inv, x[i + 3] * inv)};
+                }
+#pragma unroll
+            for (int n = 0; n < kLine / 2; ++n) {
+                const int r = n * (64 / kLine) + lane / kLine, place = lane % kLine;
+                const int64_t dst = lds_dst[wave][r];
+                const u32x4 x = *(const CF_LDS u32x4 *)(mine + r * kRow + ((place ^ (r & (kLine - 1))) << 4));
+                if (dst >= 0) *gmut<u32x4>(base + dst + d0 * 32 * kSize + place * 16) = x;
+            }
+        }
+    };
     if (a.n_splits > 1) {
-        float *dst = a.parts.o + ((int64_t)split * a.parts.n_rows + at) * D;
-#pragma unroll
-        for (int d = 0; d < kBlocks; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; i += 4)
-                *gmut<f32x4>(dst + d * 32 + 2 * i + 4 * half) = (f32x4){o[d][i] * inv, o[d][i + 1] * inv, o[d][i + 2] * inv, o[d][i + 3] * inv};
-        if (half == 0) gmut<float>(a.parts.lse)[(int64_t)split * a.parts.n_rows + at] = lse_of(m, l);
+        if (!__any(l != 0.0f)) return;                      // the join does not read outputs of parts without keys
+        if (half == 0) lds_dst[wave][col] = live ? ((int64_t)split * a.parts.n_rows + at) * (D * 4) : -1;
+        store(reinterpret_cast<char *>(a.parts.o), std::true_type{});
     } else {
-        char *dst = a.out.data + (t.seq_q + (int64_t)token) * a.out.token + head * a.out.head;
-#pragma unroll
-        for (int d = 0; d < kBlocks; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; i += 4)
-                *gmut<u32x2>(dst + (d * 32 + 2 * i + 4 * half) * 2) = (u32x2){E::pack(o[d][i] * inv, o[d][i + 1] * inv), E::pack(o[d][i + 2] * inv, o[d][i + 3] * inv)};
-        if (a.lse && half == 0) gmut<float>(a.lse)[at] = lse_of(m, l);
+        if (half == 0) lds_dst[wave][col] = live ? (t.seq_q + (int64_t)token) * a.out.token + head * a.out.head : -1;
+        store(a.out.data, std::false_type{});
     }
 }
 
