@@ -185,6 +185,12 @@ template <int DT, int D, bool MANY> __global__ __launch_bounds__(kWaves * 64, D 
                     l *= scale;
                     m = fresh;
                 }
+                if (key0 + kKeys > end) {       // the last key's value, read again for keys past it, may be infinite: 0 times it is not 0
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+#pragma unroll
+                        for (int w = 0; w < kWords; ++w) v[j][w] = j < most ? v[j][w] : 0u;
+                }
                 u32x4 p;
 #pragma unroll
                 for (int j = 0; j < 8; j += 2) {
