@@ -81,12 +81,9 @@ template <int DT, int D> __global__ __launch_bounds__(256) void k_kv_append(Appe
 
 // ---------------------------------------------------------------- join
 //
-// A lane has 8 elements of a row of every SPREAD-th part, and computes the weights of these parts for itself: the log-sum-exps of a row are
-// read by the lanes of that row together, and from the cache after the first.  Where there are many parts of few rows, SPREAD lanes
-// share an element, and their sums meet in LDS.
-constexpr int kFewParts = 4;
-
-template <int DT, int PT, int D, int SPREAD> __global__ __launch_bounds__(256) void k_attn_join(JoinArgs a)
+// SPREAD lanes share 8 elements of a row; each has every SPREAD-th part, EACH at most, and asks for all of them at once, log-sum-exps and
+// outputs.  The largest log-sum-exp and the sums meet in LDS, by a tree, so that the order is the same in every call.
+template <int DT, int PT, int D, int SPREAD, int EACH> __global__ __launch_bounds__(256) void k_attn_join(JoinArgs a)
 {
     constexpr int kLanes = D / 8;                       // of a row
     constexpr int kRows = 256 / (kLanes * SPREAD);      // of a workgroup
@@ -96,58 +93,51 @@ template <int DT, int PT, int D, int SPREAD> __global__ __launch_bounds__(256) v
     const int64_t token = (row < a.n_rows ? row : 0) / a.h.q_heads;
     const int n_parts = a.lens ? (int)max(min((gconst<int32_t>(a.lens)[token] + (int64_t)a.split_keys - 1) / a.split_keys, (int64_t)a.n_parts), (int64_t)1) : a.n_parts;
     const bool there = row < a.n_rows && !(a.lens && n_parts == 1);
-    float top = -__builtin_inff(), total = 0.0f, o[8] = {}, base = 0.0f;
-    auto weight = [&](float lse) { return exp2_fast((lse - base) * 1.44269504088896341f); };
-    auto load = [&](int p, f32x4 &x, f32x4 &y) {
-        if constexpr (PT == 0) {
-            const CF_GLOBAL f32x4 *src = gconst<f32x4>(static_cast<const float *>(a.parts[p]) + row * D + lane * 8);
-            x = src[0], y = src[1];
-        } else {
-            const u32x4 v = *gconst<u32x4>(static_cast<const uint16_t *>(a.parts[p]) + row * D + lane * 8);
-            x = (f32x4){Elem<DT>::lo(v[0]), Elem<DT>::hi(v[0]), Elem<DT>::lo(v[1]), Elem<DT>::hi(v[1])};
-            y = (f32x4){Elem<DT>::lo(v[2]), Elem<DT>::hi(v[2]), Elem<DT>::lo(v[3]), Elem<DT>::hi(v[3])};
-        }
-    };
-    auto add = [&](float lse, const f32x4 &x, const f32x4 &y) {
-        const float w = lse == -__builtin_inff() ? 0.0f : weight(lse);
-        total += w;
-        for (int k = 0; k < 4; ++k) {
-            o[k] = lse == -__builtin_inff() ? o[k] : __builtin_fmaf(w, x[k], o[k]);
-            o[4 + k] = lse == -__builtin_inff() ? o[4 + k] : __builtin_fmaf(w, y[k], o[4 + k]);
-        }
-    };
-    if constexpr (SPREAD == 1) {                        // all loads at once
-        float lse[kFewParts];
-        f32x4 x[kFewParts], y[kFewParts];
-        if (there) {
+    float lse[EACH], top = -__builtin_inff(), total = 0.0f, o[8] = {};
+    f32x4 x[EACH][2];
+    if (there) {
 #pragma unroll
-            for (int p = 0; p < kFewParts; ++p) {
-                lse[p] = -__builtin_inff();
-                if (p < n_parts) {
-                    lse[p] = gconst<float>(a.lses[p])[row];
-                    load(p, x[p], y[p]);
+        for (int i = 0; i < EACH; ++i) {
+            const int p = share + i * SPREAD;
+            lse[i] = -__builtin_inff();
+            if (p < n_parts) {
+                lse[i] = gconst<float>(a.lses[p])[row];
+                if constexpr (PT == 0) {
+                    const CF_GLOBAL f32x4 *src = gconst<f32x4>(static_cast<const float *>(a.parts[p]) + row * D + lane * 8);
+                    x[i][0] = src[0], x[i][1] = src[1];
+                } else {
+                    const u32x4 v = *gconst<u32x4>(static_cast<const uint16_t *>(a.parts[p]) + row * D + lane * 8);
+                    x[i][0] = (f32x4){Elem<DT>::lo(v[0]), Elem<DT>::hi(v[0]), Elem<DT>::lo(v[1]), Elem<DT>::hi(v[1])};
+                    x[i][1] = (f32x4){Elem<DT>::lo(v[2]), Elem<DT>::hi(v[2]), Elem<DT>::lo(v[3]), Elem<DT>::hi(v[3])};
                 }
             }
-#pragma unroll
-            for (int p = 0; p < kFewParts; ++p) top = fmaxf(top, lse[p]);
-            base = top == -__builtin_inff() ? 0.0f : top;
-#pragma unroll
-            for (int p = 0; p < kFewParts; ++p)
-                if (p < n_parts) add(lse[p], x[p], y[p]);
         }
-    } else if (there) {
-        for (int p = 0; p < n_parts; ++p) top = fmaxf(top, gconst<float>(a.lses[p])[row]);
-        base = top == -__builtin_inff() ? 0.0f : top;
-        for (int p = share; p < n_parts; p += SPREAD) {
-            const float lse = gconst<float>(a.lses[p])[row];
-            if (lse == -__builtin_inff()) continue;     // its output is not read
-            f32x4 x, y;
-            load(p, x, y);
-            add(lse, x, y);
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) top = fmaxf(top, lse[i]);
+    }
+    __shared__ float sums[SPREAD > 1 ? 256 : 1][9];
+    if constexpr (SPREAD > 1) {
+        sums[threadIdx.x][8] = top;
+        for (int w = SPREAD / 2; w > 0; w >>= 1) {
+            __syncthreads();
+            if (share < w) sums[threadIdx.x][8] = top = fmaxf(top, sums[threadIdx.x + w * kLanes][8]);
         }
+        __syncthreads();
+        top = sums[threadIdx.x - share * kLanes][8];
+        __syncthreads();
+    }
+    const float base = top == -__builtin_inff() ? 0.0f : top;
+    if (there) {
+#pragma unroll
+        for (int i = 0; i < EACH; ++i)
+            if (lse[i] != -__builtin_inff()) {          // of other parts the output is not read
+                const float w = exp2_fast((lse[i] - base) * 1.44269504088896341f);
+                total += w;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) o[k] = __builtin_fmaf(w, x[i][k >> 2][k & 3], o[k]);
+            }
     }
     if constexpr (SPREAD > 1) {
-        __shared__ float sums[256][9];
         for (int k = 0; k < 8; ++k) sums[threadIdx.x][k] = o[k];
         sums[threadIdx.x][8] = total;
         for (int w = SPREAD / 2; w > 0; w >>= 1) {
@@ -169,17 +159,24 @@ template <int DT, int PT, int D, int SPREAD> __global__ __launch_bounds__(256) v
     if (a.lse && lane == 0) gmut<float>(a.lse)[row] = total > 0.0f || total != total ? base + __log2f(total) * kLn2 : -__builtin_inff();
 }
 
-template <int DT, int PT, int D, int SPREAD> hipError_t join_spread(const JoinArgs &a, hipStream_t s)
+template <int DT, int PT, int D, int SPREAD, int EACH> hipError_t join_spread(const JoinArgs &a, hipStream_t s)
 {
     constexpr int kRows = 256 / (D / 8 * SPREAD);
-    hipLaunchKernelGGL((k_attn_join<DT, PT, D, SPREAD>), dim3((unsigned)((a.n_rows + kRows - 1) / kRows)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((k_attn_join<DT, PT, D, SPREAD, EACH>), dim3((unsigned)((a.n_rows + kRows - 1) / kRows)), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
+// Up to 8 parts a lane each alone: lanes that meet cost a row more than loads in a row do (us: 12 parts of 98304 rows of 128 bf16, spread over 4 / 16
+// lanes 76 / 141; 6 of 10656 rows of 256 floats, over 1 / 8 lanes 12.7 / 24.8).  Past that a lane's loads are too many (48 parts, over 4 / 16 lanes
+// 118 / 76), and many parts are of few rows: the lanes of a whole workgroup fill the device.
 template <int DT, int PT, int D> hipError_t join_dim(const JoinArgs &a, hipStream_t s)
 {
-    if (a.n_parts > kFewParts) return join_spread<DT, PT, D, 256 / (D / 8)>(a, s);
-    return join_spread<DT, PT, D, 1>(a, s);
+    constexpr int kMost = 256 / (D / 8);
+    if (a.n_parts <= 4) return join_spread<DT, PT, D, 1, 4>(a, s);
+    if (a.n_parts <= 8) return join_spread<DT, PT, D, 1, 8>(a, s);
+    if (a.n_parts <= 16) return join_spread<DT, PT, D, 4, 4>(a, s);
+    static_assert(kMost * (64 / kMost) == kMaxParts, "the lanes have all parts");
+    return join_spread<DT, PT, D, kMost, 64 / kMost>(a, s);
 }
 
 template <int DT, int PT> hipError_t join_typed(const JoinArgs &a, hipStream_t s)
