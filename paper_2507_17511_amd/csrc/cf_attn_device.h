@@ -35,6 +35,8 @@ constexpr float kMaxSlack = 8.0f;
 // Where the maximum is not looked for (see k_attn_prompt): the most that the weights of a lane's keys of one tile may sum up to.  No weight is
 // larger than that, so that all of them are finite in fp16.
 constexpr float kMostSum = 32768.0f;
+// ... and the largest maximum of which half a unit in the last place is 1/4 at most.
+constexpr float kMostExact = 4194304.0f;
 
 template <typename T> __device__ __forceinline__ const CF_GLOBAL T *gconst(const void *p) { return (const CF_GLOBAL T *)p; }
 template <typename T> __device__ __forceinline__ CF_GLOBAL T *gmut(void *p) { return (CF_GLOBAL T *)p; }

@@ -191,10 +191,10 @@ template <int DT, int D, bool MANY> __global__ __launch_bounds__(kWaves * 64, D 
 #pragma unroll
                         for (int w = 0; w < kWords; ++w) v[j][w] = j < most ? v[j][w] : 0u;
                 }
-                u32x4 p;
+                u32x4 p;        // scaled scores are rounded as their maximum was: of scores of any size the largest has the weight 1
 #pragma unroll
                 for (int j = 0; j < 8; j += 2) {
-                    const float p0 = exp2_fast(__builtin_fmaf(s[j >> 2][j & 3], c, -m)), p1 = exp2_fast(__builtin_fmaf(s[j >> 2][(j & 3) + 1], c, -m));
+                    const float p0 = exp2_fast(s[j >> 2][j & 3] * c - m), p1 = exp2_fast(s[j >> 2][(j & 3) + 1] * c - m);
                     l += p0 + p1;
                     p[j >> 1] = E::pack(p0, p1);
                 }
