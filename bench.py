@@ -389,11 +389,14 @@ def cpu_baseline(wl, ef: int, budget_s: float = 15.0):
 
 
 def source_fingerprint() -> str:
-    """Hash of the library's sources: a recorded profile only describes the kernels it was taken from."""
+    """Hash of the codec's sources (the attention operators' are files of their own, cf_attn*): a recorded profile only
+    describes the kernels it was taken from."""
     import glob
     import hashlib
     h = hashlib.sha256()
     for path in sorted(glob.glob(os.path.join(ROOT, "paper_2507_17511_amd", "csrc", "*"))):
+        if os.path.basename(path).startswith("cf_attn"):
+            continue
         h.update(os.path.basename(path).encode())
         h.update(open(path, "rb").read())
     return h.hexdigest()[:12]

@@ -435,7 +435,7 @@ typedef struct {
 } cf_join;
 
 /* Attention over the union of disjoint sets of keys from the attention over each: lse = log sum_p exp(lse_p),
- * out = sum_p exp(lse_p - lse) part_p, in fp32, parts in the order given.  A part whose log-sum-exp of a row is -infinity
+ * out = sum_p exp(lse_p - lse) part_p, in fp32, in an order that depends on the sizes alone.  A part whose log-sum-exp of a row is -infinity
  * adds nothing to it, whatever its output there holds. */
 cf_status cf_attn_join(const cf_attn_desc *desc, const cf_join *args, void *stream);
 

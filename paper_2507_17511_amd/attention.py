@@ -72,6 +72,8 @@ class AttentionSession:
         self._desc = ctypes.byref(self.desc)
         self.ws_bytes = workspace_bytes
         self.workspace = torch.zeros(workspace_bytes, dtype=torch.uint8, device=self.device) if workspace_bytes else None
+        if workspace_bytes and self.device.type == "cuda" and not torch.cuda.is_current_stream_capturing():
+            torch.cuda.current_stream(self.device).synchronize()        # zeros on whichever stream the first call is
         self._ws = self.workspace.data_ptr() if workspace_bytes else None
         self._stream = stream
         # the arguments of the call in hand, and how the library is handed them
@@ -84,6 +86,13 @@ class AttentionSession:
         if _raw_stream is not None:
             return _raw_stream(self._index)
         return torch.cuda.current_stream(self.device).cuda_stream
+
+    # An output is memory of the stream that it is written on: of another's it might still be in use there.
+    def _new(self, shape, dtype: torch.dtype) -> torch.Tensor:
+        if self._stream is None:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(self._stream):
+            return torch.empty(shape, dtype=dtype, device=self.device)
 
     # What a call reads of its tensors is most of its time on the host: each attribute once, and those that tell a wrong tensor.
     def _rows(self, x: torch.Tensor, tokens: int, heads: int, name: str):
@@ -121,7 +130,7 @@ class AttentionSession:
         rows_q = rows_out = (0, 0, 0)
         if q is not None:
             if q_out is None:
-                q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+                q_out = self._new(q.shape, self.dtype)
             rows_q = self._rows(q, n, self.q_heads, "q")
             rows_out = rows_q if q_out is q else self._rows(q_out, n, self.q_heads, "q_out")
         elif q_out is not None:
@@ -148,7 +157,7 @@ class AttentionSession:
         n, n_q, n_k = cu_q.shape[0] - 1, q.shape[0], k.shape[0]
         _require(n >= 0, "cu_q has an entry more than there are sequences")
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            out = self._new(q.shape, self.dtype)
         _PROMPT.pack_into(self._prompt, 0, n, causal, n_q, n_k, max_k, self._list(cu_q, torch.int32, n + 1, "cu_q"), self._list(cu_k, torch.int32, n + 1, "cu_k"),
                           *self._rows(q, n_q, self.q_heads, "q"), *self._rows(k, n_k, self.kv_heads, "k"), *self._rows(v, n_k, self.kv_heads, "v"),
                           *self._rows(out, n_q, self.q_heads, "out"), 0 if lse is None else self._plain(lse, torch.float32, (n_q, self.q_heads), "lse"))
@@ -163,7 +172,7 @@ class AttentionSession:
         table[b] (int32 both).  max_len: the longest context, a hint."""
         n = q.shape[0]
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            out = self._new(q.shape, self.dtype)
         _require(table.dim() == 2 and table.shape[0] == n and table.dtype is torch.int32 and table.get_device() == self._index, "table is [sequences, pages] int32")
         row, entry = table.stride()
         cols = table.shape[1]
@@ -187,7 +196,7 @@ class AttentionSession:
                  f"parts are [tokens, {self.q_heads}, {self.head_dim}] of {self.dtype} or torch.float32")
         tokens = shape[0]
         if out is None:
-            out = torch.empty(shape, dtype=self.dtype, device=self.device)
+            out = self._new(shape, self.dtype)
         p = (ctypes.c_void_p * n)(*[self._plain(x, pdt, shape, "a part") for x in parts])
         s = (ctypes.c_void_p * n)(*[self._plain(x, torch.float32, shape[:2], "a log-sum-exp") for x in lses])
         _JOIN.pack_into(self._join, 0, n, _CF_DT[pdt], tokens, ctypes.addressof(p), ctypes.addressof(s), *self._rows(out, tokens, self.q_heads, "out"),

@@ -6,6 +6,11 @@
 // taken transposed: S^T = K Q^T gives a lane the scores of ONE row (its column) and 16 of 32 keys; in that layout the weights are
 // the right operand of O^T = V^T P^T, up to an order of the keys that the reads of V follow, so weights
 // never leave their lane, and the row's maximum, sum and scale are scalars of the lane.
+//
+// Bound by the matrix cores, large calls by the power that they take: 16384 tokens of 24 heads of 128 over as many keys 2.94 ms, 1120 TFLOP/s,
+// and 2.09 ms where all operands are zeros, at a higher clock.  Two workgroups a CU, 256 registers a lane: a wave of 64 rows reads half of the LDS per product
+// but is alone on its SIMD (3.01 ms, zeros 2.57).  2 x 8191 tokens of 32 / 8 heads, causal, 1.04 ms (1060 TFLOP/s); ragged batches are bound by
+// what a workgroup does before its first and after its last product: 14 x 1 to 2003 tokens 99 us (580 TFLOP/s).
 #include <type_traits>
 
 #include "cf_attn_device.h"
