@@ -42,17 +42,22 @@ template <typename T> __device__ __forceinline__ const CF_GLOBAL T *gconst(const
 template <typename T> __device__ __forceinline__ CF_GLOBAL T *gmut(void *p) { return (CF_GLOBAL T *)p; }
 
 template <int DT> struct Elem;
+// Whether one of two 16-bit numbers is infinite or NaN: a carry out of the exponent, to the sign's place, tells.  Carries may be OR-ed over many.
+template <uint32_t EXPONENT> struct OddPair {
+    static __device__ __forceinline__ uint32_t carry(uint32_t w) { return (w & EXPONENT * 0x10001u) + (0x8000u - EXPONENT) * 0x10001u; }
+    static __device__ __forceinline__ bool any(uint32_t carries) { return (carries & 0x80008000u) != 0; }
+};
 template <> struct Elem<BF16> {
+    using Odd = OddPair<0x7f80u>;
     static __device__ __forceinline__ uint32_t pack(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, bf16x2)); }
-    static __device__ __forceinline__ bool any_not_finite(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
     static __device__ __forceinline__ float lo(uint32_t w) { return __uint_as_float(w << 16); }
     static __device__ __forceinline__ float hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
     static __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0); }
     static __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0); }
 };
 template <> struct Elem<F16> {
+    using Odd = OddPair<0x7c00u>;
     static __device__ __forceinline__ uint32_t pack(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, f16x2)); }
-    static __device__ __forceinline__ bool any_not_finite(uint32_t w) { return (w & 0x7c00u) == 0x7c00u || (w & 0x7c000000u) == 0x7c000000u; }
     static __device__ __forceinline__ float lo(uint32_t w) { return (float)__builtin_bit_cast(f16x2, w)[0]; }
     static __device__ __forceinline__ float hi(uint32_t w) { return (float)__builtin_bit_cast(f16x2, w)[1]; }
     static __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0); }

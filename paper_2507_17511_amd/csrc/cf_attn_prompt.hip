@@ -9,8 +9,8 @@
 //
 // Bound by the matrix cores, large calls by the power that they take: 16384 tokens of 24 heads of 128 over as many keys 2.94 ms, 1120 TFLOP/s,
 // and 2.09 ms where all operands are zeros, at a higher clock.  Two workgroups a CU, 256 registers a lane: a wave of 64 rows reads half of the LDS per product
-// but is alone on its SIMD (3.01 ms, zeros 2.57).  2 x 8191 tokens of 32 / 8 heads, causal, 1.04 ms (1060 TFLOP/s); ragged batches are bound by
-// what a workgroup does before its first and after its last product: 14 x 1 to 2003 tokens 99 us (580 TFLOP/s).
+// but is alone on its SIMD (3.01 ms, zeros 2.57).  2 x 8191 tokens of 32 / 8 heads, causal, 1.02 ms (1080 TFLOP/s); ragged batches are bound by
+// what a workgroup does before its first and after its last product: 14 x 1 to 2003 tokens 89 us (650 TFLOP/s).
 #include <type_traits>
 
 #include "cf_attn_device.h"
@@ -110,7 +110,7 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, 2) void k_att
     constexpr int kTile = kKeys * D * 2;
     __shared__ __align__(256) char lds[4 * kTile];          // two tiles of K, two of V
     char *const lds_k = lds, *const lds_v = lds + 2 * kTile;
-    __shared__ int64_t lds_dst[kWaves][32];
+    __shared__ int64_t lds_at[kWaves][32], lds_dst[kWaves][32];      // where a wave's rows go, -1: nowhere; kept here while registers are short
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5;
     const int unit = blockIdx.x % (a.h.kv_heads * a.n_splits);
@@ -131,6 +131,11 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, 2) void k_att
         const char *src = a.q.data + (t.seq_q + (int64_t)token) * a.q.token + head * a.q.head + half * 16;
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) q[i] = *gconst<u32x4>(src + i * 32);
+    }
+    if (half == 0) {
+        const int64_t at = row0 + col < rows ? (t.seq_q + (int64_t)token) * a.h.q_heads + head : -1;
+        lds_at[wave][col] = at;
+        lds_dst[wave][col] = at < 0 ? -1 : a.n_splits > 1 ? ((int64_t)split * a.parts.n_rows + at) * (D * 4) : (t.seq_q + (int64_t)token) * a.out.token + head * a.out.head;
     }
     // keys that no row of the workgroup sees begin at `end`, those that no row of the wave sees at `limit`, and those that not all of its rows see at `edge`
     const int end = min(split_end, seen_by((min((t.index + 1) * kPromptRows, rows) - 1) / a.h.group));
@@ -304,8 +309,9 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, 2) void k_att
         }
     }
     // The last of them, and tiles of which some rows see a part.
+    bool again = false;
     while (key0 < limit) {
-        bool odd = false;
+        uint32_t odd = 0;
         if constexpr (!kAhead) scores(s, buffer);
         if (key0 + kKeys > edge) {
 #pragma unroll
@@ -313,41 +319,22 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, 2) void k_att
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
                     if (b * 32 + 8 * (i >> 2) + (i & 3) >= seen - key0 - 4 * half) s[b][i] = -__builtin_inff();
-            // A weight of zero does not keep an infinity or NaN out of a sum: is there one among the values that not all rows see?
+            // A weight of zero does not keep an infinity or NaN out of a sum.  Is there one among the values that not all rows see, the wave's rows are
+            // computed once more at the end.
 #pragma unroll 1
             for (int g = max(edge - key0, 0) >> 4; g < kSub * 2; ++g)
 #pragma unroll
                 for (int d = 0; d < kBlocks; ++d) {
                     const u32x4 v = values(buffer, g, d);
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) odd |= E::any_not_finite(v[w]);
+                    for (int w = 0; w < 4; ++w) odd |= E::Odd::carry(v[w]);
                 }
         }
         const float top = largest(s);
         if (__any(top > m + kMaxSlack)) rescale(top);
         l += weights(std::true_type{});
-        if (__builtin_expect(!__any(odd), 1)) {
-            products();
-        } else {
-            // The tile's keys one by one, to the rows that see them: the n-th of 16, which the lanes of half (n >> 2) & 1 have.
-#pragma unroll 1
-            for (int key = 0; key < kKeys; ++key) {
-                const int g = key >> 4, n = key & 15;
-                u32x4 of_key = p[0];
-#pragma unroll
-                for (int i = 1; i < kSub * 2; ++i) of_key = g == i ? p[i] : of_key;
-#pragma unroll
-                for (int d = 0; d < kBlocks; ++d) {
-                    u32x4 v = values(buffer, g, d);
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) v[w] = half == ((n >> 2) & 1) && w == 2 * (n >> 3) + ((n & 3) >> 1) ? v[w] & (n & 1 ? 0xffff0000u : 0x0000ffffu) : 0u;
-                    const f32x16 more = E::mfma32(v, of_key, o[d]);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) o[d][i] = key0 + key < seen ? more[i] : o[d][i];
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-            }
-        }
+        again |= __any(E::Odd::any(odd)) != 0;
+        products();
         if (kAhead && key0 + kKeys < limit) scores(s, buffer ^ kTile);
         advance();
     }
@@ -357,16 +344,52 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, 2) void k_att
     // All waves have left the tiles behind.  A wave turns its rows in LDS, 128 columns at a time, so that it stores whole lines.
     l = sum_halves(l);
     if (row0 >= rows) return;
-    const bool live = row0 + col < rows;
+    // Key by key, to the rows that see it.  Here, where the loops above are over, this costs them no registers: done within them, it cost 14 prompts of 1 to
+    // 2003 tokens 101 us for 89, 50 of 128 54 for 42.
+    if (again) {
+        auto scaled = [&](int key) {
+            const char *from = k_base + key * (int64_t)a.k.token + half * 16;
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                const u32x4 k = *gconst<u32x4>(from + i * 32);
+#pragma unroll
+                for (int w = 0; w < 4; ++w) sum = __builtin_fmaf(E::lo(k[w]), E::lo(q[i][w]), __builtin_fmaf(E::hi(k[w]), E::hi(q[i][w]), sum));
+            }
+            return key < seen ? sum_halves(sum) * c : -__builtin_inff();
+        };
+        m = kNoMax;
+        l = 0.0f;
+#pragma unroll
+        for (int d = 0; d < kBlocks; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+#pragma unroll 1
+        for (int key = split_begin; key < limit; ++key) m = fmaxf(m, scaled(key));
+#pragma unroll 1
+        for (int key = split_begin; key < limit; ++key) {
+            const float exact = exp2_fast(scaled(key) - m), weight = E::lo(E::pack(exact, 0.0f));
+            const char *from = v_base + key * (int64_t)a.v.token + half * 8;
+            l += exact;
+#pragma unroll
+            for (int d = 0; d < kBlocks; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    const u32x2 v = *gconst<u32x2>(from + d * 64 + i * 4);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) o[d][i + j] = key < seen ? __builtin_fmaf(weight, j & 1 ? E::hi(v[j >> 1]) : E::lo(v[j >> 1]), o[d][i + j]) : o[d][i + j];
+                }
+        }
+    }
     const float inv = inverse_of(l);
     if (l == 0.0f)              // no key, or none with a score above -infinity: 0 times an infinite value is none of the row's
 #pragma unroll
         for (int d = 0; d < kBlocks; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
-    const int64_t at = (t.seq_q + (int64_t)token) * a.h.q_heads + head;
+    const int64_t at = lds_at[wave][col];
     float *lse = a.n_splits > 1 ? a.parts.lse + (int64_t)split * a.parts.n_rows : a.lse;
-    if (lse && live && half == 0) gmut<float>(lse)[at] = lse_of(m, l);
+    if (lse && at >= 0 && half == 0) gmut<float>(lse)[at] = lse_of(m, l);
     constexpr int kPass = D < 128 ? D / 32 : 4;             // blocks of 32 columns of a pass
     CF_LDS char *const mine = (CF_LDS char *)lds + wave * (kTile * 4 / kWaves);
     auto store = [&](char *base, auto wide) {
@@ -393,10 +416,8 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, 2) void k_att
     };
     if (a.n_splits > 1) {
         if (!__any(l != 0.0f)) return;                      // the join does not read outputs of parts without keys
-        if (half == 0) lds_dst[wave][col] = live ? ((int64_t)split * a.parts.n_rows + at) * (D * 4) : -1;
         store(reinterpret_cast<char *>(a.parts.o), std::true_type{});
     } else {
-        if (half == 0) lds_dst[wave][col] = live ? (t.seq_q + (int64_t)token) * a.out.token + head * a.out.head : -1;
         store(a.out.data, std::false_type{});
     }
 }
