@@ -12,6 +12,7 @@ namespace attn {
 
 #define CF_GLOBAL __attribute__((address_space(1)))
 #define CF_LDS __attribute__((address_space(3)))
+#define CF_CONST __attribute__((address_space(4)))     // memory that nothing writes during the launch
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));

@@ -44,6 +44,10 @@ template <int DT, int D, bool MANY> __global__ __launch_bounds__(kWaves * 64, D 
     constexpr int kWords = kPer / 2;
     __shared__ f32x4 lds_o[kWaves / 2][kPer][64];
     __shared__ f32x2 lds_ml[kWaves / 2][kPagedHeads];
+    // Wide queries wait in LDS, each lane's its own, where the listing of parts takes registers too: the loop's operands do not fit with them (40 contexts of
+    // 10000 keys, 40 / 8 heads of 256: 595 us for 615).
+    constexpr bool kKeepQ = D < 256 || !MANY;
+    __shared__ u32x4 lds_q[kKeepQ ? 1 : kWaves][kKeepQ ? 1 : kSteps][64];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quarter = lane >> 4;
     const int head_tiles = (a.h.group + kPagedHeads - 1) / kPagedHeads;
@@ -99,12 +103,18 @@ template <int DT, int D, bool MANY> __global__ __launch_bounds__(kWaves * 64, D 
         for (int d = 0; d < kPer; ++d) o[d] = (f32x4){0, 0, 0, 0};
 
         if (begin < end) {
-            u32x4 q[kSteps];
+            u32x4 q[kKeepQ ? kSteps : 1];
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) q[i] = *gconst<u32x4>(a.q.data + (int64_t)seq * a.q.token + (kv_head * a.h.group + head0 + min(col, heads - 1)) * a.q.head + i * 64 + quarter * 16);
+            for (int i = 0; i < kSteps; ++i) {
+                const u32x4 x = *gconst<u32x4>(a.q.data + (int64_t)seq * a.q.token + (kv_head * a.h.group + head0 + min(col, heads - 1)) * a.q.head + i * 64 + quarter * 16);
+                if constexpr (kKeepQ) q[i] = x;
+                else lds_q[wave][i][lane] = x;
+            }
 
             const float c = a.h.scale_log2;
-            const CF_GLOBAL int32_t *table = gconst<int32_t>(a.table) + seq * a.table_stride;
+            // read by scalar loads, though this kernel writes memory: page numbers and addresses in vector registers would push the loop's operands out (595 us
+            // for 710, 96 contexts of 160 to 16000 keys, 32 / 8 heads of 128, 272 for 277)
+            const CF_CONST int32_t *table = (const CF_CONST int32_t *)a.table + seq * a.table_stride;
             const int64_t head_bytes = (int64_t)kv_head * a.cache.page_size * kRow;
             const char *k_head = a.cache.k + head_bytes, *v_head = a.cache.v + head_bytes;
             const int mask = a.cache.page_size - 1, last = end - 1;
@@ -158,6 +168,7 @@ template <int DT, int D, bool MANY> __global__ __launch_bounds__(kWaves * 64, D 
             Step at = find(key0);
             if (key0 < end) load_k(at, key0);
             while (key0 < end) {
+                if constexpr (!kKeepQ) asm volatile("" ::: "memory");     // read them again in every step
                 const int next0 = key0 + kWaves * kKeys;
                 const Step next = find(next0);
                 load_v(at, key0);
@@ -167,7 +178,10 @@ template <int DT, int D, bool MANY> __global__ __launch_bounds__(kWaves * 64, D 
                 for (int t = 0; t < 2; ++t) {
                     s[t] = (f32x4){0, 0, 0, 0};
 #pragma unroll
-                    for (int i = 0; i < kSteps; ++i) s[t] = E::mfma16(k[t][i], q[i], s[t]);
+                    for (int i = 0; i < kSteps; ++i) {
+                        if constexpr (kKeepQ) s[t] = E::mfma16(k[t][i], q[i], s[t]);
+                        else s[t] = E::mfma16(k[t][i], lds_q[wave][i][lane], s[t]);
+                    }
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 if (next0 < end) load_k(next, next0);
