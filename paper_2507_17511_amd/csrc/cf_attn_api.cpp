@@ -136,19 +136,32 @@ JoinArgs parts_to_join(const Heads &h, const Parts &p, int n, const Rows &out, f
 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
-// Into how many parts the keys of `busy` workgroups are split: what takes the least time, where the device holds two workgroups a CU that
-// take 1.8 us over 64 keys of 128 elements, half a round of workgroups takes 0.6 of one, and the join moves the parts twice at 5 TB/s, 4 us at
-// least.  2 x 333 tokens over 20333 keys, 84 workgroups: 6 parts, 246 us.
+// How many workgroups of the prompt kernel a CU holds, what they take over 64 keys, us, and which share of that fewer of them take: one CU's worth of
+// whole tiles for each, 1 to 4 a CU (128 tiles of 64 keys 120 / 173 / 250 / 307 us at head_dim 64; 64 of them 82 / 133 at 128, 237 / 258 at 256).
+struct Pace {
+    int64_t per_cu;
+    double step_us, share[4];
+};
+Pace prompt_pace(int dim)
+{
+    if (dim == 64) return {4, 2.4, {0.39, 0.56, 0.81, 1.0}};
+    if (dim == 128) return {2, 1.95, {0.62, 1.0}};
+    return {2, 3.9, {0.92, 1.0}};
+}
+
+// Into how many parts the keys of `busy` workgroups are split: what takes the least time, where the join moves the parts twice at 5 TB/s, 4 us at least.
+// 2 x 333 tokens over 20333 keys, 84 workgroups: 6 parts, 235 us.
 int64_t prompt_splits(int64_t busy, int64_t longest, int64_t rows, int dim, int64_t most)
 {
-    const int64_t slots = 2 * kCUs, steps = (longest + 63) / 64;
-    const double step_us = 0.9 / 64.0 * dim, part_us = (double)rows * (dim + 1) * 4 * 2 / 5.0e6;
+    const Pace pace = prompt_pace(dim);
+    const int64_t slots = pace.per_cu * kCUs, steps = (longest + 63) / 64;
+    const double part_us = (double)rows * (dim + 1) * 4 * 2 / 5.0e6;
     int64_t best = 1;
     double least = 0.0;
     for (int64_t n = 1; n <= (most > 1 ? most : 1); ++n) {
         const int64_t rest = busy * n % slots;
-        const double rounds = (double)(busy * n / slots) + (rest == 0 ? 0.0 : rest <= kCUs ? 0.6 : 1.0);
-        const double us = rounds * (double)((steps + n - 1) / n) * step_us + (n > 1 ? 4.0 + part_us * (double)n : 0.0);
+        const double rounds = (double)(busy * n / slots) + (rest == 0 ? 0.0 : pace.share[(rest - 1) / kCUs]);
+        const double us = rounds * (double)((steps + n - 1) / n) * pace.step_us + (n > 1 ? 4.0 + part_us * (double)n : 0.0);
         if (n == 1 || us < least) {
             best = n;
             least = us;

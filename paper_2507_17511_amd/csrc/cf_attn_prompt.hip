@@ -95,11 +95,14 @@ __device__ __forceinline__ void stage(const char *base, uint32_t bytes, uint32_t
     __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (int)bytes, 0x00020000), (CF_LDS void *)to, 16, from, from_all, 0, 0);
 }
 
-template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, 2) void k_attn_prompt(PromptArgs a)
+template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 : 2) void k_attn_prompt(PromptArgs a)
 {
     using E = Elem<DT>;
     constexpr int kKeys = D == 256 ? 32 : 64;               // keys of a staged tile
-    constexpr bool kAhead = D != 256;                       // the next tile's scores are taken while this one's weights are computed
+    // Whether the next tile's scores are taken while this one's weights are computed.  Narrow heads do better with four workgroups a CU, of 128 registers a
+    // lane, that do this for one another (8192 tokens of 24 heads of 64 over as many keys: 476 us, three that take scores ahead 485, two 492; 14 of 1 to 2003
+    // tokens 49.7 / 49.4 / 54.4); wide ones lack the registers.
+    constexpr bool kAhead = D == 128;
     constexpr int kSteps = D / 16;                          // matrix instructions over the head dimension
     constexpr int kBlocks = D / 32;                         // 32-row blocks of O^T
     constexpr int kSub = kKeys / 32;
