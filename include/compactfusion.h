@@ -372,7 +372,7 @@ typedef struct {
     int64_t n_tokens;         /* >= 0 */
     cf_rows k, v;             /* [n_tokens][kv_heads][head_dim] */
     const int64_t *slots;     /* device [n_tokens]: where token t goes in the cache; a token with a slot outside the cache
-                                 (negative: padding) does not go there.  Two tokens of one call in one slot: either. */
+                                 (negative: padding) does not go there.  Two tokens of one call in one slot: elements of either. */
     cf_rows q, q_out;         /* [n_tokens][q_heads][head_dim]: rotated queries; data null: none.  q_out may be q itself. */
     const int32_t *positions; /* device [n_tokens]; a token whose position is not in [0, n_positions) is left out
                                  altogether.  Not read with rotary_dim 0. */

@@ -42,7 +42,8 @@ class PagedCache:
         _require(k.dim() == 4 and k.shape == v.shape and k.dtype == v.dtype and k.device == v.device, "k and v are [pages, kv_heads, page_size, head_dim], alike")
         pages, heads, page, dim = k.shape
         for x in (k, v):
-            _require(x.numel() > 0 and x[0].is_contiguous() and (pages == 1 or x.stride(0) == k.stride(0)), "pages are dense, and as far apart in k as in v")
+            _require(x.numel() > 0 and x[0].is_contiguous() and (pages == 1 or x.stride(0) == k.stride(0) >= heads * page * dim),
+                     "pages are dense, do not overlap, and are as far apart in k as in v")
         self.k, self.v = k, v
         self.heads, self.page_size, self.head_dim, self.dtype, self.index = heads, page, dim, k.dtype, k.get_device()
         self.struct = cf.cf_kv_cache(k.data_ptr(), v.data_ptr(), pages, k.stride(0) if pages > 1 else 0, page)
@@ -176,7 +177,7 @@ class AttentionSession:
         _require(table.dim() == 2 and table.shape[0] == n and table.dtype is torch.int32 and table.get_device() == self._index, "table is [sequences, pages] int32")
         row, entry = table.stride()
         cols = table.shape[1]
-        _require(cols == 1 or entry == 1, "the rows of table are dense")
+        _require((cols == 1 or entry == 1) and (n < 2 or row >= cols), "the rows of the table are dense and do not overlap")
         _PAGED.pack_into(self._paged, 0, n, cols, row if n > 1 else 0, max_len, table.data_ptr(), self._list(lens, torch.int32, n, "lens"),
                          *self._rows(q, n, self.q_heads, "q"), *self._rows(out, n, self.q_heads, "out"),
                          0 if lse is None else self._plain(lse, torch.float32, (n, self.q_heads), "lse"))

@@ -24,7 +24,7 @@ cf_status check_desc(const cf_attn_desc *d, Heads &h)
     if (d->dtype != CF_BF16 && d->dtype != CF_F16) return CF_ERR_UNSUPPORTED;
     if (d->head_dim != 64 && d->head_dim != 128 && d->head_dim != 256) return CF_ERR_UNSUPPORTED;
     if (d->kv_heads < 1 || d->q_heads < 1 || d->q_heads > 65536 || d->q_heads % d->kv_heads != 0) return CF_ERR_SHAPE;
-    if (!(d->scale >= 0.0f) || !(d->scale <= 3.0e38f)) return CF_ERR_INVALID_ARG;
+    if (!(d->scale >= 0.0f) || !(d->scale <= 2.0e38f)) return CF_ERR_INVALID_ARG;      // times log2 e it is finite
     h.dtype = d->dtype;
     h.q_heads = d->q_heads;
     h.kv_heads = d->kv_heads;
