@@ -297,13 +297,14 @@ cf_status cf_attn_paged(const cf_attn_desc *desc, const cf_kv_cache *cache, cons
     if (longest > kMostRows) longest = kMostRows;
     const int64_t units = args->n_seqs * (int64_t)a.h.kv_heads * ((a.h.group + kPagedHeads - 1) / kPagedHeads);
     const int64_t rows = (int64_t)args->n_seqs * a.h.q_heads;
-    // Two workgroups a CU, of 128 to 2048 keys each, and 32 parts at most where that gives every CU one: a part costs its join about 0.1 us, 128
+    // Two workgroups a CU, of 128 to 1024 keys each, and 32 parts at most where that gives every CU one: a part costs its join about 0.1 us, 128
     // keys a workgroup 1.2 us.  us, on one card: 1 x 901 keys, 2 heads of keys: parts of 128 / 256 / 512 keys 8.2 / 9.6 / 11.4; 1 x 8192, 8 heads: 128 / 256
-    // / 512 16.7 / 13.0 / 13.6; 8 x 8192, 8 heads: two / three / six workgroups a CU 45 / 49 / 53; 64 x 7 to 700: 14.5 / 18.1 / 16.1; 96 x 160 to
-    // 16000, 8 heads: parts of 512 / 1024 / 2048 keys 287 / 281 / 276, 96 x 3540 273 / 255 / 247.
+    // / 512 16.7 / 13.0 / 13.6; 8 x 8192, 8 heads: two / three / six workgroups a CU 45 / 49 / 53; 64 x 7 to 700: 14.5 / 18.1 / 16.1.  Parts of 512 / 1024 /
+    // 2048 keys, 8 heads of 128: 96 x 160 to 16000 275 / 273 / 271, 96 x 3540 264 / 251 / 243; of 256: 48 x 160 to 16000 282 / 279 / 300; of 64: 200 x 50
+    // to 5000 93 / 95 / 102; one of 128: 150 x 90 to 9000 33 / 35 / 57.
     int64_t keys = round_up((longest * units + 2 * kCUs - 1) / (2 * kCUs), 128);
     if (units * 32 >= kCUs && keys < longest / 32) keys = round_up(longest / 32, 128);
-    if (keys > 2048) keys = 2048;
+    if (keys > 1024) keys = 1024;
     int64_t splits = (longest + keys - 1) / keys;
     const int64_t fit = parts_that_fit(workspace_bytes, rows, a.h.head_dim);
     if (splits > fit) splits = fit;

@@ -5,7 +5,7 @@
 // of them is chosen so that a lane's 8 scores are those of 8 neighbouring keys, the right operand of O^T = V^T P^T.
 // For the left one a lane reads 8 (4, 16) elements of the same 8 keys and turns that block with byte permutes.
 //
-// Bound by HBM: 96 contexts of 160 to 16000 keys, 32 / 8 heads of 128, 274 us (5.1 TB/s); 2 of 131100, 24 heads of 64, 286 us (5.6 TB/s); one
+// Bound by HBM: 96 contexts of 160 to 16000 keys, 32 / 8 heads of 128, 272 us (5.1 TB/s); 2 of 131100, 24 heads of 64, 283 us (5.7 TB/s); one
 // of 901 keys, 8 / 2 heads, by latency: 7.3 us, of which the launch is a third.  Through LDS the same bytes would wait for a barrier a step, and the
 // products need 16 columns for the one to 16 heads that share keys, whoever brings them.
 #include "cf_attn_device.h"
