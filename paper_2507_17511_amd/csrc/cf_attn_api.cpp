@@ -319,7 +319,10 @@ cf_status cf_attn_paged(const cf_attn_desc *desc, const cf_kv_cache *cache, cons
     if (units * a.n_splits > kMostGrid) return CF_ERR_SHAPE;
     if (a.n_splits > 1) place_parts(a.parts, workspace, rows, a.n_splits, a.h.head_dim);
     a.counters = static_cast<uint32_t *>(workspace);
-    a.many = a.n_splits > 1 && units * a.n_splits > 4 * kCUs;
+    // Listed parts where there are more than the device holds, and where contexts that may differ could fill 128 MB: a workgroup for every part that there may
+    // be leaves those of the long contexts on a few XCDs.  us, one for each / listed: 8 x 270 to 27465 keys, 4 heads of 256, 85 / 39; 4 x 1270 to 126712, 4 of
+    // 128, 126 / 89; 16 x 40 to 4000, 8 of 128, 26 / 19, but 16 x 4000 43.1 / 44.2, 8 x 8192 43.6 / 45.8, 3 x 120 to 12000, 8 of 64, 11.6 / 12.8.
+    a.many = a.n_splits > 1 && (units * a.n_splits > 4 * kCUs || (a.n_seqs > 1 && units * longest * a.h.head_dim * 4 >= (int64_t)128 << 20));
     const hipStream_t s = static_cast<hipStream_t>(stream);
     hipError_t e = launch_paged(a, s);
     if (e == hipSuccess && a.many) {
