@@ -27,6 +27,7 @@ for _layout, _args in ((_APPEND, cf.cf_append), (_PROMPT, cf.cf_prompt), (_PAGED
     assert _layout.size == ctypes.sizeof(_args), _args
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # device index -> hipStream_t, without a Stream object
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _require(ok: bool, what: str) -> None:
@@ -88,6 +89,16 @@ class AttentionSession:
             return _raw_stream(self._index)
         return torch.cuda.current_stream(self.device).cuda_stream
 
+    # The library launches on the device that is current, and the null stream, torch's default one, is that device's.
+    def _call(self, entry, name: str, *args) -> None:
+        if self._index >= 0 and _current_device() != self._index:
+            with torch.cuda.device(self._index):
+                status = entry(*args, self._on())
+        else:
+            status = entry(*args, self._on())
+        if status:
+            raise cf.CFError(status, name)
+
     # An output is memory of the stream that it is written on: of another's it might still be in use there.
     def _new(self, shape, dtype: torch.dtype) -> torch.Tensor:
         if self._stream is None:
@@ -145,9 +156,7 @@ class AttentionSession:
             table = (shape[0], 2 * shape[1], interleaved)
         _APPEND.pack_into(self._append, 0, n, *self._rows(k, n, self.kv_heads, "k"), *self._rows(v, n, self.kv_heads, "v"),
                           self._list(slots, torch.int64, n, "slots"), *rows_q, *rows_out, *at, *table)
-        status = self._lib.cf_kv_append(self._desc, self._cache(cache), self._refs[0], self._on())
-        if status:
-            raise cf.CFError(status, "cf_kv_append")
+        self._call(self._lib.cf_kv_append, "cf_kv_append", self._desc, self._cache(cache), self._refs[0])
         return q_out
 
     def prompt(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor, cu_k: Optional[torch.Tensor] = None,
@@ -162,9 +171,7 @@ class AttentionSession:
         _PROMPT.pack_into(self._prompt, 0, n, causal, n_q, n_k, max_k, self._list(cu_q, torch.int32, n + 1, "cu_q"), self._list(cu_k, torch.int32, n + 1, "cu_k"),
                           *self._rows(q, n_q, self.q_heads, "q"), *self._rows(k, n_k, self.kv_heads, "k"), *self._rows(v, n_k, self.kv_heads, "v"),
                           *self._rows(out, n_q, self.q_heads, "out"), 0 if lse is None else self._plain(lse, torch.float32, (n_q, self.q_heads), "lse"))
-        status = self._lib.cf_attn_prompt(self._desc, self._refs[1], self._ws, self.ws_bytes, self._on())
-        if status:
-            raise cf.CFError(status, "cf_attn_prompt")
+        self._call(self._lib.cf_attn_prompt, "cf_attn_prompt", self._desc, self._refs[1], self._ws, self.ws_bytes)
         return out
 
     def paged(self, cache: PagedCache, q: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, out: Optional[torch.Tensor] = None,
@@ -181,9 +188,7 @@ class AttentionSession:
         _PAGED.pack_into(self._paged, 0, n, cols, row if n > 1 else 0, max_len, table.data_ptr(), self._list(lens, torch.int32, n, "lens"),
                          *self._rows(q, n, self.q_heads, "q"), *self._rows(out, n, self.q_heads, "out"),
                          0 if lse is None else self._plain(lse, torch.float32, (n, self.q_heads), "lse"))
-        status = self._lib.cf_attn_paged(self._desc, self._cache(cache), self._refs[2], self._ws, self.ws_bytes, self._on())
-        if status:
-            raise cf.CFError(status, "cf_attn_paged")
+        self._call(self._lib.cf_attn_paged, "cf_attn_paged", self._desc, self._cache(cache), self._refs[2], self._ws, self.ws_bytes)
         return out
 
     def join(self, parts: Sequence[torch.Tensor], lses: Sequence[torch.Tensor], out: Optional[torch.Tensor] = None,
@@ -202,7 +207,5 @@ class AttentionSession:
         s = (ctypes.c_void_p * n)(*[self._plain(x, torch.float32, shape[:2], "a log-sum-exp") for x in lses])
         _JOIN.pack_into(self._join, 0, n, _CF_DT[pdt], tokens, ctypes.addressof(p), ctypes.addressof(s), *self._rows(out, tokens, self.q_heads, "out"),
                         0 if lse is None else self._plain(lse, torch.float32, shape[:2], "lse"))
-        status = self._lib.cf_attn_join(self._desc, self._refs[3], self._on())
-        if status:
-            raise cf.CFError(status, "cf_attn_join")
+        self._call(self._lib.cf_attn_join, "cf_attn_join", self._desc, self._refs[3])
         return out

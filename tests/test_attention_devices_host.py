@@ -1,0 +1,84 @@
+"""On which device the library is called.  Kernels launched with the null stream run on the device that is current, so that a session must make
+its own current, whichever the caller has: with a stand-in for the library, needs no GPU."""
+import types
+
+import pytest
+import torch
+
+from paper_2507_17511_amd import attention
+from paper_2507_17511_amd.attention import AttentionSession
+
+
+class Tensor:
+    """As much of a tensor on some device as a session looks at."""
+    requires_grad = False
+
+    def __init__(self, shape, dtype=torch.bfloat16, index=1):
+        self.shape, self.dtype, self.index = torch.Size(shape), dtype, index
+        self.device = torch.device("cuda", index)
+
+    def get_device(self):
+        return self.index
+
+    def numel(self):
+        return self.shape.numel()
+
+    def dim(self):
+        return len(self.shape)
+
+    def stride(self):
+        return torch.empty(self.shape, device="meta").stride()
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return 1 << 20
+
+
+@pytest.fixture
+def machine(monkeypatch):
+    """Two devices, of which 0 is current; where `calls` were made."""
+    now = types.SimpleNamespace(device=0, calls=[])
+
+    class guard:
+        def __init__(self, device):
+            self.device = device if isinstance(device, int) else torch.device(device).index
+
+        def __enter__(self):
+            self.before, now.device = now.device, self.device
+
+        def __exit__(self, *error):
+            now.device = self.before
+
+    monkeypatch.setattr(torch.cuda, "device", guard)
+    monkeypatch.setattr(attention, "_current_device", lambda: now.device, raising=False)
+    monkeypatch.setattr(attention, "_raw_stream", lambda index: 0)
+
+    def entry(*args):
+        now.calls.append(now.device)
+        return 0
+
+    now.entry = entry
+    now.library = types.SimpleNamespace(**{name: entry for name in ("cf_kv_append", "cf_attn_prompt", "cf_attn_paged", "cf_attn_join")})
+    return now
+
+
+@pytest.mark.parametrize("mine,current", [(1, 0), (0, 1), (1, 1), (0, 0)])
+def test_attention_is_called_on_the_sessions_device(machine, mine, current):
+    machine.device = current
+    s = AttentionSession(4, 2, 64, device=f"cuda:{mine}", workspace_bytes=0)
+    s._lib = machine.library
+
+    def on(*shape, dtype=torch.bfloat16):
+        return Tensor(shape, dtype, mine)
+
+    cache = types.SimpleNamespace(heads=2, head_dim=64, dtype=torch.bfloat16, index=mine, ref=None, k=on(1), v=on(1))
+    numbers = on(3, dtype=torch.int32)
+    q, k, v, out = on(3, 4, 64), on(3, 2, 64), on(3, 2, 64), on(3, 4, 64)
+    table = on(3, 2, dtype=torch.int32)
+    s.append(cache, k, v, on(3, dtype=torch.int64), q=q, q_out=out)
+    s.prompt(q, k, v, on(2, dtype=torch.int32), out=out)
+    s.paged(cache, q, table, numbers, out=out)
+    s.join([q, q], [on(3, 4, dtype=torch.float32)] * 2, out=out)
+    assert machine.calls == [mine] * 4 and machine.device == current
