@@ -327,7 +327,8 @@ const char *cf_profile_kernel_name(const cf_ctx *ctx, int32_t k);
  * and the join of attentions over parts of the keys (the hops of ring attention, App. B Alg. 2).
  *
  * These calls have no context and keep nothing between calls.  They follow the rules above: device pointers of the
- * caller's, work enqueued on `stream` without synchronising, arguments validated on the host before anything is
+ * caller's, work enqueued on `stream`, a stream of the device that is current at the call (as the codec's calls: null is that
+ * device's), without synchronising, arguments validated on the host before anything is
  * enqueued, nothing allocated, nothing thrown.  They may be captured into a HIP graph.  Calls that share a workspace
  * must not overlap in time; calls that do not may run from any threads and on any streams.
  *

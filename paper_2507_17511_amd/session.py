@@ -3,12 +3,14 @@ scale and workspace buffers of a batch of layer tensors with torch and keeps the
 host pointer arrays.  No codec arithmetic happens here."""
 from __future__ import annotations
 
+import contextlib
 from typing import List, Optional, Sequence
 
 import torch
 
 import paper_2507_17511_amd as cf
 
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 _TORCH_DT = {cf.CF_F32: torch.float32, cf.CF_BF16: torch.bfloat16}
 
 
@@ -18,6 +20,8 @@ class CodecSession:
         self.descs = list(descs)
         self.opts = opts if opts is not None else cf.options()
         self.device = torch.device(device)
+        if self.device.type == "cuda" and self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
         self.n = len(self.descs)
         self.recon: List[torch.Tensor] = []
         self.err: List[torch.Tensor] = []
@@ -49,6 +53,10 @@ class CodecSession:
         s = self._stream if self._stream is not None else torch.cuda.current_stream(self.device)
         return s.cuda_stream
 
+    def _here(self):
+        """The session's device made current: the library launches on the one that is, and the null stream, torch's default one, is that device's."""
+        return contextlib.nullcontext() if _current_device() == self.device.index else torch.cuda.device(self.device)
+
     def _slice(self, arr, first, count):
         if first == 0 and count == self.n:
             return arr
@@ -61,26 +69,30 @@ class CodecSession:
 
     def warmup(self, x0, first: int = 0, count: Optional[int] = None) -> None:
         count = self.n - first if count is None else count
-        cf.cf_warmup(self.ctx, first, count, self._x(x0, count), self._slice(self.p_recon, first, count),
-                     self._slice(self.p_err, first, count), self.stream_handle)
+        with self._here():
+            cf.cf_warmup(self.ctx, first, count, self._x(x0, count), self._slice(self.p_recon, first, count),
+                         self._slice(self.p_err, first, count), self.stream_handle)
 
     def step_fused(self, x, first: int = 0, count: Optional[int] = None) -> None:
         count = self.n - first if count is None else count
-        cf.cf_step_fused(self.ctx, first, count, self._x(x, count), self._slice(self.p_recon, first, count),
-                         self._slice(self.p_err, first, count), self._slice(self.p_codes, first, count),
-                         self._slice(self.p_scales, first, count), self.stream_handle)
+        with self._here():
+            cf.cf_step_fused(self.ctx, first, count, self._x(x, count), self._slice(self.p_recon, first, count),
+                             self._slice(self.p_err, first, count), self._slice(self.p_codes, first, count),
+                             self._slice(self.p_scales, first, count), self.stream_handle)
 
     def compress(self, x, first: int = 0, count: Optional[int] = None) -> None:
         count = self.n - first if count is None else count
-        cf.cf_compress(self.ctx, first, count, self._x(x, count), self._slice(self.p_recon, first, count),
-                       self._slice(self.p_err, first, count), self._slice(self.p_codes, first, count),
-                       self._slice(self.p_scales, first, count), self.stream_handle)
+        with self._here():
+            cf.cf_compress(self.ctx, first, count, self._x(x, count), self._slice(self.p_recon, first, count),
+                           self._slice(self.p_err, first, count), self._slice(self.p_codes, first, count),
+                           self._slice(self.p_scales, first, count), self.stream_handle)
 
     def decompress(self, first: int = 0, count: Optional[int] = None, recon=None) -> None:
         count = self.n - first if count is None else count
         p_recon = self._slice(self.p_recon, first, count) if recon is None else cf.ptr_array(recon)
-        cf.cf_decompress(self.ctx, first, count, self._slice(self.p_codes, first, count),
-                         self._slice(self.p_scales, first, count), p_recon, self.stream_handle)
+        with self._here():
+            cf.cf_decompress(self.ctx, first, count, self._slice(self.p_codes, first, count),
+                             self._slice(self.p_scales, first, count), p_recon, self.stream_handle)
 
     def close(self) -> None:
         if self.ctx is not None:

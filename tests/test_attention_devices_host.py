@@ -5,7 +5,7 @@ import types
 import pytest
 import torch
 
-from paper_2507_17511_amd import attention
+from paper_2507_17511_amd import attention, session
 from paper_2507_17511_amd.attention import AttentionSession
 
 
@@ -52,7 +52,8 @@ def machine(monkeypatch):
             now.device = self.before
 
     monkeypatch.setattr(torch.cuda, "device", guard)
-    monkeypatch.setattr(attention, "_current_device", lambda: now.device, raising=False)
+    for module in (attention, session):
+        monkeypatch.setattr(module, "_current_device", lambda: now.device, raising=False)
     monkeypatch.setattr(attention, "_raw_stream", lambda index: 0)
 
     def entry(*args):
@@ -81,4 +82,21 @@ def test_attention_is_called_on_the_sessions_device(machine, mine, current):
     s.prompt(q, k, v, on(2, dtype=torch.int32), out=out)
     s.paged(cache, q, table, numbers, out=out)
     s.join([q, q], [on(3, 4, dtype=torch.float32)] * 2, out=out)
+    assert machine.calls == [mine] * 4 and machine.device == current
+
+
+@pytest.mark.parametrize("mine,current", [(1, 0), (0, 1), (1, 1), (0, 0)])
+def test_the_codec_is_called_on_the_sessions_device(machine, monkeypatch, mine, current):
+    machine.device = current
+    for name in ("cf_warmup", "cf_step_fused", "cf_compress", "cf_decompress"):
+        monkeypatch.setattr(session.cf, name, machine.entry)
+    s = session.CodecSession.__new__(session.CodecSession)          # its buffers are not looked at here
+    s.device, s.n, s.ctx, s._stream = torch.device("cuda", mine), 1, None, types.SimpleNamespace(cuda_stream=0)
+    s.p_recon = s.p_err = s.p_codes = s.p_scales = (None,)
+    x = Tensor((4, 64), index=mine)
+    monkeypatch.setattr(session.cf, "ptr_array", lambda xs: xs)
+    s.warmup([x])
+    s.step_fused([x])
+    s.compress([x])
+    s.decompress()
     assert machine.calls == [mine] * 4 and machine.device == current
