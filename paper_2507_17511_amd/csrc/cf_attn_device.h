@@ -27,12 +27,18 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int BF16 = 1, F16 = 2;    // cf_dtype
 constexpr float kLn2 = 0.693147180559945309f;
-// Where the running maximum (of scores times log2 e) begins: below every finite score, and not -infinity, so that
+// Where a row's reference, which its scores (times log2 e) are taken relative to, begins: below every finite score, and not -infinity, so that
 // score - maximum is -infinity, and the weight 0, for a masked score of a row that has seen no other.
 constexpr float kNoMax = -3.0e38f;
-// A row's accumulators are scaled down when a score passes the maximum in use by so many powers of two.  Weights then reach 2^8 at
-// most: their rounding is relative, sums of 2^31 of them stay finite in fp32, and 2^8 is far from the largest fp16.
-constexpr float kMaxSlack = 8.0f;
+// A row's accumulators are scaled down when a score passes the reference in use by more than Elem::kMostOver powers of two.  bf16: the reference is a maximum, weights
+// reach 2^8 at most, their rounding is relative, and sums of 2^31 of them stay finite in fp32.  fp16 holds numbers from 2^-14 on in full and none below 2^-25, and keys that weigh
+// less than that next to the largest may weigh much together.  So there the reference lies kLift below the maximum, and it follows the scores down, too: where all of a
+// row's keys at hand (64 at most) have scores less than kLeastOver over it, or weights that sum up to less than kLeastSum, it is lowered and the accumulators are
+// scaled up.  Their rounding is then within 2^-15 of their sum.  The sum of all weights stays below 2^kMostTotal; past kFullTotal nothing is lowered: what is at hand is below 2^-60 of the row.
+constexpr float kLeastOver = -4.0f;
+constexpr float kLeastSum = 0.0625f;
+constexpr float kMostTotal = 60.0f;
+constexpr float kFullTotal = 288230376151711744.0f;        // 2^58
 // Where the maximum is not looked for (see k_attn_prompt): the most that the weights of a lane's keys of one tile may sum up to.  No weight is
 // larger than that, so that all of them are finite in fp16.
 constexpr float kMostSum = 32768.0f;
@@ -50,6 +56,8 @@ template <uint32_t EXPONENT> struct OddPair {
 };
 template <> struct Elem<BF16> {
     using Odd = OddPair<0x7f80u>;
+    static constexpr bool kFollow = false;                          // whether the reference follows the scores down
+    static constexpr float kLift = 0.0f, kMostOver = 8.0f;
     static __device__ __forceinline__ uint32_t pack(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, bf16x2)); }
     static __device__ __forceinline__ float lo(uint32_t w) { return __uint_as_float(w << 16); }
     static __device__ __forceinline__ float hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
@@ -58,6 +66,8 @@ template <> struct Elem<BF16> {
 };
 template <> struct Elem<F16> {
     using Odd = OddPair<0x7c00u>;
+    static constexpr bool kFollow = true;
+    static constexpr float kLift = 6.0f, kMostOver = 14.0f;         // 32 weights of 2^6 stay below kMostSum
     static __device__ __forceinline__ uint32_t pack(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, f16x2)); }
     static __device__ __forceinline__ float lo(uint32_t w) { return (float)__builtin_bit_cast(f16x2, w)[0]; }
     static __device__ __forceinline__ float hi(uint32_t w) { return (float)__builtin_bit_cast(f16x2, w)[1]; }
@@ -87,6 +97,13 @@ __device__ __forceinline__ float sum_quarters(float x)
 {
     const u32x2 r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false));
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// The reference after keys whose largest score is `top`, given the largest part of the row's sum that a lane has.
+template <int DT> __device__ __forceinline__ float reference(float m, float top, float total)
+{
+    if constexpr (Elem<DT>::kFollow) return top > -__builtin_inff() ? fmaxf(top - Elem<DT>::kLift, m - fmaxf(kMostTotal - __log2f(total), 0.0f)) : m;
+    else return fmaxf(m, top);
 }
 
 __device__ __forceinline__ float lse_of(float m, float l) { return l > 0.0f || l != l ? (m + __log2f(l)) * kLn2 : -__builtin_inff(); }

@@ -194,8 +194,18 @@ template <int DT, int D, bool MANY> __global__ __launch_bounds__(kWaves * 64, D 
                     top = fmaxf(top, s[j >> 2][j & 3]);
                 }
                 top *= c;
-                if (__any(top > m + kMaxSlack)) {
-                    const float fresh = fmaxf(m, max_quarters(max_halves(top))), scale = exp2_fast(m - fresh);
+                bool moves = __any(top > m + E::kMostOver);
+                if constexpr (E::kFollow) {     // a row's four lanes: has one of them a key that is near enough?
+                    uint64_t near = __ballot(!(top < m + kLeastOver));
+                    near |= near >> 32;
+                    near |= near >> 16;
+                    if ((near & 0xffff) != 0xffff) {
+                        const float row_top = max_quarters(max_halves(top));
+                        moves |= __any(row_top < m + kLeastOver && row_top > -__builtin_inff() && max_quarters(max_halves(l)) < kFullTotal);
+                    }
+                }
+                if (moves) {
+                    const float fresh = reference<DT>(m, max_quarters(max_halves(top)), E::kFollow ? max_quarters(max_halves(l)) : 0.0f), scale = exp2_fast(m - fresh);
 #pragma unroll
                     for (int d = 0; d < kPer; ++d)
 #pragma unroll

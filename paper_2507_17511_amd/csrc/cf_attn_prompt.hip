@@ -228,7 +228,7 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 :
         return max_halves(top) * c;
     };
     auto rescale = [&](float top) {
-        const float fresh = fmaxf(m, top), scale = exp2_fast(m - fresh);
+        const float fresh = reference<DT>(m, top, E::kFollow ? max_halves(l) : 0.0f), scale = exp2_fast(m - fresh);
 #pragma unroll
         for (int d = 0; d < kBlocks; ++d)
 #pragma unroll
@@ -277,19 +277,27 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 :
     // Tiles that all rows of the wave see, up to the last but one.  Their maximum is not looked for: weights are positive, so
     // that none is larger than their sum.  Where that passes kMostSum, in any lane, the tile is done again after its maximum has been taken and the
     // accumulators scaled; most often that is the first tile alone.  That happens outside of the inner loop, where the compiler keeps them in place.
-    // A tile is done again once, for a lane's weights sum up to less than 2 * 32 then: either scores are rounded as the maximum is, or that is
+    // A tile is done again once, for a lane's weights sum up to less than 2^kLift * 2 * 32 then, and too little once is enough: either scores are rounded as the maximum is, or that is
     // kMostExact at most, and the wave of a row beyond it, whose scores are of no use, infinite or none, takes the loop after this one.  The rounding costs
     // 16384 rows of 24 heads of 128 3022 us for 2937; with the way out instead of it, wide heads' accumulators would leave the registers (325 us for
     // 245: 2 x 333 tokens over 20333 keys).
+    int settled = 0;            // the tile that the reference was set for
+    // Whether a tile has to be done again: its weights sum up to too much, or in fp16 to too little.
+    auto unfit = [&](float sum) -> bool {
+        if constexpr (!E::kFollow) return __any(sum > kMostSum);
+        if (!__any(sum > kMostSum || sum < kLeastSum)) return false;
+        return __any(sum > kMostSum) || (key0 != settled && __any(sum_halves(sum) < kLeastSum && max_halves(l) < kFullTotal));
+    };
     if constexpr (kAhead) {
         while (key0 + 2 * kKeys <= edge) {
             rescale(largest(s));
+            settled = key0;
             if (__any(fabsf(m) > kMostExact)) break;
             do {
                 f32x16 next[kSub];
                 scores(next, buffer ^ kTile);
                 const float sum = weights(std::false_type{});
-                if (__any(sum > kMostSum)) break;
+                if (unfit(sum)) break;
                 l += sum;
                 products();
 #pragma unroll
@@ -301,10 +309,11 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 :
         while (key0 + kKeys <= edge) {
             scores(s, buffer);
             rescale(largest(s));
+            settled = key0;
             do {
                 scores(s, buffer);
                 const float sum = weights(std::true_type{});
-                if (__any(sum > kMostSum)) break;
+                if (unfit(sum)) break;
                 l += sum;
                 products();
                 advance();
@@ -334,7 +343,7 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 :
                 }
         }
         const float top = largest(s);
-        if (__any(top > m + kMaxSlack)) rescale(top);
+        if (__any(top > m + E::kMostOver || (E::kFollow && top < m + kLeastOver && top > -__builtin_inff() && max_halves(l) < kFullTotal))) rescale(top);
         l += weights(std::true_type{});
         again |= __any(E::Odd::any(odd)) != 0;
         products();
