@@ -285,7 +285,7 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 :
     // Whether a tile has to be done again: its weights sum up to too much, or in fp16 to too little.
     auto unfit = [&](float sum) -> bool {
         if constexpr (!E::kFollow) return __any(sum > kMostSum);
-        if (!__any(sum > kMostSum || sum < kLeastSum)) return false;
+        if (__builtin_expect(!__any(sum > kMostSum || sum < kLeastSum), 1)) return false;
         return __any(sum > kMostSum) || (key0 != settled && __any(sum_halves(sum) < kLeastSum && max_halves(l) < kFullTotal));
     };
     if constexpr (kAhead) {
@@ -321,18 +321,27 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 :
         }
     }
     // The last of them, and tiles of which some rows see a part.
-    bool again = false;
+    auto mask = [&](int key0) {
+#pragma unroll
+        for (int b = 0; b < kSub; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (b * 32 + 8 * (i >> 2) + (i & 3) >= seen - key0 - 4 * half) s[b][i] = -__builtin_inff();
+    };
+    // Takes s in.
+    auto weigh = [&]() {
+        const float top = largest(s);
+        if (__any(top > m + E::kMostOver || (E::kFollow && top < m + kLeastOver && top > -__builtin_inff() && max_halves(l) < kFullTotal))) rescale(top);
+        l += weights(std::true_type{});
+    };
+    int odd_from = limit;       // the tiles from here on are done at the end
     while (key0 < limit) {
-        uint32_t odd = 0;
         if constexpr (!kAhead) scores(s, buffer);
         if (key0 + kKeys > edge) {
-#pragma unroll
-            for (int b = 0; b < kSub; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (b * 32 + 8 * (i >> 2) + (i & 3) >= seen - key0 - 4 * half) s[b][i] = -__builtin_inff();
-            // A weight of zero does not keep an infinity or NaN out of a sum.  Is there one among the values that not all rows see, the wave's rows are
-            // computed once more at the end.
+            mask(key0);
+            // A weight of zero does not keep an infinity or NaN out of a sum.  Is there one among the values that not all rows see, this tile and the one after it,
+            // if there is one, wait for the end.
+            uint32_t odd = 0;
 #pragma unroll 1
             for (int g = max(edge - key0, 0) >> 4; g < kSub * 2; ++g)
 #pragma unroll
@@ -341,11 +350,12 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 :
 #pragma unroll
                     for (int w = 0; w < 4; ++w) odd |= E::Odd::carry(v[w]);
                 }
+            if (__builtin_expect(__any(E::Odd::any(odd)) != 0, 0)) {
+                odd_from = key0;
+                break;
+            }
         }
-        const float top = largest(s);
-        if (__any(top > m + E::kMostOver || (E::kFollow && top < m + kLeastOver && top > -__builtin_inff() && max_halves(l) < kFullTotal))) rescale(top);
-        l += weights(std::true_type{});
-        again |= __any(E::Odd::any(odd)) != 0;
+        weigh();
         products();
         if (kAhead && key0 + kKeys < limit) scores(s, buffer ^ kTile);
         advance();
@@ -353,46 +363,69 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 :
     // Tiles that only other waves see.
     while (key0 < end) advance();
 
-    // All waves have left the tiles behind.  A wave turns its rows in LDS, 128 columns at a time, so that it stores whole lines.
-    l = sum_halves(l);
     if (row0 >= rows) return;
-    // Key by key, to the rows that see it.  Here, where the loops above are over, this costs them no registers: done within them, it cost 14 prompts of 1 to
-    // 2003 tokens 101 us for 89, 50 of 128 54 for 42.
-    if (again) {
-        auto scaled = [&](int key) {
-            const char *from = k_base + key * (int64_t)a.k.token + half * 16;
+    // The tiles with infinities or NaN among values that not all rows see, as above, but from memory, and with zeros in the place of these: that leaves all sums
+    // that they are no part of as they are, to the last bit.  Then they are added, key by key, to the rows that see them.  Here, where the loops above are over, this costs
+    // them no registers: done within them, it cost 14 prompts of 1 to 2003 tokens 101 us for 89, 50 of 128 54 for 42.  16384 tokens of 4 heads of 64 / 128 / 256, causal,
+    // with a NaN in the last value: 272 / 490 / 1060 us, without it 278 / 337 / 904.
+    if (__builtin_expect(odd_from < limit, 0)) {
+#pragma unroll 1
+        for (int first = odd_from; first < limit; first += kKeys) {
+#pragma unroll
+            for (int b = 0; b < kSub; ++b) {
+                const char *from = k_base + min(first + b * 32 + col, t.len_k - 1) * (int64_t)a.k.token + half * 16;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[b][i] = 0.0f;
+#pragma unroll
+                for (int i = 0; i < kSteps; ++i) s[b] = E::mfma32(*gconst<u32x4>(from + i * 32), q[i], s[b]);
+            }
+            mask(first);
+            weigh();
+#pragma unroll
+            for (int g = 0; g < kSub * 2; ++g)
+#pragma unroll
+                for (int d = 0; d < kBlocks; ++d) {
+                    u32x4 v;
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        uint32_t x[2];
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const int key = first + g * 16 + half * 4 + (w >> 1) * 8 + (w & 1) * 2 + j;
+                            x[j] = *gconst<uint16_t>(v_base + min(key, t.len_k - 1) * (int64_t)a.v.token + d * 64 + col * 2);
+                            if (key >= t.len_k || E::Odd::any(E::Odd::carry(x[j]))) x[j] = 0;
+                        }
+                        v[w] = x[0] | x[1] << 16;
+                    }
+                    o[d] = E::mfma32(v, p[g], o[d]);
+                }
+        }
+#pragma unroll 1
+        for (int key = odd_from; key < limit; ++key) {
+            const char *k_from = k_base + key * (int64_t)a.k.token + half * 16, *v_from = v_base + key * (int64_t)a.v.token + half * 8;
             float sum = 0.0f;
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
-                const u32x4 k = *gconst<u32x4>(from + i * 32);
+                const u32x4 k = *gconst<u32x4>(k_from + i * 32);
 #pragma unroll
                 for (int w = 0; w < 4; ++w) sum = __builtin_fmaf(E::lo(k[w]), E::lo(q[i][w]), __builtin_fmaf(E::hi(k[w]), E::hi(q[i][w]), sum));
             }
-            return key < seen ? sum_halves(sum) * c : -__builtin_inff();
-        };
-        m = kNoMax;
-        l = 0.0f;
-#pragma unroll
-        for (int d = 0; d < kBlocks; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
-#pragma unroll 1
-        for (int key = split_begin; key < limit; ++key) m = fmaxf(m, scaled(key));
-#pragma unroll 1
-        for (int key = split_begin; key < limit; ++key) {
-            const float exact = exp2_fast(scaled(key) - m), weight = E::lo(E::pack(exact, 0.0f));
-            const char *from = v_base + key * (int64_t)a.v.token + half * 8;
-            l += exact;
+            const float weight = exp2_fast(sum_halves(sum) * c - m);
 #pragma unroll
             for (int d = 0; d < kBlocks; ++d)
 #pragma unroll
                 for (int i = 0; i < 16; i += 4) {
-                    const u32x2 v = *gconst<u32x2>(from + d * 64 + i * 4);
+                    const u32x2 v = *gconst<u32x2>(v_from + d * 64 + i * 4);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) o[d][i + j] = key < seen ? __builtin_fmaf(weight, j & 1 ? E::hi(v[j >> 1]) : E::lo(v[j >> 1]), o[d][i + j]) : o[d][i + j];
+                    for (int j = 0; j < 4; ++j) {
+                        const float x = j & 1 ? E::hi(v[j >> 1]) : E::lo(v[j >> 1]);
+                        if (key < seen && !(fabsf(x) < __builtin_inff())) o[d][i + j] = __builtin_fmaf(weight, x, o[d][i + j]);
+                    }
                 }
         }
     }
+    // All waves have left the tiles behind.  A wave turns its rows in LDS, 128 columns at a time, so that it stores whole lines.
+    l = sum_halves(l);
     const float inv = inverse_of(l);
     if (l == 0.0f)              // no key, or none with a score above -infinity: 0 times an infinite value is none of the row's
 #pragma unroll
