@@ -58,7 +58,8 @@ class PagedCache:
 
 
 class AttentionSession:
-    """The geometry of a model's attention on one device, and the workspace of its calls: one stream at a time."""
+    """The geometry of a model's attention on one device, and the workspace of its calls: one stream at a time.  Calls go to the session's own
+    stream, if it has one, or to the current one.  As with every stream but their own, tensors are kept until the work on them is done, or recorded on that stream; the workspace is."""
 
     def __init__(self, q_heads: int, kv_heads: int, head_dim: int, dtype: torch.dtype = torch.bfloat16, scale: float = 0.0,
                  device: str | torch.device = "cuda:0", stream: Optional[torch.cuda.Stream] = None,
@@ -73,11 +74,16 @@ class AttentionSession:
         self._lib = cf.lib()
         self._desc = ctypes.byref(self.desc)
         self.ws_bytes = workspace_bytes
-        self.workspace = torch.zeros(workspace_bytes, dtype=torch.uint8, device=self.device) if workspace_bytes else None
-        if workspace_bytes and self.device.type == "cuda" and not torch.cuda.is_current_stream_capturing():
-            torch.cuda.current_stream(self.device).synchronize()        # zeros on whichever stream the first call is
-        self._ws = self.workspace.data_ptr() if workspace_bytes else None
         self._stream = stream
+        # The workspace is memory of the session's stream, or else of the current one, and recorded on every other that a call goes to.
+        self._streams = {None if stream is None else stream.cuda_stream}
+        self.workspace = self._ws = None
+        if workspace_bytes:
+            with torch.cuda.stream(stream):
+                self.workspace = torch.zeros(workspace_bytes, dtype=torch.uint8, device=self.device)
+            self._ws = self.workspace.data_ptr()
+            if stream is None and self.device.type == "cuda" and not torch.cuda.is_current_stream_capturing():
+                torch.cuda.current_stream(self.device).synchronize()        # zeros on whichever stream the first call is
         # the arguments of the call in hand, and how the library is handed them
         self._append, self._prompt, self._paged, self._join = cf.cf_append(), cf.cf_prompt(), cf.cf_paged(), cf.cf_join()
         self._refs = [ctypes.byref(x) for x in (self._append, self._prompt, self._paged, self._join)]
@@ -91,11 +97,16 @@ class AttentionSession:
 
     # The library launches on the device that is current, and the null stream, torch's default one, is that device's.
     def _call(self, entry, name: str, *args) -> None:
+        on = self._on()
+        if on not in self._streams:
+            if self.workspace is not None:
+                self.workspace.record_stream(torch.cuda.current_stream(self.device))
+            self._streams.add(on)
         if self._index >= 0 and _current_device() != self._index:
             with torch.cuda.device(self._index):
-                status = entry(*args, self._on())
+                status = entry(*args, on)
         else:
-            status = entry(*args, self._on())
+            status = entry(*args, on)
         if status:
             raise cf.CFError(status, name)
 

@@ -100,3 +100,21 @@ def test_the_codec_is_called_on_the_sessions_device(machine, monkeypatch, mine, 
     s.compress([x])
     s.decompress()
     assert machine.calls == [mine] * 4 and machine.device == current
+
+
+def test_the_workspace_is_recorded_on_every_stream_that_uses_it(machine, monkeypatch):
+    """The allocator must not hand it out again while a call on some other stream than the one it was made on is under way."""
+    now, recorded = types.SimpleNamespace(handle=0), []
+    monkeypatch.setattr(attention, "_raw_stream", lambda index: now.handle)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: types.SimpleNamespace(cuda_stream=now.handle))
+    s = AttentionSession(4, 2, 64, device="cuda:0", workspace_bytes=0)
+    s._lib, s.ws_bytes = machine.library, 1 << 20
+    s.workspace, s._ws = types.SimpleNamespace(record_stream=lambda stream: recorded.append(stream.cuda_stream)), 1 << 20
+    cache = types.SimpleNamespace(heads=2, head_dim=64, dtype=torch.bfloat16, index=0, ref=None, k=Tensor((1,)), v=Tensor((1,)))
+    q, k, v, out = (Tensor((3, h, 64), index=0) for h in (4, 2, 2, 4))
+    starts, table, lens = (Tensor(shape, torch.int32, 0) for shape in ((2,), (3, 2), (3,)))
+    for handle in (0, 0, 7, 7, 9, 7, 0):
+        now.handle = handle
+        s.prompt(q, k, v, starts, out=out)
+        s.paged(cache, q, table, lens, out=out)
+    assert set(recorded) >= {7, 9} and len(recorded) <= 3       # each once, the one it was made on at most once

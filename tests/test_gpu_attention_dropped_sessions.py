@@ -1,0 +1,36 @@
+"""Sessions that are dropped while a call of theirs on a busy stream is yet to run: memory that is allocated next is not their workspace."""
+import pytest
+import torch
+
+import paper_2507_17511_amd as cf
+from paper_2507_17511_amd.attention import AttentionSession
+from test_gpu_attention import DEV
+from test_gpu_attention_streams import D, HK, HQ, busy, check_out, problem
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("own", [False, True])
+def test_a_session_dropped_before_its_call_runs(own):
+    cache, q, table, lens = problem()
+    work, side = torch.randn(6144, 6144, device=DEV).bfloat16(), torch.cuda.Stream()
+    torch.mm(work, work)
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    with torch.cuda.stream(side):
+        busy(work)
+    if own:
+        s = AttentionSession(HQ, HK, D, stream=side)
+        workspace = s.workspace.data_ptr()
+        out = s.paged(cache, q, table, lens)
+    else:
+        s = AttentionSession(HQ, HK, D)
+        workspace = s.workspace.data_ptr()
+        with torch.cuda.stream(side):
+            out = s.paged(cache, q, table, lens)
+    assert not side.query()
+    del s
+    junk = [torch.full((cf.CF_ATTN_WORKSPACE_BYTES,), 255, dtype=torch.uint8, device=DEV) for _ in range(3)]
+    assert not side.query() and all(j.data_ptr() != workspace for j in junk)
+    torch.cuda.synchronize()
+    check_out(cache, q, out)
