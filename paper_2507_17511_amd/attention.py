@@ -78,11 +78,13 @@ class AttentionSession:
         # The workspace is memory of the session's stream, or else of the current one, and recorded on every other that a call goes to.
         self._streams = {None if stream is None else stream.cuda_stream}
         self.workspace = self._ws = None
+        self._unset = False         # whether the workspace's zeros were captured into a graph, which is yet to run
         if workspace_bytes:
-            with torch.cuda.stream(stream):
+            with torch.cuda.device(self._index), torch.cuda.stream(stream):
                 self.workspace = torch.zeros(workspace_bytes, dtype=torch.uint8, device=self.device)
+                self._unset = self._index >= 0 and torch.cuda.is_current_stream_capturing()
             self._ws = self.workspace.data_ptr()
-            if stream is None and self.device.type == "cuda" and not torch.cuda.is_current_stream_capturing():
+            if stream is None and self._index >= 0 and not self._unset:
                 torch.cuda.current_stream(self.device).synchronize()        # zeros on whichever stream the first call is
         # the arguments of the call in hand, and how the library is handed them
         self._append, self._prompt, self._paged, self._join = cf.cf_append(), cf.cf_prompt(), cf.cf_paged(), cf.cf_join()
@@ -102,6 +104,10 @@ class AttentionSession:
             if self.workspace is not None:
                 self.workspace.record_stream(torch.cuda.current_stream(self.device))
             self._streams.add(on)
+        if self._unset:
+            with torch.cuda.device(self._index), torch.cuda.stream(self._stream):
+                self.workspace[:cf.CF_ATTN_COUNTER_BYTES].zero_()
+                self._unset = torch.cuda.is_current_stream_capturing()
         if self._index >= 0 and _current_device() != self._index:
             with torch.cuda.device(self._index):
                 status = entry(*args, on)

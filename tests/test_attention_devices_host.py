@@ -118,3 +118,30 @@ def test_the_workspace_is_recorded_on_every_stream_that_uses_it(machine, monkeyp
         s.prompt(q, k, v, starts, out=out)
         s.paged(cache, q, table, lens, out=out)
     assert set(recorded) >= {7, 9} and len(recorded) <= 3       # each once, the one it was made on at most once
+
+
+def test_a_workspace_made_during_a_capture_is_zero_for_calls_outside_of_it(machine, monkeypatch):
+    """The fill that zeroes it is captured, not run: calls until the first one outside of a capture zero the counters themselves."""
+    capturing, found = [True], []
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing[0])
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: types.SimpleNamespace(cuda_stream=0))
+    monkeypatch.setattr(torch, "zeros", lambda n, dtype, device: torch.full((n,), 255, dtype=dtype))
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda x, stream: None)
+    s = AttentionSession(4, 2, 64, device="cuda:0", workspace_bytes=1 << 20)
+    counters = s.workspace[:attention.cf.CF_ATTN_COUNTER_BYTES]
+
+    def entry(*args):
+        found.append(int(counters.max()))
+        return 0
+
+    s._lib = types.SimpleNamespace(cf_attn_paged=entry)
+    cache = types.SimpleNamespace(heads=2, head_dim=64, dtype=torch.bfloat16, index=0, ref=None, k=Tensor((1,)), v=Tensor((1,)))
+    q, out, table, lens = Tensor((3, 4, 64), index=0), Tensor((3, 4, 64), index=0), Tensor((3, 2), torch.int32, 0), Tensor((3,), torch.int32, 0)
+    for now in (True, True, False, True, False):
+        capturing[0] = now
+        s.paged(cache, q, table, lens, out=out)
+        if now and len(found) < 3:
+            counters.fill_(255)             # what the captured call did has not happened
+        elif len(found) == 3:
+            counters[5] = 9                 # every call leaves them zero, so that no later one has to: this would stay
+    assert found == [0, 0, 0, 9, 9]

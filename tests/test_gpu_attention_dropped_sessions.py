@@ -1,4 +1,5 @@
-"""Sessions that are dropped while a call of theirs on a busy stream is yet to run: memory that is allocated next is not their workspace."""
+"""Sessions that are dropped while a call of theirs on a busy stream is yet to run: memory that is allocated next is not their workspace.  And one that is made
+during a capture, where its zero fill is only recorded."""
 import pytest
 import torch
 
@@ -34,3 +35,22 @@ def test_a_session_dropped_before_its_call_runs(own):
     assert not side.query() and all(j.data_ptr() != workspace for j in junk)
     torch.cuda.synchronize()
     check_out(cache, q, out)
+
+
+def test_a_session_made_during_a_capture():
+    cache, q, table, lens = problem()
+    AttentionSession(HQ, HK, D).paged(cache, q, table, lens)
+    out, graph = torch.empty_like(q), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        s = AttentionSession(HQ, HK, D)
+        s.paged(cache, q, table, lens, out=out)
+    check_out(cache, q, s.paged(cache, q, table, lens))         # before the graph has run
+    for _ in range(3):
+        out.fill_(7.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        check_out(cache, q, out)
+        check_out(cache, q, s.paged(cache, q, table, lens))
+        torch.cuda.synchronize()
