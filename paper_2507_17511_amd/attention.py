@@ -99,6 +99,8 @@ class AttentionSession:
 
     # The library launches on the device that is current, and the null stream, torch's default one, is that device's.
     def _call(self, entry, name: str, *args) -> None:
+        if self._index < 0:
+            raise ValueError(f"attention runs on a GPU: the session's device is {self.device}")
         on = self._on()
         if on not in self._streams:
             if self.workspace is not None:
@@ -108,7 +110,7 @@ class AttentionSession:
             with torch.cuda.device(self._index), torch.cuda.stream(self._stream):
                 self.workspace[:cf.CF_ATTN_COUNTER_BYTES].zero_()
                 self._unset = torch.cuda.is_current_stream_capturing()
-        if self._index >= 0 and _current_device() != self._index:
+        if _current_device() != self._index:
             with torch.cuda.device(self._index):
                 status = entry(*args, on)
         else:

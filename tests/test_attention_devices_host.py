@@ -145,3 +145,19 @@ def test_a_workspace_made_during_a_capture_is_zero_for_calls_outside_of_it(machi
         elif len(found) == 3:
             counters[5] = 9                 # every call leaves them zero, so that no later one has to: this would stay
     assert found == [0, 0, 0, 9, 9]
+
+
+def test_tensors_of_the_host_do_not_reach_the_library():
+    """Its kernels would read and write the host's addresses."""
+    calls = []
+    s = AttentionSession(4, 2, 64, device="cpu", workspace_bytes=0, stream=types.SimpleNamespace(cuda_stream=0))
+    s._lib = types.SimpleNamespace(**{name: lambda *a: calls.append(a) or 0 for name in ("cf_kv_append", "cf_attn_prompt", "cf_attn_paged", "cf_attn_join")})
+    q, k, v = (torch.zeros(3, h, 64, dtype=torch.bfloat16) for h in (4, 2, 2))
+    cache = attention.PagedCache.empty(3, 2, 64, page_size=16, device="cpu")
+    numbers, starts = torch.ones(3, dtype=torch.int32), torch.tensor([0, 3], dtype=torch.int32)
+    out = torch.empty_like(q)
+    for call in (lambda: s.append(cache, k, v, torch.arange(3), q=q, q_out=out), lambda: s.prompt(q, k, v, starts, out=out),
+                 lambda: s.paged(cache, q, torch.zeros(3, 2, dtype=torch.int32), numbers, out=out), lambda: s.join([q, q], [torch.zeros(3, 4)] * 2, out=out)):
+        with pytest.raises(ValueError, match="cpu"):
+            call()
+    assert not calls
