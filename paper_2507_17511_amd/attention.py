@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import struct
+import threading
 from typing import Optional, Sequence
 
 import torch
@@ -57,8 +58,16 @@ class PagedCache:
         return cls(kv[0], kv[1])
 
 
+class _Arguments(threading.local):
+    """A thread's structures for the call in hand: the interpreter's lock is free while the library reads them."""
+
+    def __init__(self):
+        self.append, self.prompt, self.paged, self.join = cf.cf_append(), cf.cf_prompt(), cf.cf_paged(), cf.cf_join()
+        self.refs = [ctypes.byref(x) for x in (self.append, self.prompt, self.paged, self.join)]
+
+
 class AttentionSession:
-    """The geometry of a model's attention on one device, and the workspace of its calls: one stream at a time.  Calls go to the session's own
+    """The geometry of a model's attention on one device, and the workspace of its calls: one stream at a time, from any threads.  Calls go to the session's own
     stream, if it has one, or to the current one.  As with every stream but their own, tensors are kept until the work on them is done, or recorded on that stream; the workspace is."""
 
     def __init__(self, q_heads: int, kv_heads: int, head_dim: int, dtype: torch.dtype = torch.bfloat16, scale: float = 0.0,
@@ -86,9 +95,7 @@ class AttentionSession:
             self._ws = self.workspace.data_ptr()
             if stream is None and self._index >= 0 and not self._unset:
                 torch.cuda.current_stream(self.device).synchronize()        # zeros on whichever stream the first call is
-        # the arguments of the call in hand, and how the library is handed them
-        self._append, self._prompt, self._paged, self._join = cf.cf_append(), cf.cf_prompt(), cf.cf_paged(), cf.cf_join()
-        self._refs = [ctypes.byref(x) for x in (self._append, self._prompt, self._paged, self._join)]
+        self._arguments = _Arguments()
 
     def _on(self) -> int:
         if self._stream is not None:
@@ -173,9 +180,10 @@ class AttentionSession:
             at = (self._list(positions, torch.int32, n, "positions"), self._plain(cos, torch.float32, shape, "cos"),
                   self._plain(sin, torch.float32, shape, "sin"))
             table = (shape[0], 2 * shape[1], interleaved)
-        _APPEND.pack_into(self._append, 0, n, *self._rows(k, n, self.kv_heads, "k"), *self._rows(v, n, self.kv_heads, "v"),
+        mine = self._arguments
+        _APPEND.pack_into(mine.append, 0, n, *self._rows(k, n, self.kv_heads, "k"), *self._rows(v, n, self.kv_heads, "v"),
                           self._list(slots, torch.int64, n, "slots"), *rows_q, *rows_out, *at, *table)
-        self._call(self._lib.cf_kv_append, "cf_kv_append", self._desc, self._cache(cache), self._refs[0])
+        self._call(self._lib.cf_kv_append, "cf_kv_append", self._desc, self._cache(cache), mine.refs[0])
         return q_out
 
     def prompt(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor, cu_k: Optional[torch.Tensor] = None,
@@ -187,10 +195,11 @@ class AttentionSession:
         _require(n >= 0, "cu_q has an entry more than there are sequences")
         if out is None:
             out = self._new(q.shape, self.dtype)
-        _PROMPT.pack_into(self._prompt, 0, n, causal, n_q, n_k, max_k, self._list(cu_q, torch.int32, n + 1, "cu_q"), self._list(cu_k, torch.int32, n + 1, "cu_k"),
+        mine = self._arguments
+        _PROMPT.pack_into(mine.prompt, 0, n, causal, n_q, n_k, max_k, self._list(cu_q, torch.int32, n + 1, "cu_q"), self._list(cu_k, torch.int32, n + 1, "cu_k"),
                           *self._rows(q, n_q, self.q_heads, "q"), *self._rows(k, n_k, self.kv_heads, "k"), *self._rows(v, n_k, self.kv_heads, "v"),
                           *self._rows(out, n_q, self.q_heads, "out"), 0 if lse is None else self._plain(lse, torch.float32, (n_q, self.q_heads), "lse"))
-        self._call(self._lib.cf_attn_prompt, "cf_attn_prompt", self._desc, self._refs[1], self._ws, self.ws_bytes)
+        self._call(self._lib.cf_attn_prompt, "cf_attn_prompt", self._desc, mine.refs[1], self._ws, self.ws_bytes)
         return out
 
     def paged(self, cache: PagedCache, q: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, out: Optional[torch.Tensor] = None,
@@ -204,10 +213,11 @@ class AttentionSession:
         row, entry = table.stride()
         cols = table.shape[1]
         _require((cols == 1 or entry == 1) and (n < 2 or row >= cols), "the rows of the table are dense and do not overlap")
-        _PAGED.pack_into(self._paged, 0, n, cols, row if n > 1 else 0, max_len, table.data_ptr(), self._list(lens, torch.int32, n, "lens"),
+        mine = self._arguments
+        _PAGED.pack_into(mine.paged, 0, n, cols, row if n > 1 else 0, max_len, table.data_ptr(), self._list(lens, torch.int32, n, "lens"),
                          *self._rows(q, n, self.q_heads, "q"), *self._rows(out, n, self.q_heads, "out"),
                          0 if lse is None else self._plain(lse, torch.float32, (n, self.q_heads), "lse"))
-        self._call(self._lib.cf_attn_paged, "cf_attn_paged", self._desc, self._cache(cache), self._refs[2], self._ws, self.ws_bytes)
+        self._call(self._lib.cf_attn_paged, "cf_attn_paged", self._desc, self._cache(cache), mine.refs[2], self._ws, self.ws_bytes)
         return out
 
     def join(self, parts: Sequence[torch.Tensor], lses: Sequence[torch.Tensor], out: Optional[torch.Tensor] = None,
@@ -224,7 +234,8 @@ class AttentionSession:
             out = self._new(shape, self.dtype)
         p = (ctypes.c_void_p * n)(*[self._plain(x, pdt, shape, "a part") for x in parts])
         s = (ctypes.c_void_p * n)(*[self._plain(x, torch.float32, shape[:2], "a log-sum-exp") for x in lses])
-        _JOIN.pack_into(self._join, 0, n, _CF_DT[pdt], tokens, ctypes.addressof(p), ctypes.addressof(s), *self._rows(out, tokens, self.q_heads, "out"),
+        mine = self._arguments
+        _JOIN.pack_into(mine.join, 0, n, _CF_DT[pdt], tokens, ctypes.addressof(p), ctypes.addressof(s), *self._rows(out, tokens, self.q_heads, "out"),
                         0 if lse is None else self._plain(lse, torch.float32, shape[:2], "lse"))
-        self._call(self._lib.cf_attn_join, "cf_attn_join", self._desc, self._refs[3])
+        self._call(self._lib.cf_attn_join, "cf_attn_join", self._desc, mine.refs[3])
         return out
