@@ -7,6 +7,7 @@ strided (slices of a wider projection).  Calls enqueue work on the session's str
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import struct
 import threading
@@ -96,6 +97,7 @@ class AttentionSession:
             if stream is None and self._index >= 0 and not self._unset:
                 torch.cuda.current_stream(self.device).synchronize()        # zeros on whichever stream the first call is
         self._arguments = _Arguments()
+        self._one = threading.Lock() if workspace_bytes else contextlib.nullcontext()      # a call's kernels are enqueued one after another, as they share the workspace
 
     def _on(self) -> int:
         if self._stream is not None:
@@ -199,7 +201,8 @@ class AttentionSession:
         _PROMPT.pack_into(mine.prompt, 0, n, causal, n_q, n_k, max_k, self._list(cu_q, torch.int32, n + 1, "cu_q"), self._list(cu_k, torch.int32, n + 1, "cu_k"),
                           *self._rows(q, n_q, self.q_heads, "q"), *self._rows(k, n_k, self.kv_heads, "k"), *self._rows(v, n_k, self.kv_heads, "v"),
                           *self._rows(out, n_q, self.q_heads, "out"), 0 if lse is None else self._plain(lse, torch.float32, (n_q, self.q_heads), "lse"))
-        self._call(self._lib.cf_attn_prompt, "cf_attn_prompt", self._desc, mine.refs[1], self._ws, self.ws_bytes)
+        with self._one:
+            self._call(self._lib.cf_attn_prompt, "cf_attn_prompt", self._desc, mine.refs[1], self._ws, self.ws_bytes)
         return out
 
     def paged(self, cache: PagedCache, q: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, out: Optional[torch.Tensor] = None,
@@ -217,7 +220,8 @@ class AttentionSession:
         _PAGED.pack_into(mine.paged, 0, n, cols, row if n > 1 else 0, max_len, table.data_ptr(), self._list(lens, torch.int32, n, "lens"),
                          *self._rows(q, n, self.q_heads, "q"), *self._rows(out, n, self.q_heads, "out"),
                          0 if lse is None else self._plain(lse, torch.float32, (n, self.q_heads), "lse"))
-        self._call(self._lib.cf_attn_paged, "cf_attn_paged", self._desc, self._cache(cache), mine.refs[2], self._ws, self.ws_bytes)
+        with self._one:
+            self._call(self._lib.cf_attn_paged, "cf_attn_paged", self._desc, self._cache(cache), mine.refs[2], self._ws, self.ws_bytes)
         return out
 
     def join(self, parts: Sequence[torch.Tensor], lses: Sequence[torch.Tensor], out: Optional[torch.Tensor] = None,

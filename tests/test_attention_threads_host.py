@@ -2,6 +2,7 @@
 over must not be another's to overwrite.  A stand-in for the library looks at it after others have had their turn."""
 import ctypes
 import threading
+import time
 import types
 
 import pytest
@@ -50,3 +51,31 @@ def test_arguments_are_the_callers_own(monkeypatch, name):
     for w in workers:
         w.join(60)
     assert len(seen) == threads and not wrong
+
+
+@pytest.mark.parametrize("name", ["cf_attn_prompt", "cf_attn_paged"])
+def test_calls_with_the_workspace_come_one_after_another(monkeypatch, name):
+    """A call enqueues two kernels at most, of which the second reads from the workspace what the first wrote there."""
+    inside, most = [0], [0]
+
+    def entry(*args):
+        inside[0] += 1
+        most[0] = max(most[0], inside[0])
+        time.sleep(0.05)
+        inside[0] -= 1
+        return 0
+
+    s = AttentionSession(4, 2, 64, device="cpu", workspace_bytes=1 << 20)
+    s._lib = types.SimpleNamespace(**{name: entry})
+    monkeypatch.setattr(AttentionSession, "_call", lambda self, entry, name, *args: entry(*args))
+    q, k, v = (torch.zeros(3, h, 64, dtype=torch.bfloat16) for h in (4, 2, 2))
+    cache = PagedCache.empty(3, 2, 64, page_size=16, device="cpu")
+    numbers, starts, table = torch.ones(3, dtype=torch.int32), torch.tensor([0, 3], dtype=torch.int32), torch.zeros(3, 2, dtype=torch.int32)
+    out = torch.empty_like(q)
+    call = {"cf_attn_prompt": lambda: s.prompt(q, k, v, starts, out=out), "cf_attn_paged": lambda: s.paged(cache, q, table, numbers, out=out)}[name]
+    workers = [threading.Thread(target=call) for _ in range(4)]
+    for w in workers:
+        w.start()
+    for w in workers:
+        w.join(60)
+    assert most[0] == 1
