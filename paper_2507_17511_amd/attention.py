@@ -1,6 +1,7 @@
 """Attention over exchanged keys and values: device-memory plumbing around the C entry points cf_kv_append, cf_attn_prompt,
 cf_attn_paged and cf_attn_join, for torch tensors.  Checks types, shapes and devices, allocates outputs that are not given,
-and keeps a workspace.  No arithmetic happens here.
+and keeps a workspace.  No arithmetic happens here, and nothing has a gradient: tensors that want one are refused while gradients are
+recorded.
 
 Queries, keys, values and outputs are [tokens, heads, head_dim] with the last dimension contiguous; tokens and heads may be
 strided (slices of a wider projection).  Calls enqueue work on the session's stream, or on torch's current one, and return.
@@ -30,6 +31,8 @@ for _layout, _args in ((_APPEND, cf.cf_append), (_PROMPT, cf.cf_prompt), (_PAGED
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # device index -> hipStream_t, without a Stream object
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_written = getattr(torch._C, "_increment_version", torch.autograd.graph.increment_version)     # [tensors]: autograd notices where it had kept one of them
+_NO_GRADIENT = "has no gradient: call under torch.no_grad() or torch.inference_mode(), or detach it"
 
 
 def _require(ok: bool, what: str) -> None:
@@ -47,6 +50,7 @@ class PagedCache:
         for x in (k, v):
             _require(x.numel() > 0 and x[0].is_contiguous() and (pages == 1 or x.stride(0) == k.stride(0) >= heads * page * dim),
                      "pages are dense, do not overlap, and are as far apart in k as in v")
+        _require(not ((k.requires_grad or v.requires_grad) and torch.is_grad_enabled()), f"a cache {_NO_GRADIENT}")
         self.k, self.v = k, v
         self.heads, self.page_size, self.head_dim, self.dtype, self.index = heads, page, dim, k.dtype, k.get_device()
         self.struct = cf.cf_kv_cache(k.data_ptr(), v.data_ptr(), pages, k.stride(0) if pages > 1 else 0, page)
@@ -140,6 +144,8 @@ class AttentionSession:
         if x.shape == (tokens, heads, self.head_dim) and x.dtype is self.dtype and x.get_device() == self._index:
             token, head, last = x.stride()
             if last == 1:
+                if x.requires_grad and torch.is_grad_enabled():
+                    raise ValueError(f"attention {_NO_GRADIENT} ({name})")
                 return x.data_ptr(), token, head
         raise ValueError(f"{name} is [{tokens}, {heads}, {self.head_dim}] of {self.dtype} on {self.device}, the elements of a head next to one another: "
                          f"got {tuple(x.shape)} of {x.dtype} on {x.device}, strides {x.stride()}")
@@ -152,6 +158,8 @@ class AttentionSession:
     def _plain(self, x: torch.Tensor, dtype: torch.dtype, shape, name: str) -> int:
         if x.shape != shape or x.dtype is not dtype or x.get_device() != self._index or not x.is_contiguous():
             raise ValueError(f"{name} is dense {tuple(shape)} of {dtype} on {self.device}: got {tuple(x.shape)} of {x.dtype} on {x.device}")
+        if x.requires_grad and torch.is_grad_enabled():
+            raise ValueError(f"attention {_NO_GRADIENT} ({name})")
         return x.data_ptr()
 
     def _cache(self, cache: PagedCache):
@@ -168,8 +176,11 @@ class AttentionSession:
         which may be q."""
         n = k.shape[0]
         rows_q = rows_out = (0, 0, 0)
+        written = [cache.k, cache.v]
         if q is not None:
-            if q_out is None:
+            if q_out is not None:
+                written.append(q_out)
+            else:
                 q_out = self._new(q.shape, self.dtype)
             rows_q = self._rows(q, n, self.q_heads, "q")
             rows_out = rows_q if q_out is q else self._rows(q_out, n, self.q_heads, "q_out")
@@ -186,6 +197,7 @@ class AttentionSession:
         _APPEND.pack_into(mine.append, 0, n, *self._rows(k, n, self.kv_heads, "k"), *self._rows(v, n, self.kv_heads, "v"),
                           self._list(slots, torch.int64, n, "slots"), *rows_q, *rows_out, *at, *table)
         self._call(self._lib.cf_kv_append, "cf_kv_append", self._desc, self._cache(cache), mine.refs[0])
+        _written(written)
         return q_out
 
     def prompt(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor, cu_k: Optional[torch.Tensor] = None,
@@ -195,6 +207,7 @@ class AttentionSession:
         cu_k = cu_q if cu_k is None else cu_k
         n, n_q, n_k = cu_q.shape[0] - 1, q.shape[0], k.shape[0]
         _require(n >= 0, "cu_q has an entry more than there are sequences")
+        written = [x for x in (out, lse) if x is not None]
         if out is None:
             out = self._new(q.shape, self.dtype)
         mine = self._arguments
@@ -203,6 +216,8 @@ class AttentionSession:
                           *self._rows(out, n_q, self.q_heads, "out"), 0 if lse is None else self._plain(lse, torch.float32, (n_q, self.q_heads), "lse"))
         with self._one:
             self._call(self._lib.cf_attn_prompt, "cf_attn_prompt", self._desc, mine.refs[1], self._ws, self.ws_bytes)
+        if written:
+            _written(written)
         return out
 
     def paged(self, cache: PagedCache, q: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, out: Optional[torch.Tensor] = None,
@@ -210,6 +225,7 @@ class AttentionSession:
         """Attention of one token per sequence, q [sequences, q_heads, head_dim], over its context: lens[b] tokens in the pages
         table[b] (int32 both).  max_len: the longest context, a hint."""
         n = q.shape[0]
+        written = [x for x in (out, lse) if x is not None]
         if out is None:
             out = self._new(q.shape, self.dtype)
         _require(table.dim() == 2 and table.shape[0] == n and table.dtype is torch.int32 and table.get_device() == self._index, "table is [sequences, pages] int32")
@@ -222,6 +238,8 @@ class AttentionSession:
                          0 if lse is None else self._plain(lse, torch.float32, (n, self.q_heads), "lse"))
         with self._one:
             self._call(self._lib.cf_attn_paged, "cf_attn_paged", self._desc, self._cache(cache), mine.refs[2], self._ws, self.ws_bytes)
+        if written:
+            _written(written)
         return out
 
     def join(self, parts: Sequence[torch.Tensor], lses: Sequence[torch.Tensor], out: Optional[torch.Tensor] = None,
@@ -234,6 +252,7 @@ class AttentionSession:
         _require(len(shape) == 3 and shape[1] == self.q_heads and shape[2] == self.head_dim and (pdt is self.dtype or pdt is torch.float32),
                  f"parts are [tokens, {self.q_heads}, {self.head_dim}] of {self.dtype} or torch.float32")
         tokens = shape[0]
+        written = [x for x in (out, lse) if x is not None]
         if out is None:
             out = self._new(shape, self.dtype)
         p = (ctypes.c_void_p * n)(*[self._plain(x, pdt, shape, "a part") for x in parts])
@@ -242,4 +261,6 @@ class AttentionSession:
         _JOIN.pack_into(mine.join, 0, n, _CF_DT[pdt], tokens, ctypes.addressof(p), ctypes.addressof(s), *self._rows(out, tokens, self.q_heads, "out"),
                         0 if lse is None else self._plain(lse, torch.float32, shape[:2], "lse"))
         self._call(self._lib.cf_attn_join, "cf_attn_join", self._desc, mine.refs[3])
+        if written:
+            _written(written)
         return out

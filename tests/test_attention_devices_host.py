@@ -55,6 +55,7 @@ def machine(monkeypatch):
     for module in (attention, session):
         monkeypatch.setattr(module, "_current_device", lambda: now.device, raising=False)
     monkeypatch.setattr(attention, "_raw_stream", lambda index: 0)
+    monkeypatch.setattr(attention, "_written", lambda tensors: None)
 
     def entry(*args):
         now.calls.append(now.device)
