@@ -12,6 +12,7 @@ import contextlib
 import ctypes
 import struct
 import threading
+import types
 from typing import Optional, Sequence
 
 import torch
@@ -20,8 +21,8 @@ import paper_2507_17511_amd as cf
 
 _CF_DT = {torch.bfloat16: cf.CF_BF16, torch.float16: cf.CF_F16, torch.float32: cf.CF_F32}
 
-# The arguments of a call, as one struct.pack_into writes them: filling a ctypes structure field by field takes several times as long
-# as the call itself.  A cf_rows is "Pqq".
+# The arguments of a call, as one struct.pack writes them: filling a ctypes structure field by field takes several times as long
+# as the call itself.  A cf_rows is "Pqq".  What is packed is the call's own, so that threads may call at once: the interpreter's lock is free during a call.
 _APPEND = struct.Struct("@q Pqq Pqq P Pqq Pqq PPP q ii")
 _PROMPT = struct.Struct("@ii qqq PP Pqq Pqq Pqq Pqq P")
 _PAGED = struct.Struct("@ii qq PP Pqq Pqq P")
@@ -29,7 +30,17 @@ _JOIN = struct.Struct("@ii q PP Pqq P")
 for _layout, _args in ((_APPEND, cf.cf_append), (_PROMPT, cf.cf_prompt), (_PAGED, cf.cf_paged), (_JOIN, cf.cf_join)):
     assert _layout.size == ctypes.sizeof(_args), _args
 
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # device index -> hipStream_t, without a Stream object
+
+def _entries() -> types.SimpleNamespace:
+    """The library's entry points, with packed arguments as bytes."""
+    desc, cache, args, workspace, stream = ctypes.c_void_p, ctypes.c_void_p, ctypes.c_char_p, (ctypes.c_void_p, ctypes.c_size_t), ctypes.c_void_p
+    takes = {"cf_kv_append": (desc, cache, args, stream), "cf_attn_prompt": (desc, args, *workspace, stream),
+             "cf_attn_paged": (desc, cache, args, *workspace, stream), "cf_attn_join": (desc, args, stream)}
+    return types.SimpleNamespace(**{name: ctypes.CFUNCTYPE(ctypes.c_int32, *given)((name, cf.lib())) for name, given in takes.items()})
+
+
+# device index -> hipStream_t, without a Stream object
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda index: torch.cuda.current_stream(index).cuda_stream)
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 _written = getattr(torch._C, "_increment_version", torch.autograd.graph.increment_version)     # [tensors]: autograd notices where it had kept one of them
 _NO_GRADIENT = "has no gradient: call under torch.no_grad() or torch.inference_mode(), or detach it"
@@ -63,14 +74,6 @@ class PagedCache:
         return cls(kv[0], kv[1])
 
 
-class _Arguments(threading.local):
-    """A thread's structures for the call in hand: the interpreter's lock is free while the library reads them."""
-
-    def __init__(self):
-        self.append, self.prompt, self.paged, self.join = cf.cf_append(), cf.cf_prompt(), cf.cf_paged(), cf.cf_join()
-        self.refs = [ctypes.byref(x) for x in (self.append, self.prompt, self.paged, self.join)]
-
-
 class AttentionSession:
     """The geometry of a model's attention on one device, and the workspace of its calls: one stream at a time, from any threads.  Calls go to the session's own
     stream, if it has one, or to the current one.  As with every stream but their own, tensors are kept until the work on them is done, or recorded on that stream; the workspace is."""
@@ -85,51 +88,46 @@ class AttentionSession:
             self.device = torch.device("cuda", torch.cuda.current_device())
         self._index = self.device.index if self.device.type == "cuda" else -1
         self.desc = cf.cf_attn_desc(_CF_DT[dtype], q_heads, kv_heads, head_dim, scale)
-        self._lib = cf.lib()
+        self._lib = _entries()
         self._desc = ctypes.byref(self.desc)
         self.ws_bytes = workspace_bytes
         self._stream = stream
-        # The workspace is memory of the session's stream, or else of the current one, and recorded on every other that a call goes to.
-        self._streams = {None if stream is None else stream.cuda_stream}
+        self._settled = set()       # streams on which there is nothing more to do for a call than to make it
         self.workspace = self._ws = None
         self._unset = False         # whether the workspace's zeros were captured into a graph, which is yet to run
-        if workspace_bytes:
+        if workspace_bytes:         # memory of the session's stream, or else of the current one, and recorded on those that calls go to
             with torch.cuda.device(self._index), torch.cuda.stream(stream):
                 self.workspace = torch.zeros(workspace_bytes, dtype=torch.uint8, device=self.device)
                 self._unset = self._index >= 0 and torch.cuda.is_current_stream_capturing()
             self._ws = self.workspace.data_ptr()
             if stream is None and self._index >= 0 and not self._unset:
                 torch.cuda.current_stream(self.device).synchronize()        # zeros on whichever stream the first call is
-        self._arguments = _Arguments()
         self._one = threading.Lock() if workspace_bytes else contextlib.nullcontext()      # a call's kernels are enqueued one after another, as they share the workspace
-
-    def _on(self) -> int:
-        if self._stream is not None:
-            return self._stream.cuda_stream
-        if _raw_stream is not None:
-            return _raw_stream(self._index)
-        return torch.cuda.current_stream(self.device).cuda_stream
 
     # The library launches on the device that is current, and the null stream, torch's default one, is that device's.
     def _call(self, entry, name: str, *args) -> None:
-        if self._index < 0:
-            raise ValueError(f"attention runs on a GPU: the session's device is {self.device}")
-        on = self._on()
-        if on not in self._streams:
-            if self.workspace is not None:
-                self.workspace.record_stream(torch.cuda.current_stream(self.device))
-            self._streams.add(on)
-        if self._unset:
-            with torch.cuda.device(self._index), torch.cuda.stream(self._stream):
-                self.workspace[:cf.CF_ATTN_COUNTER_BYTES].zero_()
-                self._unset = torch.cuda.is_current_stream_capturing()
-        if _current_device() != self._index:
-            with torch.cuda.device(self._index):
-                status = entry(*args, on)
-        else:
+        on = _raw_stream(self._index) if self._stream is None else self._stream.cuda_stream
+        if on in self._settled and _current_device() == self._index:
             status = entry(*args, on)
+        else:
+            status = self._call_elsewhere(entry, args, on)
         if status:
             raise cf.CFError(status, name)
+
+    # ... on a stream for the first time, or with another device current.
+    def _call_elsewhere(self, entry, args, on: int) -> int:
+        if self._index < 0:
+            raise ValueError(f"attention runs on a GPU: the session's device is {self.device}")
+        with torch.cuda.device(self._index):
+            if on not in self._settled and self._stream is None and self.workspace is not None:
+                self.workspace.record_stream(torch.cuda.current_stream(self.device))
+            if self._unset:
+                with torch.cuda.stream(self._stream):
+                    self.workspace[:cf.CF_ATTN_COUNTER_BYTES].zero_()
+                    self._unset = torch.cuda.is_current_stream_capturing()
+            if not self._unset:
+                self._settled.add(on)
+            return entry(*args, on)
 
     # An output is memory of the stream that it is written on: of another's it might still be in use there.
     def _new(self, shape, dtype: torch.dtype) -> torch.Tensor:
@@ -193,10 +191,9 @@ class AttentionSession:
             at = (self._list(positions, torch.int32, n, "positions"), self._plain(cos, torch.float32, shape, "cos"),
                   self._plain(sin, torch.float32, shape, "sin"))
             table = (shape[0], 2 * shape[1], interleaved)
-        mine = self._arguments
-        _APPEND.pack_into(mine.append, 0, n, *self._rows(k, n, self.kv_heads, "k"), *self._rows(v, n, self.kv_heads, "v"),
-                          self._list(slots, torch.int64, n, "slots"), *rows_q, *rows_out, *at, *table)
-        self._call(self._lib.cf_kv_append, "cf_kv_append", self._desc, self._cache(cache), mine.refs[0])
+        args = _APPEND.pack(n, *self._rows(k, n, self.kv_heads, "k"), *self._rows(v, n, self.kv_heads, "v"),
+                            self._list(slots, torch.int64, n, "slots"), *rows_q, *rows_out, *at, *table)
+        self._call(self._lib.cf_kv_append, "cf_kv_append", self._desc, self._cache(cache), args)
         _written(written)
         return q_out
 
@@ -204,20 +201,20 @@ class AttentionSession:
                causal: bool = True, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, max_k: int = 0) -> torch.Tensor:
         """Attention of packed sequences: sequence b has rows cu_q[b] .. cu_q[b + 1] of q and cu_k[b] .. of k and v (int32; cu_k is
         cu_q if not given).  `lse`: fp32 [tokens, q_heads], filled with the rows' log-sum-exps.  max_k: keys of the longest sequence, a hint."""
-        cu_k = cu_q if cu_k is None else cu_k
         n, n_q, n_k = cu_q.shape[0] - 1, q.shape[0], k.shape[0]
-        _require(n >= 0, "cu_q has an entry more than there are sequences")
-        written = [x for x in (out, lse) if x is not None]
+        if n < 0:
+            raise ValueError("cu_q has an entry more than there are sequences")
+        at_q = self._list(cu_q, torch.int32, n + 1, "cu_q")
+        at_k = at_q if cu_k is None or cu_k is cu_q else self._list(cu_k, torch.int32, n + 1, "cu_k")
+        given = () if out is None else (out,)
         if out is None:
             out = self._new(q.shape, self.dtype)
-        mine = self._arguments
-        _PROMPT.pack_into(mine.prompt, 0, n, causal, n_q, n_k, max_k, self._list(cu_q, torch.int32, n + 1, "cu_q"), self._list(cu_k, torch.int32, n + 1, "cu_k"),
-                          *self._rows(q, n_q, self.q_heads, "q"), *self._rows(k, n_k, self.kv_heads, "k"), *self._rows(v, n_k, self.kv_heads, "v"),
-                          *self._rows(out, n_q, self.q_heads, "out"), 0 if lse is None else self._plain(lse, torch.float32, (n_q, self.q_heads), "lse"))
+        args = _PROMPT.pack(n, causal, n_q, n_k, max_k, at_q, at_k, *self._rows(q, n_q, self.q_heads, "q"), *self._rows(k, n_k, self.kv_heads, "k"),
+                            *self._rows(v, n_k, self.kv_heads, "v"), *self._rows(out, n_q, self.q_heads, "out"), 0 if lse is None else self._plain(lse, torch.float32, (n_q, self.q_heads), "lse"))
         with self._one:
-            self._call(self._lib.cf_attn_prompt, "cf_attn_prompt", self._desc, mine.refs[1], self._ws, self.ws_bytes)
-        if written:
-            _written(written)
+            self._call(self._lib.cf_attn_prompt, "cf_attn_prompt", self._desc, args, self._ws, self.ws_bytes)
+        if given or lse is not None:
+            _written(given if lse is None else (*given, lse))
         return out
 
     def paged(self, cache: PagedCache, q: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, out: Optional[torch.Tensor] = None,
@@ -225,21 +222,21 @@ class AttentionSession:
         """Attention of one token per sequence, q [sequences, q_heads, head_dim], over its context: lens[b] tokens in the pages
         table[b] (int32 both).  max_len: the longest context, a hint."""
         n = q.shape[0]
-        written = [x for x in (out, lse) if x is not None]
+        given = () if out is None else (out,)
         if out is None:
             out = self._new(q.shape, self.dtype)
-        _require(table.dim() == 2 and table.shape[0] == n and table.dtype is torch.int32 and table.get_device() == self._index, "table is [sequences, pages] int32")
+        shape = table.shape
+        _require(len(shape) == 2 and shape[0] == n and table.dtype is torch.int32 and table.get_device() == self._index, "table is [sequences, pages] int32")
         row, entry = table.stride()
-        cols = table.shape[1]
+        cols = shape[1]
         _require((cols == 1 or entry == 1) and (n < 2 or row >= cols), "the rows of the table are dense and do not overlap")
-        mine = self._arguments
-        _PAGED.pack_into(mine.paged, 0, n, cols, row if n > 1 else 0, max_len, table.data_ptr(), self._list(lens, torch.int32, n, "lens"),
+        args = _PAGED.pack(n, cols, row if n > 1 else 0, max_len, table.data_ptr(), self._list(lens, torch.int32, n, "lens"),
                          *self._rows(q, n, self.q_heads, "q"), *self._rows(out, n, self.q_heads, "out"),
                          0 if lse is None else self._plain(lse, torch.float32, (n, self.q_heads), "lse"))
         with self._one:
-            self._call(self._lib.cf_attn_paged, "cf_attn_paged", self._desc, self._cache(cache), mine.refs[2], self._ws, self.ws_bytes)
-        if written:
-            _written(written)
+            self._call(self._lib.cf_attn_paged, "cf_attn_paged", self._desc, self._cache(cache), args, self._ws, self.ws_bytes)
+        if given or lse is not None:
+            _written(given if lse is None else (*given, lse))
         return out
 
     def join(self, parts: Sequence[torch.Tensor], lses: Sequence[torch.Tensor], out: Optional[torch.Tensor] = None,
@@ -249,18 +246,17 @@ class AttentionSession:
         n = len(parts)
         _require(n > 0 and n == len(lses), "a log-sum-exp for every part, and one part at least")
         shape, pdt = parts[0].shape, parts[0].dtype
-        _require(len(shape) == 3 and shape[1] == self.q_heads and shape[2] == self.head_dim and (pdt is self.dtype or pdt is torch.float32),
-                 f"parts are [tokens, {self.q_heads}, {self.head_dim}] of {self.dtype} or torch.float32")
+        if len(shape) != 3 or shape[1] != self.q_heads or shape[2] != self.head_dim or (pdt is not self.dtype and pdt is not torch.float32):
+            raise ValueError(f"parts are [tokens, {self.q_heads}, {self.head_dim}] of {self.dtype} or torch.float32")
         tokens = shape[0]
-        written = [x for x in (out, lse) if x is not None]
+        given = () if out is None else (out,)
         if out is None:
             out = self._new(shape, self.dtype)
         p = (ctypes.c_void_p * n)(*[self._plain(x, pdt, shape, "a part") for x in parts])
         s = (ctypes.c_void_p * n)(*[self._plain(x, torch.float32, shape[:2], "a log-sum-exp") for x in lses])
-        mine = self._arguments
-        _JOIN.pack_into(mine.join, 0, n, _CF_DT[pdt], tokens, ctypes.addressof(p), ctypes.addressof(s), *self._rows(out, tokens, self.q_heads, "out"),
+        args = _JOIN.pack(n, _CF_DT[pdt], tokens, ctypes.addressof(p), ctypes.addressof(s), *self._rows(out, tokens, self.q_heads, "out"),
                         0 if lse is None else self._plain(lse, torch.float32, shape[:2], "lse"))
-        self._call(self._lib.cf_attn_join, "cf_attn_join", self._desc, mine.refs[3])
-        if written:
-            _written(written)
+        self._call(self._lib.cf_attn_join, "cf_attn_join", self._desc, args)
+        if given or lse is not None:
+            _written(given if lse is None else (*given, lse))
         return out
