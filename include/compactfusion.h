@@ -329,7 +329,7 @@ const char *cf_profile_kernel_name(const cf_ctx *ctx, int32_t k);
  * These calls have no context and keep nothing between calls.  They follow the rules above: device pointers of the
  * caller's, work enqueued on `stream`, a stream of the device that is current at the call (as the codec's calls: null is that
  * device's), without synchronising, arguments validated on the host before anything is
- * enqueued, nothing allocated, nothing thrown.  They may be captured into a HIP graph.  Calls that share a workspace
+ * enqueued, nothing allocated, nothing thrown.  A call that would take more work-items than one launch counts, 2^32 - 1, is refused (CF_ERR_SHAPE).  They may be captured into a HIP graph.  Calls that share a workspace
  * must not overlap in time; calls that do not may run from any threads and on any streams.
  *
  * Numbers held on the device cannot be refused.  Whatever they are, no call reads or writes outside the buffers it
@@ -366,7 +366,7 @@ typedef struct {
 typedef struct {
     void *k, *v;         /* 16-byte aligned; they must not overlap, except that pages of one may lie between pages of the other */
     int64_t n_pages;     /* 1 .. 2^31 - 1 */
-    int64_t page_stride; /* elements from page to page, a multiple of 8; 0 = kv_heads * page_size * head_dim (dense), less is refused */
+    int64_t page_stride; /* elements from page to page, a multiple of 8; 0 = kv_heads * page_size * head_dim (dense), less is refused, and so is more than 2^60 bytes of pages */
     int32_t page_size;   /* tokens of a page: a power of two, 16 .. 32768 */
 } cf_kv_cache;
 

@@ -88,6 +88,35 @@ struct AppendArgs {
     int32_t n_positions, rotary_dim, interleaved;
 };
 
+// Workgroups of 256 threads that a call launches.  A launch counts its work-items with 32 bits.
+constexpr int64_t kMostWorkgroups = (((int64_t)1 << 32) - 1) / 256;
+
+inline int64_t prompt_tiles(const PromptArgs &a) { return ((int64_t)a.n_q * a.h.group + kPromptRows - 1) / kPromptRows + a.n_seqs; }      // at most: a part of one for every sequence
+inline int64_t prompt_workgroups(const PromptArgs &a) { return prompt_tiles(a) * a.h.kv_heads * a.n_splits; }
+
+inline int64_t paged_units(const PagedArgs &a) { return a.n_seqs * (int64_t)a.h.kv_heads * ((a.h.group + kPagedHeads - 1) / kPagedHeads); }
+inline int64_t paged_workgroups(const PagedArgs &a)
+{
+    const int64_t items = paged_units(a) * a.n_splits, held = 256 * (a.h.head_dim == 64 ? 4 : a.h.head_dim == 128 ? 3 : 2);
+    return a.many && held < items ? held : items;
+}
+
+// Lanes that share 8 elements of a row.  Up to 8 parts a lane each alone: lanes that meet cost a row more than loads in a row do (us: 12 parts of 98304 rows of 128 bf16,
+// spread over 4 / 16 lanes 76 / 141; 6 of 10656 rows of 256 floats, over 1 / 8 lanes 12.7 / 24.8).  Past that a lane's loads are too many (48 parts, over 4 / 16 lanes
+// 118 / 76), and many parts are of few rows: the lanes of a whole workgroup fill the device.
+constexpr int join_spread(int n_parts, int dim) { return n_parts <= 8 ? 1 : n_parts <= 16 ? 4 : 256 / (dim / 8); }
+inline int64_t join_workgroups(const JoinArgs &a)
+{
+    const int rows = 256 / (a.h.head_dim / 8 * join_spread(a.n_parts, a.h.head_dim));
+    return (a.n_rows + rows - 1) / rows;
+}
+
+inline int64_t append_workgroups(const AppendArgs &a)
+{
+    const int64_t rows = (a.q.data ? a.h.q_heads : 0) + 2 * (int64_t)a.h.kv_heads;
+    return (a.n_tokens * rows * (a.h.head_dim / 16) + 255) / 256;
+}
+
 hipError_t launch_prompt(const PromptArgs &a, hipStream_t s);
 hipError_t launch_paged(const PagedArgs &a, hipStream_t s);
 hipError_t launch_join(const JoinArgs &a, hipStream_t s);

@@ -12,7 +12,7 @@ namespace {
 
 constexpr int64_t kMostStride = (int64_t)1 << 24;       // elements: a tile's rows are addressed with 32 bits
 constexpr int64_t kMostRows = (int64_t)1 << 30;
-constexpr int64_t kMostGrid = ((int64_t)1 << 31) - 1;
+constexpr int64_t kMostCache = (int64_t)1 << 60;        // bytes from a cache's first page to its last
 constexpr int64_t kCUs = 256;
 constexpr int64_t kCounters = CF_ATTN_COUNTER_BYTES / sizeof(uint32_t);
 
@@ -57,10 +57,9 @@ bool meet(const Span &a, const Span &b)
 cf_status check_rows(const cf_rows &in, int64_t tokens, int64_t heads, int64_t dim, bool output, int64_t least, Rows &out, Span &span)
 {
     int64_t token = in.token, head = in.head;
-    if (heads == 1) head = dim;             // strides that no element goes by
-    if (tokens == 1) token = heads == 1 ? dim : (heads - 1) * head + dim;
-    if (tokens == 1 && head >= 0 && token > kMostStride) token = dim;
     if (!in.data || !aligned(in.data, 16)) return CF_ERR_INVALID_ARG;
+    if (heads == 1) head = dim;             // strides that no element goes by
+    if (tokens == 1) token = dim;
     if (token < 0 || head < 0 || token % 8 != 0 || head % 8 != 0 || token >= kMostStride || head >= kMostStride) return CF_ERR_SHAPE;
     if (tokens > 1 && token < least) return CF_ERR_SHAPE;
     if (output) {
@@ -83,7 +82,7 @@ cf_status check_cache(const cf_kv_cache *c, const Heads &h, Cache &out, Span &k,
     if (c->n_pages < 1 || c->n_pages > INT32_MAX) return CF_ERR_SHAPE;
     const int64_t dense = (int64_t)h.kv_heads * c->page_size * h.head_dim;
     const int64_t stride = c->page_stride ? c->page_stride : dense;
-    if (stride < dense || stride % 8 != 0 || stride > ((int64_t)1 << 40)) return CF_ERR_SHAPE;
+    if (stride < dense || stride % 8 != 0 || stride > ((int64_t)1 << 40) || c->n_pages > kMostCache / 2 / stride) return CF_ERR_SHAPE;
     out.k = static_cast<char *>(c->k);
     out.v = static_cast<char *>(c->v);
     out.page_bytes = stride * 2;
@@ -208,8 +207,7 @@ cf_status cf_kv_append(const cf_attn_desc *desc, const cf_kv_cache *cache, const
     a.n_tokens = n;
     a.rotary_dim = args->rotary_dim;
     a.interleaved = args->interleaved ? 1 : 0;
-    const int64_t rows = (a.q.data ? a.h.q_heads : 0) + 2 * (int64_t)a.h.kv_heads;
-    if (n * rows > kMostGrid) return CF_ERR_SHAPE;
+    if (append_workgroups(a) > kMostWorkgroups) return CF_ERR_SHAPE;
     return status_of(launch_append(a, static_cast<hipStream_t>(stream)));
 }
 
@@ -242,7 +240,6 @@ cf_status cf_attn_prompt(const cf_attn_desc *desc, const cf_prompt *args, void *
     a.causal = args->causal ? 1 : 0;
 
     const int64_t longest = args->max_k > 0 && args->max_k < args->n_k ? args->max_k : args->n_k;
-    const int64_t tiles = (args->n_q * a.h.group + kPromptRows - 1) / kPromptRows + args->n_seqs;
     const int64_t rows = args->n_q * a.h.q_heads;
     const int64_t busy = (args->n_q * a.h.group + kPromptRows - 1) / kPromptRows * a.h.kv_heads;
     int64_t most = parts_that_fit(workspace_bytes, rows, a.h.head_dim);
@@ -250,12 +247,13 @@ cf_status cf_attn_prompt(const cf_attn_desc *desc, const cf_prompt *args, void *
     if (most > kMaxParts) most = kMaxParts;
     a.n_splits = 1;
     a.split_keys = (int32_t)kMostRows;
+    if (prompt_workgroups(a) > kMostWorkgroups) return CF_ERR_SHAPE;
+    if (most > kMostWorkgroups / prompt_workgroups(a)) most = kMostWorkgroups / prompt_workgroups(a);
     const int64_t splits = prompt_splits(busy, longest, rows, a.h.head_dim, most);
     if (splits > 1) {
         a.split_keys = (int32_t)round_up((longest + splits - 1) / splits, 64);
         a.n_splits = (int32_t)((longest + a.split_keys - 1) / a.split_keys);
     }
-    if (tiles * a.h.kv_heads * a.n_splits > kMostGrid) return CF_ERR_SHAPE;
     if (a.n_splits > 1) place_parts(a.parts, workspace, rows, a.n_splits, a.h.head_dim);
     const hipStream_t s = static_cast<hipStream_t>(stream);
     hipError_t e = launch_prompt(a, s);
@@ -295,7 +293,8 @@ cf_status cf_attn_paged(const cf_attn_desc *desc, const cf_kv_cache *cache, cons
     const int64_t capacity = (int64_t)args->max_pages * a.cache.page_size;
     int64_t longest = args->max_len > 0 && args->max_len < capacity ? args->max_len : capacity;
     if (longest > kMostRows) longest = kMostRows;
-    const int64_t units = args->n_seqs * (int64_t)a.h.kv_heads * ((a.h.group + kPagedHeads - 1) / kPagedHeads);
+    const int64_t units = paged_units(a);
+    if (units > kMostWorkgroups) return CF_ERR_SHAPE;
     const int64_t rows = (int64_t)args->n_seqs * a.h.q_heads;
     // Two workgroups a CU, of 128 to 1024 keys each, and 32 parts at most where that gives every CU one: a part costs its join about 0.1 us, 128
     // keys a workgroup 1.2 us.  us, on one card: 1 x 901 keys, 2 heads of keys: parts of 128 / 256 / 512 keys 8.2 / 9.6 / 11.4; 1 x 8192, 8 heads: 128 / 256
@@ -316,7 +315,6 @@ cf_status cf_attn_paged(const cf_attn_desc *desc, const cf_kv_cache *cache, cons
         a.split_keys = (int32_t)round_up((longest + splits - 1) / splits, 128);
         a.n_splits = (int32_t)((longest + a.split_keys - 1) / a.split_keys);
     }
-    if (units * a.n_splits > kMostGrid) return CF_ERR_SHAPE;
     if (a.n_splits > 1) place_parts(a.parts, workspace, rows, a.n_splits, a.h.head_dim);
     a.counters = static_cast<uint32_t *>(workspace);
     // Listed parts where there are more than the device holds, and where contexts that may differ could fill 128 MB: a workgroup for every part that there may
@@ -358,6 +356,7 @@ cf_status cf_attn_join(const cf_attn_desc *desc, const cf_join *args, void *stre
     a.lse = args->lse;
     a.n_parts = args->n_parts;
     a.part_dtype = args->part_dtype;
+    if (join_workgroups(a) > kMostWorkgroups) return CF_ERR_SHAPE;
     return status_of(launch_join(a, static_cast<hipStream_t>(stream)));
 }
 

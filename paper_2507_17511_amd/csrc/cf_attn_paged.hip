@@ -366,9 +366,9 @@ template <int DT, int D, bool MANY> __global__ __launch_bounds__(kWaves * 64, D 
 
 template <int DT, int D> hipError_t paged_dim(const PagedArgs &a, hipStream_t s)
 {
-    const int64_t items = (int64_t)a.n_seqs * a.n_splits * a.h.kv_heads * ((a.h.group + kPagedHeads - 1) / kPagedHeads);
-    if (a.many) hipLaunchKernelGGL((k_attn_paged<DT, D, true>), dim3((unsigned)min(items, (int64_t)256 * (D == 64 ? 4 : D == 128 ? 3 : 2))), dim3(kWaves * 64), 0, s, a);
-    else hipLaunchKernelGGL((k_attn_paged<DT, D, false>), dim3((unsigned)items), dim3(kWaves * 64), 0, s, a);
+    const dim3 grid((unsigned)paged_workgroups(a));
+    if (a.many) hipLaunchKernelGGL((k_attn_paged<DT, D, true>), grid, dim3(kWaves * 64), 0, s, a);
+    else hipLaunchKernelGGL((k_attn_paged<DT, D, false>), grid, dim3(kWaves * 64), 0, s, a);
     return hipGetLastError();
 }
 

@@ -469,8 +469,7 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 :
 
 template <int DT, int D> hipError_t prompt_dim(const PromptArgs &a, hipStream_t s)
 {
-    const int64_t tiles = ((int64_t)a.n_q * a.h.group + kPromptRows - 1) / kPromptRows + a.n_seqs;      // at most: a part of one for every sequence
-    hipLaunchKernelGGL((k_attn_prompt<DT, D>), dim3((unsigned)(tiles * a.h.kv_heads * a.n_splits)), dim3(kWaves * 64), 0, s, a);
+    hipLaunchKernelGGL((k_attn_prompt<DT, D>), dim3((unsigned)prompt_workgroups(a)), dim3(kWaves * 64), 0, s, a);
     return hipGetLastError();
 }
 

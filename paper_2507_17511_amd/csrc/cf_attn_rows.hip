@@ -160,24 +160,20 @@ template <int DT, int PT, int D, int SPREAD, int EACH> __global__ __launch_bound
     if (a.lse && lane == 0) gmut<float>(a.lse)[row] = total > 0.0f || total != total ? base + __log2f(total) * kLn2 : -__builtin_inff();
 }
 
-template <int DT, int PT, int D, int SPREAD, int EACH> hipError_t join_spread(const JoinArgs &a, hipStream_t s)
+template <int DT, int PT, int D, int SPREAD, int EACH> hipError_t join_over(const JoinArgs &a, hipStream_t s)
 {
-    constexpr int kRows = 256 / (D / 8 * SPREAD);
-    hipLaunchKernelGGL((k_attn_join<DT, PT, D, SPREAD, EACH>), dim3((unsigned)((a.n_rows + kRows - 1) / kRows)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((k_attn_join<DT, PT, D, SPREAD, EACH>), dim3((unsigned)join_workgroups(a)), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
-// Up to 8 parts a lane each alone: lanes that meet cost a row more than loads in a row do (us: 12 parts of 98304 rows of 128 bf16, spread over 4 / 16
-// lanes 76 / 141; 6 of 10656 rows of 256 floats, over 1 / 8 lanes 12.7 / 24.8).  Past that a lane's loads are too many (48 parts, over 4 / 16 lanes
-// 118 / 76), and many parts are of few rows: the lanes of a whole workgroup fill the device.
 template <int DT, int PT, int D> hipError_t join_dim(const JoinArgs &a, hipStream_t s)
 {
-    constexpr int kMost = 256 / (D / 8);
-    if (a.n_parts <= 4) return join_spread<DT, PT, D, 1, 4>(a, s);
-    if (a.n_parts <= 8) return join_spread<DT, PT, D, 1, 8>(a, s);
-    if (a.n_parts <= 16) return join_spread<DT, PT, D, 4, 4>(a, s);
-    static_assert(kMost * (64 / kMost) == kMaxParts, "the lanes have all parts");
-    return join_spread<DT, PT, D, kMost, 64 / kMost>(a, s);
+    constexpr int kMost = join_spread(kMaxParts, D);
+    static_assert(join_spread(8, D) == 1 && join_spread(16, D) == 4 && kMost * (kMaxParts / kMost) == kMaxParts, "the lanes have all parts");
+    if (a.n_parts <= 4) return join_over<DT, PT, D, 1, 4>(a, s);
+    if (a.n_parts <= 8) return join_over<DT, PT, D, 1, 8>(a, s);
+    if (a.n_parts <= 16) return join_over<DT, PT, D, 4, 4>(a, s);
+    return join_over<DT, PT, D, kMost, kMaxParts / kMost>(a, s);
 }
 
 template <int DT, int PT> hipError_t join_typed(const JoinArgs &a, hipStream_t s)
@@ -191,8 +187,7 @@ template <int DT, int PT> hipError_t join_typed(const JoinArgs &a, hipStream_t s
 
 template <int DT> hipError_t append_typed(const AppendArgs &a, hipStream_t s)
 {
-    const int64_t rows = (a.q.data ? a.h.q_heads : 0) + 2 * a.h.kv_heads;
-    const unsigned grid = (unsigned)((a.n_tokens * rows * (a.h.head_dim / 16) + 255) / 256);
+    const unsigned grid = (unsigned)append_workgroups(a);
     switch (a.h.head_dim) {
     case 64: hipLaunchKernelGGL((k_kv_append<DT, 64>), dim3(grid), dim3(256), 0, s, a); break;
     case 128: hipLaunchKernelGGL((k_kv_append<DT, 128>), dim3(grid), dim3(256), 0, s, a); break;
