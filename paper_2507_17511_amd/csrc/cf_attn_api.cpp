@@ -12,7 +12,7 @@ namespace {
 
 constexpr int64_t kMostStride = (int64_t)1 << 24;       // elements: a tile's rows are addressed with 32 bits
 constexpr int64_t kMostRows = (int64_t)1 << 30;
-constexpr int64_t kMostCache = (int64_t)1 << 60;        // bytes from a cache's first page to its last
+constexpr int64_t kMostSpan = (int64_t)1 << 60;         // bytes that a cache or a table spans
 constexpr int64_t kCUs = 256;
 constexpr int64_t kCounters = CF_ATTN_COUNTER_BYTES / sizeof(uint32_t);
 
@@ -82,7 +82,7 @@ cf_status check_cache(const cf_kv_cache *c, const Heads &h, Cache &out, Span &k,
     if (c->n_pages < 1 || c->n_pages > INT32_MAX) return CF_ERR_SHAPE;
     const int64_t dense = (int64_t)h.kv_heads * c->page_size * h.head_dim;
     const int64_t stride = c->page_stride ? c->page_stride : dense;
-    if (stride < dense || stride % 8 != 0 || stride > ((int64_t)1 << 40) || c->n_pages > kMostCache / 2 / stride) return CF_ERR_SHAPE;
+    if (stride < dense || stride % 8 != 0 || stride > ((int64_t)1 << 40) || c->n_pages > kMostSpan / 2 / stride) return CF_ERR_SHAPE;
     out.k = static_cast<char *>(c->k);
     out.v = static_cast<char *>(c->v);
     out.page_bytes = stride * 2;
@@ -167,6 +167,48 @@ int64_t prompt_splits(int64_t busy, int64_t longest, int64_t rows, int dim, int6
         }
     }
     return best;
+}
+
+constexpr int64_t kMostPartKeys = 1024, kMostPartKeysOfMany = 4096, kLongOfMany = 16384;
+
+// One launch, and another one that joins parts of more than the device holds at a time.
+hipError_t paged_at_once(PagedArgs &a, int64_t longest, int64_t most_keys, void *workspace, size_t workspace_bytes, hipStream_t s)
+{
+    const int64_t units = paged_units(a);
+    const int64_t rows = (int64_t)a.n_seqs * a.h.q_heads;
+    // Two workgroups a CU, of 128 to 1024 keys each, and 32 parts at most where that gives every CU one: a part costs its join about 0.1 us, 128
+    // keys a workgroup 1.2 us.  us, on one card: 1 x 901 keys, 2 heads of keys: parts of 128 / 256 / 512 keys 8.2 / 9.6 / 11.4; 1 x 8192, 8 heads: 128 / 256
+    // / 512 16.7 / 13.0 / 13.6; 8 x 8192, 8 heads: two / three / six workgroups a CU 45 / 49 / 53; 64 x 7 to 700: 14.5 / 18.1 / 16.1.  Parts of 512 / 1024 /
+    // 2048 keys, 8 heads of 128: 96 x 160 to 16000 275 / 273 / 271, 96 x 3540 264 / 251 / 243; of 256: 48 x 160 to 16000 282 / 279 / 300; of 64: 200 x 50
+    // to 5000 93 / 95 / 102; one of 128: 150 x 90 to 9000 33 / 35 / 57.
+    int64_t keys = round_up((longest * units + 2 * kCUs - 1) / (2 * kCUs), 128);
+    if (units * 32 >= kCUs && keys < longest / 32) keys = round_up(longest / 32, 128);
+    if (keys > most_keys) keys = most_keys;
+    int64_t splits = (longest + keys - 1) / keys;
+    const int64_t fit = parts_that_fit(workspace_bytes, rows, a.h.head_dim);
+    if (splits > fit) splits = fit;
+    if (splits > kMaxParts) splits = kMaxParts;
+    if (a.n_seqs > kMostListed || units > kCounters) splits = 1;        // no places for more in the kernel's list, or for more counters
+    a.n_splits = 1;
+    a.split_keys = (int32_t)kMostRows;
+    if (splits > 1) {
+        a.split_keys = (int32_t)round_up((longest + splits - 1) / splits, 128);
+        a.n_splits = (int32_t)((longest + a.split_keys - 1) / a.split_keys);
+    }
+    if (a.n_splits > 1) place_parts(a.parts, workspace, rows, a.n_splits, a.h.head_dim);
+    a.counters = static_cast<uint32_t *>(workspace);
+    // Listed parts where there are more than the device holds, and where contexts that may differ could fill 128 MB: a workgroup for every part that there may
+    // be leaves those of the long contexts on a few XCDs.  us, one for each / listed: 8 x 270 to 27465 keys, 4 heads of 256, 85 / 39; 4 x 1270 to 126712, 4 of
+    // 128, 126 / 89; 16 x 40 to 4000, 8 of 128, 26 / 19, but 16 x 4000 43.1 / 44.2, 8 x 8192 43.6 / 45.8, 3 x 120 to 12000, 8 of 64, 11.6 / 12.8.
+    a.many = a.n_splits > 1 && (units * a.n_splits > 4 * kCUs || (a.n_seqs > 1 && units * longest * a.h.head_dim * 4 >= (int64_t)128 << 20));
+    hipError_t e = launch_paged(a, s);
+    if (e == hipSuccess && a.many) {
+        JoinArgs j = parts_to_join(a.h, a.parts, a.n_splits, a.out, a.lse);
+        j.lens = a.lens;
+        j.split_keys = a.split_keys;
+        e = launch_join(j, s);
+    }
+    return e;
 }
 
 }  // namespace
@@ -279,6 +321,7 @@ cf_status cf_attn_paged(const cf_attn_desc *desc, const cf_kv_cache *cache, cons
     const int64_t stride = args->table_stride ? args->table_stride : args->max_pages;
     if (args->n_seqs < 0 || args->max_pages < 1 || stride < args->max_pages || stride > ((int64_t)1 << 40) || args->max_len < 0 || args->n_seqs > kMostRows / desc->q_heads) return CF_ERR_SHAPE;
     if (args->n_seqs == 0) return CF_OK;
+    if (stride > kMostSpan / (int64_t)sizeof(int32_t) / args->n_seqs) return CF_ERR_SHAPE;
     if ((st = check_rows(args->q, args->n_seqs, desc->q_heads, desc->head_dim, false, 0, a.q, sq)) != CF_OK) return st;
     if ((st = check_rows(args->out, args->n_seqs, desc->q_heads, desc->head_dim, true, 0, a.out, so)) != CF_OK) return st;
     if (meet(so, sq) || meet(so, ck) || meet(so, cv)) return CF_ERR_INVALID_ARG;
@@ -293,41 +336,25 @@ cf_status cf_attn_paged(const cf_attn_desc *desc, const cf_kv_cache *cache, cons
     const int64_t capacity = (int64_t)args->max_pages * a.cache.page_size;
     int64_t longest = args->max_len > 0 && args->max_len < capacity ? args->max_len : capacity;
     if (longest > kMostRows) longest = kMostRows;
-    const int64_t units = paged_units(a);
-    if (units > kMostWorkgroups) return CF_ERR_SHAPE;
-    const int64_t rows = (int64_t)args->n_seqs * a.h.q_heads;
-    // Two workgroups a CU, of 128 to 1024 keys each, and 32 parts at most where that gives every CU one: a part costs its join about 0.1 us, 128
-    // keys a workgroup 1.2 us.  us, on one card: 1 x 901 keys, 2 heads of keys: parts of 128 / 256 / 512 keys 8.2 / 9.6 / 11.4; 1 x 8192, 8 heads: 128 / 256
-    // / 512 16.7 / 13.0 / 13.6; 8 x 8192, 8 heads: two / three / six workgroups a CU 45 / 49 / 53; 64 x 7 to 700: 14.5 / 18.1 / 16.1.  Parts of 512 / 1024 /
-    // 2048 keys, 8 heads of 128: 96 x 160 to 16000 275 / 273 / 271, 96 x 3540 264 / 251 / 243; of 256: 48 x 160 to 16000 282 / 279 / 300; of 64: 200 x 50
-    // to 5000 93 / 95 / 102; one of 128: 150 x 90 to 9000 33 / 35 / 57.
-    int64_t keys = round_up((longest * units + 2 * kCUs - 1) / (2 * kCUs), 128);
-    if (units * 32 >= kCUs && keys < longest / 32) keys = round_up(longest / 32, 128);
-    if (keys > 1024) keys = 1024;
-    int64_t splits = (longest + keys - 1) / keys;
-    const int64_t fit = parts_that_fit(workspace_bytes, rows, a.h.head_dim);
-    if (splits > fit) splits = fit;
-    if (units > kCounters || args->n_seqs > kMostListed) splits = 1;
-    if (splits > kMaxParts) splits = kMaxParts;
-    a.n_splits = 1;
-    a.split_keys = (int32_t)kMostRows;
-    if (splits > 1) {
-        a.split_keys = (int32_t)round_up((longest + splits - 1) / splits, 128);
-        a.n_splits = (int32_t)((longest + a.split_keys - 1) / a.split_keys);
-    }
-    if (a.n_splits > 1) place_parts(a.parts, workspace, rows, a.n_splits, a.h.head_dim);
-    a.counters = static_cast<uint32_t *>(workspace);
-    // Listed parts where there are more than the device holds, and where contexts that may differ could fill 128 MB: a workgroup for every part that there may
-    // be leaves those of the long contexts on a few XCDs.  us, one for each / listed: 8 x 270 to 27465 keys, 4 heads of 256, 85 / 39; 4 x 1270 to 126712, 4 of
-    // 128, 126 / 89; 16 x 40 to 4000, 8 of 128, 26 / 19, but 16 x 4000 43.1 / 44.2, 8 x 8192 43.6 / 45.8, 3 x 120 to 12000, 8 of 64, 11.6 / 12.8.
-    a.many = a.n_splits > 1 && (units * a.n_splits > 4 * kCUs || (a.n_seqs > 1 && units * longest * a.h.head_dim * 4 >= (int64_t)128 << 20));
-    const hipStream_t s = static_cast<hipStream_t>(stream);
-    hipError_t e = launch_paged(a, s);
-    if (e == hipSuccess && a.many) {
-        JoinArgs j = parts_to_join(a.h, a.parts, a.n_splits, a.out, a.lse);
-        j.lens = a.lens;
-        j.split_keys = a.split_keys;
-        e = launch_join(j, s);
+    // Of many sequences some at a time: as many as a launch has workgroups for, or, where their contexts are split, as a workgroup lists.  us, a workgroup for each of 2100
+    // contexts, 8 heads over one of 128 / parts of 4096 keys: up to 32768 keys, ragged 1410 / 1278, all as long 5035 / 4930, one long one among 1 to 500 keys 335 /
+    // 125; up to 16384 694 / 725, 2518 / 2525, 179 / 120; 32 over 8 heads of 64, 4096 keys each (up to 32768, it was said) 2710 / 2775.  Parts of 1024 keys: up to 16384 668 / 641,
+    // 2522 / 2707, up to 4096 182 / 226, 638 / 706.
+    const int64_t units = paged_units(a) / a.n_seqs, listed = kCounters / units < kMostListed ? kCounters / units : kMostListed;
+    const bool many = a.n_seqs > listed;
+    int64_t most = many ? kMostWorkgroups / units : a.n_seqs;
+    if (many && longest > kLongOfMany && parts_that_fit(workspace_bytes, listed * a.h.q_heads, a.h.head_dim) > 1) most = listed;
+    most = (a.n_seqs + (a.n_seqs + most - 1) / most - 1) / ((a.n_seqs + most - 1) / most);
+    hipError_t e = hipSuccess;
+    for (int64_t first = 0; e == hipSuccess && first < args->n_seqs; first += most) {
+        PagedArgs some = a;
+        some.n_seqs = (int32_t)(args->n_seqs - first < most ? args->n_seqs - first : most);
+        some.q.data += first * a.q.token;
+        some.out.data += first * a.out.token;
+        if (a.lse) some.lse += first * a.h.q_heads;
+        some.table += first * a.table_stride;
+        some.lens += first;
+        e = paged_at_once(some, longest, many ? kMostPartKeysOfMany : kMostPartKeys, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
     }
     return status_of(e);
 }

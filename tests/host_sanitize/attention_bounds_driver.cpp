@@ -10,6 +10,9 @@
 
 namespace {
 int g_failures, g_launches, g_shape;
+int64_t g_sequences;            // that the last paged call's launches took, one after another
+const int32_t *g_first_len;
+int g_least_splits;
 
 void expect(bool ok, const char *what, int line)
 {
@@ -27,7 +30,15 @@ static hipError_t check_grid(int64_t workgroups)
     return hipSuccess;
 }
 hipError_t launch_prompt(const PromptArgs &a, hipStream_t) { return check_grid(prompt_workgroups(a)); }
-hipError_t launch_paged(const PagedArgs &a, hipStream_t) { return check_grid(paged_workgroups(a)); }
+hipError_t launch_paged(const PagedArgs &a, hipStream_t)
+{
+    if (g_sequences == 0) g_first_len = a.lens, g_least_splits = a.n_splits;
+    EXPECT(a.lens == g_first_len + g_sequences);
+    EXPECT(a.n_splits == 1 || (a.n_seqs <= kMostListed && paged_units(a) * (int64_t)sizeof(uint32_t) <= (int64_t)CF_ATTN_COUNTER_BYTES));      // what the device has places for
+    g_sequences += a.n_seqs;
+    if (a.n_splits < g_least_splits) g_least_splits = a.n_splits;
+    return check_grid(paged_workgroups(a));
+}
 hipError_t launch_join(const JoinArgs &a, hipStream_t) { return check_grid(join_workgroups(a)); }
 hipError_t launch_append(const AppendArgs &a, hipStream_t) { return check_grid(append_workgroups(a)); }
 }  // namespace attn
@@ -65,7 +76,9 @@ int main()
             st = cf_attn_prompt(&d, &p, ws, ws ? CF_ATTN_WORKSPACE_BYTES : 0, nullptr);
         } else if (i % 4 == 1) {
             cf_paged p = {(int32_t)any(1 << 30), 1 + (int32_t)any(INT32_MAX - 1), up_to(1) ? wide() : 0, any(INT64_MAX), (int32_t *)f, (int32_t *)f, rows(8, false), rows(9, true), nullptr};
+            g_sequences = 0;
             st = cf_attn_paged(&d, &c, &p, ws, ws ? CF_ATTN_WORKSPACE_BYTES : 0, nullptr);
+            EXPECT(g_sequences == (st == CF_OK ? p.n_seqs : 0));
         } else if (i % 4 == 2) {
             cf_append p;
             std::memset(&p, 0, sizeof p);
@@ -91,6 +104,19 @@ int main()
     const cf_kv_cache c = {reinterpret_cast<void *>(at), reinterpret_cast<void *>(at + ((uintptr_t)1 << 41)), (int64_t)1 << 30, (int64_t)1 << 40, 16};
     cf_paged p = {1, 1, 0, 0, (int32_t *)f, (int32_t *)f, {f, 64, 64}, {f + 64, 64, 64}, nullptr};
     EXPECT(cf_attn_paged(&d, &c, &p, nullptr, 0, nullptr) == CF_ERR_SHAPE);
+
+    // More sequences than a workgroup lists are split as fewer are, whatever their number; without a workspace they stay whole, in one launch.
+    const cf_attn_desc g = {CF_BF16, 8, 1, 128, 0.0f};
+    const cf_kv_cache k = {reinterpret_cast<void *>(at), reinterpret_cast<void *>(at + ((uintptr_t)1 << 41)), 100000, 0, 16};
+    for (int i = 0; i < 5 * 16; ++i) {
+        const int n = i % 5 == 0 ? 2048 : i % 5 == 1 ? 2049 : i % 5 == 2 ? 2100 : i % 5 == 3 ? 4096 : 30000, pages = 1 << (i / 5);
+        cf_paged q = {n, pages, 0, 0, (int32_t *)f, (int32_t *)f, {(void *)((uintptr_t)1 << 50), 1024, 128}, {(void *)((uintptr_t)1 << 51), 1024, 128}, nullptr};
+        g_sequences = 0;
+        EXPECT(cf_attn_paged(&g, &k, &q, reinterpret_cast<void *>((uintptr_t)1 << 40), CF_ATTN_WORKSPACE_BYTES, nullptr) == CF_OK && g_sequences == n && (g_least_splits > 3 || pages < 2048));
+        const int before = g_launches;
+        g_sequences = 0;
+        EXPECT(cf_attn_paged(&g, &k, &q, nullptr, 0, nullptr) == CF_OK && g_sequences == n && g_launches == before + 1);
+    }
     if (g_failures) return 1;
     std::printf("all calls hold\n");
     return 0;
