@@ -35,20 +35,23 @@ cf_status check_desc(const cf_attn_desc *d, Heads &h)
     return CF_OK;
 }
 
-// A span of memory: per token, `width` bytes from `at`; tokens lie `step` bytes apart.
+// A span of memory: `width` bytes for each of `heads` heads of `tokens` tokens, which lie so many bytes apart.
 struct Span {
     uintptr_t at;
-    int64_t tokens, step, width;
-    uintptr_t end() const { return at + (uintptr_t)((tokens - 1) * step + width); }
+    int64_t tokens, token, heads, head, width;
+    uintptr_t end() const { return at + (uintptr_t)((tokens - 1) * token + (heads - 1) * head + width); }
+    // All of it, seen modulo a step that its strides are multiples of or do not reach.
+    int64_t modulo(int64_t step) const { return width + (token % step == 0 ? 0 : (tokens - 1) * token) + (head % step == 0 ? 0 : (heads - 1) * head); }
 };
 
-// Whether two spans may share a byte.  Spans with the same step that lie side by side within it do not.
+// Whether two spans may share a byte.  Spans that lie side by side within a stride of theirs, token by token or head by head, do not.
 bool meet(const Span &a, const Span &b)
 {
     if (a.tokens < 1 || b.tokens < 1 || a.end() <= b.at || b.end() <= a.at) return false;
-    if (a.step == b.step && a.step > 0) {
-        const int64_t ahead = (int64_t)((b.at - a.at) % (uintptr_t)a.step), off = b.at >= a.at ? ahead : (a.step - (int64_t)((a.at - b.at) % (uintptr_t)a.step)) % a.step;
-        if (off >= a.width && off + b.width <= a.step) return false;
+    for (const int64_t step : {a.token, a.head, b.token, b.head}) {
+        if (step < 1) continue;
+        const int64_t behind = (int64_t)((b.at > a.at ? b.at - a.at : a.at - b.at) % (uintptr_t)step), off = b.at >= a.at ? behind : (step - behind) % step;
+        if (off >= a.modulo(step) && off + b.modulo(step) <= step) return false;
     }
     return true;
 }
@@ -70,7 +73,7 @@ cf_status check_rows(const cf_rows &in, int64_t tokens, int64_t heads, int64_t d
     out.data = static_cast<char *>(in.data);
     out.token = token * 2;
     out.head = head * 2;
-    span = {reinterpret_cast<uintptr_t>(in.data), tokens, out.token, ((heads - 1) * head + dim) * 2};
+    span = {reinterpret_cast<uintptr_t>(in.data), tokens, out.token, heads, out.head, dim * 2};
     return CF_OK;
 }
 
@@ -89,7 +92,7 @@ cf_status check_cache(const cf_kv_cache *c, const Heads &h, Cache &out, Span &k,
     out.n_pages = (int32_t)c->n_pages;
     out.page_size = c->page_size;
     out.page_shift = __builtin_ctz((unsigned)c->page_size);
-    k = {reinterpret_cast<uintptr_t>(c->k), c->n_pages, stride * 2, dense * 2};
+    k = {reinterpret_cast<uintptr_t>(c->k), c->n_pages, stride * 2, 1, 0, dense * 2};
     v = k;
     v.at = reinterpret_cast<uintptr_t>(c->v);
     return meet(k, v) ? CF_ERR_INVALID_ARG : CF_OK;
@@ -375,8 +378,8 @@ cf_status cf_attn_join(const cf_attn_desc *desc, const cf_join *args, void *stre
     const int64_t width = (int64_t)desc->q_heads * desc->head_dim * (args->part_dtype == CF_F32 ? 4 : 2);
     for (int i = 0; i < args->n_parts; ++i) {
         if (!args->parts[i] || !aligned(args->parts[i], 16) || !args->lses[i] || !aligned(args->lses[i], 4)) return CF_ERR_INVALID_ARG;
-        if (meet(so, {reinterpret_cast<uintptr_t>(args->parts[i]), 1, 0, args->n_tokens * width})) return CF_ERR_INVALID_ARG;
-        if (args->lse && meet({reinterpret_cast<uintptr_t>(args->lse), 1, 0, a.n_rows * 4}, {reinterpret_cast<uintptr_t>(args->lses[i]), 1, 0, a.n_rows * 4})) return CF_ERR_INVALID_ARG;
+        if (meet(so, {reinterpret_cast<uintptr_t>(args->parts[i]), 1, 0, 1, 0, args->n_tokens * width})) return CF_ERR_INVALID_ARG;
+        if (args->lse && meet({reinterpret_cast<uintptr_t>(args->lse), 1, 0, 1, 0, a.n_rows * 4}, {reinterpret_cast<uintptr_t>(args->lses[i]), 1, 0, 1, 0, a.n_rows * 4})) return CF_ERR_INVALID_ARG;
         a.parts[i] = args->parts[i];
         a.lses[i] = args->lses[i];
     }
