@@ -27,9 +27,9 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int BF16 = 1, F16 = 2;    // cf_dtype
 constexpr float kLn2 = 0.693147180559945309f;
-// Where a row's reference, which its scores (times log2 e) are taken relative to, begins: below every finite score, and not -infinity, so that
-// score - maximum is -infinity, and the weight 0, for a masked score of a row that has seen no other.
-constexpr float kNoMax = -3.0e38f;
+// Where a row's reference, which its scores (times log2 e) are taken relative to, begins: the lowest finite number, and not -infinity, so that
+// score - reference is -infinity, and the weight 0, for a masked score of a row that has seen no other.
+constexpr float kNoMax = -3.402823466e38f;
 // A row's accumulators are scaled down when a score passes the reference in use by more than Elem::kMostOver powers of two.  bf16: the reference is a maximum, weights
 // reach 2^8 at most, their rounding is relative, and sums of 2^31 of them stay finite in fp32.  fp16 holds numbers from 2^-14 on in full and none below 2^-25, and keys that weigh
 // less than that next to the largest may weigh much together.  So there the reference lies kLift below the maximum, and it follows the scores down, too: where all of a
