@@ -106,6 +106,15 @@ template <int DT> __device__ __forceinline__ float reference(float m, float top,
     else return fmaxf(m, top);
 }
 
+// Enqueues a kernel of 256 threads a workgroup.  -> what came of it, and not of some call before it: the runtime remembers an error until it is asked.
+template <typename Args> hipError_t enqueue(void (*kernel)(Args), int64_t workgroups, hipStream_t s, Args a)
+{
+    void *args[] = {&a};
+    const hipError_t e = hipLaunchKernel(reinterpret_cast<const void *>(kernel), dim3((unsigned)workgroups), dim3(256), args, 0, s);
+    if (e != hipSuccess) (void)hipGetLastError();
+    return e;
+}
+
 __device__ __forceinline__ float lse_of(float m, float l) { return l > 0.0f || l != l ? (m + __log2f(l)) * kLn2 : -__builtin_inff(); }
 __device__ __forceinline__ float inverse_of(float l) { return l > 0.0f || l != l ? 1.0f / l : 0.0f; }
 

@@ -366,10 +366,7 @@ template <int DT, int D, bool MANY> __global__ __launch_bounds__(kWaves * 64, D 
 
 template <int DT, int D> hipError_t paged_dim(const PagedArgs &a, hipStream_t s)
 {
-    const dim3 grid((unsigned)paged_workgroups(a));
-    if (a.many) hipLaunchKernelGGL((k_attn_paged<DT, D, true>), grid, dim3(kWaves * 64), 0, s, a);
-    else hipLaunchKernelGGL((k_attn_paged<DT, D, false>), grid, dim3(kWaves * 64), 0, s, a);
-    return hipGetLastError();
+    return a.many ? enqueue(k_attn_paged<DT, D, true>, paged_workgroups(a), s, a) : enqueue(k_attn_paged<DT, D, false>, paged_workgroups(a), s, a);
 }
 
 template <int DT> hipError_t paged_typed(const PagedArgs &a, hipStream_t s)

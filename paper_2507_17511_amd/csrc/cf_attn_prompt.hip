@@ -19,7 +19,7 @@ namespace cf {
 namespace attn {
 namespace {
 
-constexpr int kWaves = 4;
+constexpr int kWaves = 4;           // enqueue() launches as many
 static_assert(kPromptRows == kWaves * 32, "a wave has 32 rows");
 
 // Where the 16-byte vectors of a staged tile's row lie: XORed so that neither the reads of K (16 rows, one vector each) nor the
@@ -467,21 +467,16 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 :
     }
 }
 
-template <int DT, int D> hipError_t prompt_dim(const PromptArgs &a, hipStream_t s)
-{
-    hipLaunchKernelGGL((k_attn_prompt<DT, D>), dim3((unsigned)prompt_workgroups(a)), dim3(kWaves * 64), 0, s, a);
-    return hipGetLastError();
-}
-
 }  // namespace
 
 hipError_t launch_prompt(const PromptArgs &a, hipStream_t s)
 {
     const bool bf16 = a.h.dtype == BF16;
+    const int64_t n = prompt_workgroups(a);
     switch (a.h.head_dim) {
-    case 64: return bf16 ? prompt_dim<BF16, 64>(a, s) : prompt_dim<F16, 64>(a, s);
-    case 128: return bf16 ? prompt_dim<BF16, 128>(a, s) : prompt_dim<F16, 128>(a, s);
-    default: return bf16 ? prompt_dim<BF16, 256>(a, s) : prompt_dim<F16, 256>(a, s);
+    case 64: return bf16 ? enqueue(k_attn_prompt<BF16, 64>, n, s, a) : enqueue(k_attn_prompt<F16, 64>, n, s, a);
+    case 128: return bf16 ? enqueue(k_attn_prompt<BF16, 128>, n, s, a) : enqueue(k_attn_prompt<F16, 128>, n, s, a);
+    default: return bf16 ? enqueue(k_attn_prompt<BF16, 256>, n, s, a) : enqueue(k_attn_prompt<F16, 256>, n, s, a);
     }
 }
 

@@ -162,8 +162,7 @@ template <int DT, int PT, int D, int SPREAD, int EACH> __global__ __launch_bound
 
 template <int DT, int PT, int D, int SPREAD, int EACH> hipError_t join_over(const JoinArgs &a, hipStream_t s)
 {
-    hipLaunchKernelGGL((k_attn_join<DT, PT, D, SPREAD, EACH>), dim3((unsigned)join_workgroups(a)), dim3(256), 0, s, a);
-    return hipGetLastError();
+    return enqueue(k_attn_join<DT, PT, D, SPREAD, EACH>, join_workgroups(a), s, a);
 }
 
 template <int DT, int PT, int D> hipError_t join_dim(const JoinArgs &a, hipStream_t s)
@@ -187,13 +186,12 @@ template <int DT, int PT> hipError_t join_typed(const JoinArgs &a, hipStream_t s
 
 template <int DT> hipError_t append_typed(const AppendArgs &a, hipStream_t s)
 {
-    const unsigned grid = (unsigned)append_workgroups(a);
+    const int64_t n = append_workgroups(a);
     switch (a.h.head_dim) {
-    case 64: hipLaunchKernelGGL((k_kv_append<DT, 64>), dim3(grid), dim3(256), 0, s, a); break;
-    case 128: hipLaunchKernelGGL((k_kv_append<DT, 128>), dim3(grid), dim3(256), 0, s, a); break;
-    default: hipLaunchKernelGGL((k_kv_append<DT, 256>), dim3(grid), dim3(256), 0, s, a); break;
+    case 64: return enqueue(k_kv_append<DT, 64>, n, s, a);
+    case 128: return enqueue(k_kv_append<DT, 128>, n, s, a);
+    default: return enqueue(k_kv_append<DT, 256>, n, s, a);
     }
-    return hipGetLastError();
 }
 
 }  // namespace
