@@ -338,8 +338,8 @@ const char *cf_profile_kernel_name(const cf_ctx *ctx, int32_t k);
  *
  * Arithmetic.  Scores, the running maximum and sum of the softmax and all accumulators are fp32; the weights
  * exp(score - maximum) are rounded once to `dtype` for the product with the values on the matrix cores, and outputs are
- * rounded once.  In fp16, whose smallest numbers are 2^-24, weights are taken relative to scores near their own keys', so that keys that weigh little
- * each and much together keep their part: what is rounded to fewer bits than 11 is within 2^-15 of the weights of the keys around it.  Results do not depend on timing: the same call on the same data gives the same bits.
+ * rounded once.  In fp16, whose smallest numbers are 2^-24, what weights are relative to falls with the scores, so that keys that weigh little
+ * each and much together, behind a first key that leads them all by far, keep their part; where scores differ so much again and again, it stays.  Results do not depend on timing: the same call on the same data gives the same bits.
  * Keys that a row does not see (masked, past the end of a sequence, on a page beyond the context) do not
  * reach its output or its log-sum-exp, whatever those places hold, NaN and infinities included.  A row that sees no
  * key, or whose scores are all -infinity, gives zeros and a log-sum-exp of -infinity. */

@@ -32,11 +32,14 @@ constexpr float kLn2 = 0.693147180559945309f;
 constexpr float kNoMax = -3.402823466e38f;
 // A row's accumulators are scaled down when a score passes the reference in use by more than Elem::kMostOver powers of two.  bf16: the reference is a maximum, weights
 // reach 2^8 at most, their rounding is relative, and sums of 2^31 of them stay finite in fp32.  fp16 holds numbers from 2^-14 on in full and none below 2^-25, and keys that weigh
-// less than that next to the largest may weigh much together.  So there the reference lies kLift below the maximum, and it follows the scores down, too: where all of a
-// row's keys at hand (64 at most) have scores less than kLeastOver over it, or weights that sum up to less than kLeastSum, it is lowered and the accumulators are
-// scaled up.  Their rounding is then within 2^-15 of their sum.  The sum of all weights stays below 2^kMostTotal; past kFullTotal nothing is lowered: what is at hand is below 2^-60 of the row.
-constexpr float kLeastOver = -4.0f;
-constexpr float kLeastSum = 0.0625f;
+// less than that next to the largest may weigh much together, behind a first token that all rows attend to, say.  So there
+// - a score that passes the reference by more than kJump, as the first keys' do, sets it kLift below itself: what shares a tile with it keeps more of its bits;
+// - the reference falls, too, and the accumulators are scaled up, where all of a row's keys at hand (64 at most) are less than kLeastOver over it, or their weights sum up to
+//   less than kLeastSum.  Other sums are off by the rounding of 64 weights to 2^-24 at most: 2^-8 of the least if all were rounded one way, and they average out.
+// The sum of all weights stays below 2^kMostTotal; past kFullTotal nothing falls: what is at hand is below 2^-60 of the row.
+constexpr float kJump = 15.0f, kLift = 6.0f;
+constexpr float kLeastOver = -11.0f;
+constexpr float kLeastSum = 0.00048828125f;                 // 2^-11
 constexpr float kMostTotal = 60.0f;
 constexpr float kFullTotal = 288230376151711744.0f;        // 2^58
 // Where the maximum is not looked for (see k_attn_prompt): the most that the weights of a lane's keys of one tile may sum up to.  No weight is
@@ -57,7 +60,7 @@ template <uint32_t EXPONENT> struct OddPair {
 template <> struct Elem<BF16> {
     using Odd = OddPair<0x7f80u>;
     static constexpr bool kFollow = false;                          // whether the reference follows the scores down
-    static constexpr float kLift = 0.0f, kMostOver = 8.0f;
+    static constexpr float kMostOver = 8.0f;
     static __device__ __forceinline__ uint32_t pack(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, bf16x2)); }
     static __device__ __forceinline__ float lo(uint32_t w) { return __uint_as_float(w << 16); }
     static __device__ __forceinline__ float hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
@@ -67,7 +70,7 @@ template <> struct Elem<BF16> {
 template <> struct Elem<F16> {
     using Odd = OddPair<0x7c00u>;
     static constexpr bool kFollow = true;
-    static constexpr float kLift = 6.0f, kMostOver = 14.0f;         // 32 weights of 2^6 stay below kMostSum
+    static constexpr float kMostOver = 15.0f;
     static __device__ __forceinline__ uint32_t pack(float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, f16x2)); }
     static __device__ __forceinline__ float lo(uint32_t w) { return (float)__builtin_bit_cast(f16x2, w)[0]; }
     static __device__ __forceinline__ float hi(uint32_t w) { return (float)__builtin_bit_cast(f16x2, w)[1]; }
@@ -99,11 +102,12 @@ __device__ __forceinline__ float sum_quarters(float x)
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// The reference after keys whose largest score is `top`, given the largest part of the row's sum that a lane has.
-template <int DT> __device__ __forceinline__ float reference(float m, float top, float total)
+// The reference after keys whose largest score is `top`; whether it may fall, and the largest part of the row's sum that a lane has.
+template <int DT> __device__ __forceinline__ float reference(float m, float top, bool fall, float total)
 {
-    if constexpr (Elem<DT>::kFollow) return top > -__builtin_inff() ? fmaxf(top - Elem<DT>::kLift, m - fmaxf(kMostTotal - __log2f(total), 0.0f)) : m;
-    else return fmaxf(m, top);
+    if constexpr (!Elem<DT>::kFollow) return fmaxf(m, top);
+    const float raised = top > m + kJump ? top - kLift : fmaxf(m, top);
+    return fall && top < m + kLeastOver && top > -__builtin_inff() ? fmaxf(top, m - fmaxf(kMostTotal - __log2f(total), 0.0f)) : raised;
 }
 
 // Enqueues a kernel of 256 threads a workgroup.  -> what came of it, and not of some call before it: the runtime remembers an error until it is asked.

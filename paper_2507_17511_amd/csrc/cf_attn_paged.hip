@@ -205,7 +205,7 @@ template <int DT, int D, bool MANY> __global__ __launch_bounds__(kWaves * 64, D 
                     }
                 }
                 if (moves) {
-                    const float fresh = reference<DT>(m, max_quarters(max_halves(top)), E::kFollow ? max_quarters(max_halves(l)) : 0.0f), scale = exp2_fast(m - fresh);
+                    const float fresh = reference<DT>(m, max_quarters(max_halves(top)), true, E::kFollow ? max_quarters(max_halves(l)) : 0.0f), scale = exp2_fast(m - fresh);
 #pragma unroll
                     for (int d = 0; d < kPer; ++d)
 #pragma unroll

@@ -20,6 +20,10 @@ namespace attn {
 namespace {
 
 constexpr int kWaves = 4;           // enqueue() launches as many
+// How often the reference of a wave's rows falls.  For a first token that all rows attend to, and for one in a sequence's middle, once; where scores differ widely everywhere rows
+// would have it fall and rise in turn, a tile done again for each (us, queries 3 and 10 times as large, without a limit / two falls / none and no lift: 8192 tokens of 24 heads of
+// 128 over as many keys 929 / 887 / 871 and 1318 / 893 / 863; of 64 587 / 526 / 507 and 953 / 566 / 540).
+constexpr int kMostFalls = 2;
 static_assert(kPromptRows == kWaves * 32, "a wave has 32 rows");
 
 // Where the 16-byte vectors of a staged tile's row lie: XORed so that neither the reads of K (16 rows, one vector each) nor the
@@ -227,8 +231,8 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 :
             for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
         return max_halves(top) * c;
     };
-    auto rescale = [&](float top) {
-        const float fresh = reference<DT>(m, top, E::kFollow ? max_halves(l) : 0.0f), scale = exp2_fast(m - fresh);
+    auto rescale = [&](float top, bool fall) {
+        const float fresh = reference<DT>(m, top, fall, E::kFollow ? max_halves(l) : 0.0f), scale = exp2_fast(m - fresh);
 #pragma unroll
         for (int d = 0; d < kBlocks; ++d)
 #pragma unroll
@@ -277,20 +281,24 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 :
     // Tiles that all rows of the wave see, up to the last but one.  Their maximum is not looked for: weights are positive, so
     // that none is larger than their sum.  Where that passes kMostSum, in any lane, the tile is done again after its maximum has been taken and the
     // accumulators scaled; most often that is the first tile alone.  That happens outside of the inner loop, where the compiler keeps them in place.
-    // A tile is done again once, for a lane's weights sum up to less than 2^kLift * 2 * 32 then, and too little once is enough: either scores are rounded as the maximum is, or that is
+    // A tile is done again once, for a lane's weights sum up to less than 2^kLift * 2 * 32 then, and falls are counted: either scores are rounded as the maximum is, or that is
     // kMostExact at most, and the wave of a row beyond it, whose scores are of no use, infinite or none, takes the loop after this one.  The rounding costs
     // 16384 rows of 24 heads of 128 3022 us for 2937; with the way out instead of it, wide heads' accumulators would leave the registers (325 us for
     // 245: 2 x 333 tokens over 20333 keys).
     int settled = 0;            // the tile that the reference was set for
+    int falls = kMostFalls;
+    bool fall = false;
     // Whether a tile has to be done again: its weights sum up to too much, or in fp16 to too little.
     auto unfit = [&](float sum) -> bool {
         if constexpr (!E::kFollow) return __any(sum > kMostSum);
         if (__builtin_expect(!__any(sum > kMostSum || sum < kLeastSum), 1)) return false;
-        return __any(sum > kMostSum) || (key0 != settled && __any(sum_halves(sum) < kLeastSum && max_halves(l) < kFullTotal));
+        fall = falls > 0 && key0 != settled && __any(sum_halves(sum) < kLeastSum && max_halves(l) < kFullTotal);
+        falls -= fall;
+        return fall || __any(sum > kMostSum);
     };
     if constexpr (kAhead) {
         while (key0 + 2 * kKeys <= edge) {
-            rescale(largest(s));
+            rescale(largest(s), fall);
             settled = key0;
             if (__any(fabsf(m) > kMostExact)) break;
             do {
@@ -308,7 +316,7 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 :
     } else {
         while (key0 + kKeys <= edge) {
             scores(s, buffer);
-            rescale(largest(s));
+            rescale(largest(s), fall);
             settled = key0;
             do {
                 scores(s, buffer);
@@ -331,7 +339,9 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 :
     // Takes s in.
     auto weigh = [&]() {
         const float top = largest(s);
-        if (__any(top > m + E::kMostOver || (E::kFollow && top < m + kLeastOver && top > -__builtin_inff() && max_halves(l) < kFullTotal))) rescale(top);
+        fall = E::kFollow && falls > 0 && __any(top < m + kLeastOver && top > -__builtin_inff() && max_halves(l) < kFullTotal);
+        falls -= fall;
+        if (fall || __any(top > m + E::kMostOver)) rescale(top, fall);
         l += weights(std::true_type{});
     };
     int odd_from = limit;       // the tiles from here on are done at the end

@@ -1,10 +1,11 @@
 """fp16 keys that weigh little each and much together, behind a first key that leads by `ahead` and whose value is nearly zero: what most models'
 first token is to the rest.  Their weights, relative to the largest, are below what fp16 holds in full (2^-14) or at all (2^-25).
 
-Tolerances.  u = 2^-11.  A weight is rounded by a relative u, or below 2^-14 by 2^-25, as it is stored: 2^4 times itself at least, relative to the largest
-of its 64 keys (a tile), whose weights sum up to 2^-4 at least, or to 2^6 where the largest of all keys is among them.  So the 64 keys that the leading one shares a tile
-with are off by 64 2^-25 / 2^6 = 2^-25 max|v|, and others by 64 2^-25 / 2^-4 = 2^-15 of their share of the weights times max|v|, on top of what attention_reference
-says of the relative roundings.  That is no smaller than what the kernels promise, but 2^-9 of what the lost weights summed up to."""
+Tolerances.  u = 2^-11.  A weight is rounded by a relative u, or below 2^-14 by 2^-25 as it is stored: relative to 2^-6 of the largest of its 64 keys (a tile) that were
+there first, or so that they sum up to 2^-11 at least.  So the 64 keys that the leading one shares a tile with are off by 64 2^-25 / 2^6 = 2^-25 max|v| at most.  Other
+keys' weights, which differ from one another here, are rounded up as often as down: 2^-15 of their share of the weights times max|v| are 2^-7 of what 64 weights of 2^-17 could
+be off by all one way, a tile's average over some hundred tiles and more, and 2^-5 for a handful, where attention_reference's relative roundings, 2^-11 each, cover
+them.  That is 2^-9 of what the lost weights summed up to."""
 import math
 
 import pytest
