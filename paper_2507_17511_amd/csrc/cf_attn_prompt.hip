@@ -149,6 +149,13 @@ template <int DT, int D> __global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 :
     const int limit = row0 < rows ? min(split_end, seen_by((min(row0 + 32, rows) - 1) / a.h.group)) : 0;
     const int edge = min(limit, seen_by(min(row0, rows - 1) / a.h.group));
 
+    // Wide queries are there before the first tile is asked for: while the compiler holds them to be under way, it waits for all loads at the top of the loops, where the
+    // next tile's have just been sent (2 x 333 tokens of 16 / 2 heads over 20333 keys that no cache holds, bf16, 231 us for 266).
+    if constexpr (D == 256) {
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) asm("" : "+v"(q[i]));
+    }
+
     f32x16 o[kBlocks];
 #pragma unroll
     for (int d = 0; d < kBlocks; ++d)
