@@ -55,9 +55,10 @@ struct PagedArgs {
     float *lse;
     const int32_t *table, *lens;
     int64_t table_stride;
-    int32_t n_seqs, max_pages;
+    int32_t n_seqs, max_pages;      // of one launch: some of a call's sequences where there are many
     int32_t n_splits, split_keys;
-    int32_t many;                   // more parts than workgroups; they are joined by a kernel of its own
+    int32_t many;                   // parts are listed and taken in turn, and joined by a kernel of its own: where there are more than four a CU, or contexts that may differ
+                                    // could fill 128 MB
     uint32_t *counters;             // one for every (sequence, unit of heads): parts that have landed; zero between calls
     Parts parts;                    // its log-sum-exps are of powers of two unless `many`
 };

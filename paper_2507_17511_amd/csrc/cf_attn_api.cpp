@@ -179,7 +179,8 @@ hipError_t paged_at_once(PagedArgs &a, int64_t longest, int64_t most_keys, void 
 {
     const int64_t units = paged_units(a);
     const int64_t rows = (int64_t)a.n_seqs * a.h.q_heads;
-    // Two workgroups a CU, of 128 to 1024 keys each, and 32 parts at most where that gives every CU one: a part costs its join about 0.1 us, 128
+    // Two workgroups a CU, of 128 to 1024 keys each (4096 where there are many sequences, more where 64 parts or the workspace's do not reach), and 32 parts at most
+    // where that gives every CU one: a part costs its join about 0.1 us, 128
     // keys a workgroup 1.2 us.  us, on one card: 1 x 901 keys, 2 heads of keys: parts of 128 / 256 / 512 keys 8.2 / 9.6 / 11.4; 1 x 8192, 8 heads: 128 / 256
     // / 512 16.7 / 13.0 / 13.6; 8 x 8192, 8 heads: two / three / six workgroups a CU 45 / 49 / 53; 64 x 7 to 700: 14.5 / 18.1 / 16.1.  Parts of 512 / 1024 /
     // 2048 keys, 8 heads of 128: 96 x 160 to 16000 275 / 273 / 271, 96 x 3540 264 / 251 / 243; of 256: 48 x 160 to 16000 282 / 279 / 300; of 64: 200 x 50

@@ -1,12 +1,13 @@
-// Attention of one new token per sequence over a paged cache: every cached key and value is read once, by one
-// workgroup, straight into registers in the layouts that the matrix instructions take; nothing is staged.
+// Attention of one new token per sequence over a paged cache: every cached key and value is read once for 16 query heads
+// that share it (a group of 17 reads it twice), by one workgroup, straight into registers in the layouts that the matrix
+// instructions take; nothing is staged.
 //
 // A wave takes 32 keys at a time.  S^T = K Q^T in two products of 16 keys by 16 heads; which key is which row
 // of them is chosen so that a lane's 8 scores are those of 8 neighbouring keys, the right operand of O^T = V^T P^T.
 // For the left one a lane reads 8 (4, 16) elements of the same 8 keys and turns that block with byte permutes.
 //
-// Bound by HBM: 96 contexts of 160 to 16000 keys, 32 / 8 heads of 128, 272 us (5.1 TB/s); 2 of 131100, 24 heads of 64, 283 us (5.7 TB/s); one
-// of 901 keys, 8 / 2 heads, by latency: 7.3 us, of which the launch is a third.  Through LDS the same bytes would wait for a barrier a step, and the
+// Bound by HBM: 96 contexts of 160 to 16000 keys, 32 / 8 heads of 128, 275 us (5.1 TB/s; sums over rows of 2 GiB, read once, reach 5.9); 2 of 131100, 24 heads
+// of 64, 285 us (5.7 TB/s); one of 901 keys, 8 / 2 heads, by latency: 7.6 us, of which the launch is a third.  Through LDS the same bytes would wait for a barrier a step, and the
 // products need 16 columns for the one to 16 heads that share keys, whoever brings them.
 #include "cf_attn_device.h"
 #include "compactfusion.h"

@@ -7,10 +7,10 @@
 // the right operand of O^T = V^T P^T, up to an order of the keys that the reads of V follow, so weights
 // never leave their lane, and the row's maximum, sum and scale are scalars of the lane.
 //
-// Bound by the matrix cores, large calls by the power that they take: 16384 tokens of 24 heads of 128 over as many keys 2.94 ms, 1120 TFLOP/s,
-// and 2.09 ms where all operands are zeros, at a higher clock.  Two workgroups a CU, 256 registers a lane: a wave of 64 rows reads half of the LDS per product
-// but is alone on its SIMD (3.01 ms, zeros 2.57).  2 x 8191 tokens of 32 / 8 heads, causal, 1.02 ms (1080 TFLOP/s); ragged batches are bound by
-// what a workgroup does before its first and after its last product: 14 x 1 to 2003 tokens 89 us (650 TFLOP/s).
+// Bound by the matrix cores and what feeds them: 16384 tokens of 24 heads of 128 over as many keys 2.84 to 3.04 ms on three cards, 1085 to 1160 TFLOP/s.  The matrix cores
+// are busy in 63 % of the cycles, with 4.5 vector instructions each beside them, and the clock falls with the power that this takes: 2.06 ms where all operands are zeros.  Two workgroups a CU, 256 registers a lane: a wave of 64 rows reads half of the LDS per product
+// but is alone on its SIMD (3.01 ms, zeros 2.57).  2 x 8191 tokens of 32 / 8 heads, causal, 0.97 to 1.05 ms (1045 to 1130 TFLOP/s); ragged batches are bound by
+// what a workgroup does before its first and after its last product: 14 x 1 to 2003 tokens 79 to 83 us (700 to 730 TFLOP/s).
 #include <type_traits>
 
 #include "cf_attn_device.h"

@@ -6,7 +6,7 @@ entry point next to the codec, as a serving program would run them.
 `peers` devices hold a shard of one layer's tokens each (they take turns on one GPU here; the packed codes in its memory stand in for the
 wire).  In every step each peer sends its keys and values through the codec, and attends its own queries to one shard after
 another -- its own as they are, the others as reconstructed -- joining the hops by their log-sum-exps (arxiv 2507.17511, App. B
-Alg. 2).  After the last step one peer takes all keys and values into a paged cache, rotated by their positions, and decodes
+Alg. 2); a hop's output is rounded to bf16 before that.  After the last step one peer takes all keys and values into a paged cache, rotated by their positions, and decodes
 tokens from it.  Inputs are synthetic; the command prints how far each result is from fp32 attention over the same keys and values.
 """
 from __future__ import annotations
