@@ -92,6 +92,7 @@ class AttentionSession:
         self._desc = ctypes.byref(self.desc)
         self.ws_bytes = workspace_bytes
         self._stream = stream
+        self._handle = stream.cuda_stream if stream is not None else None if self._index >= 0 else 0       # None: torch's current one
         self._settled = set()       # streams on which there is nothing more to do for a call than to make it
         self.workspace = self._ws = None
         self._unset = False         # whether the workspace's zeros were captured into a graph, which is yet to run
@@ -106,7 +107,7 @@ class AttentionSession:
 
     # The library launches on the device that is current, and the null stream, torch's default one, is that device's.
     def _call(self, entry, name: str, *args) -> None:
-        on = _raw_stream(self._index) if self._stream is None else self._stream.cuda_stream
+        on = _raw_stream(self._index) if self._handle is None else self._handle
         if on in self._settled and _current_device() == self._index:
             status = entry(*args, on)
         else:

@@ -148,10 +148,11 @@ def test_a_workspace_made_during_a_capture_is_zero_for_calls_outside_of_it(machi
     assert found == [0, 0, 0, 9, 9]
 
 
-def test_tensors_of_the_host_do_not_reach_the_library():
+@pytest.mark.parametrize("stream", [None, types.SimpleNamespace(cuda_stream=0)])
+def test_tensors_of_the_host_do_not_reach_the_library(stream):
     """Its kernels would read and write the host's addresses."""
     calls = []
-    s = AttentionSession(4, 2, 64, device="cpu", workspace_bytes=0, stream=types.SimpleNamespace(cuda_stream=0))
+    s = AttentionSession(4, 2, 64, device="cpu", workspace_bytes=0, stream=stream)
     s._lib = types.SimpleNamespace(**{name: lambda *a: calls.append(a) or 0 for name in ("cf_kv_append", "cf_attn_prompt", "cf_attn_paged", "cf_attn_join")})
     q, k, v = (torch.zeros(3, h, 64, dtype=torch.bfloat16) for h in (4, 2, 2))
     cache = attention.PagedCache.empty(3, 2, 64, page_size=16, device="cpu")
