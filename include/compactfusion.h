@@ -441,6 +441,92 @@ typedef struct {
  * adds nothing to it, whatever its output there holds. */
 cf_status cf_attn_join(const cf_attn_desc *desc, const cf_join *args, void *stream);
 
+/* ---------------------------------------------------------------- serving from a cache in 8 bits
+ *
+ * What a program calls that generates tokens step by step: pages and slots from the sequences' lengths (cf_kv_plan), keys and
+ * values appended as 8-bit codes (cf_kv_append8), attention of one token per sequence over them (cf_attn_paged8), or over those
+ * pages alone that a cheap score selects for each head (cf_attn_select).  The rules of the calls above hold for these too.
+ *
+ * Codes.  An element is code x scale, rounded once: codes are 8-bit floats of 4 exponent and 3 mantissa bits (OCP e4m3: largest 448,
+ * least 2^-9, no infinities), the scale is one for all keys (values) of a head on a page, and a power of two from 2^-100 to 2^119: the least that
+ * brings the largest magnitude to 448 at most.  Magnitudes, infinite ones among them, are 448 x 2^119 (bf16) or 240 x 2^8 (fp16) at most, the
+ * largest codes that the type holds; NaN stays NaN, and counts as 0 in scales and bounds. */
+
+/* Codes and scales in pages: code i of head h of slot s is k[(s / page_size) * page_stride + (h * page_size + s % page_size) * head_dim + i],
+ * its scale k_scale[(s / page_size) * kv_heads + h]. */
+typedef struct {
+    void *k, *v;             /* 16-byte aligned; they must not overlap, except that pages of one may lie between pages of the other */
+    float *k_scale, *v_scale;/* [n_pages][kv_heads] each, dense.  Of a number that is no such power of two the exponent counts */
+    void *bounds;            /* bf16 [n_pages][kv_heads][2][head_dim], dense, 16-byte aligned: the least and the largest of each channel of a page's keys; may be null (cf_attn_select reads it) */
+    int64_t n_pages;         /* 1 .. 2^31 - 1 */
+    int64_t page_stride;     /* elements (bytes) from page to page, a multiple of 16; 0 = kv_heads * page_size * head_dim (dense), less is refused, and so is more than 2^60 bytes of pages */
+    int32_t page_size;       /* tokens of a page: 16, 32, 64 or 128 */
+} cf_kv_cache8;
+
+/* cf_kv_append into such a cache: rotation in fp32, then codes, with one rounding.  Tokens of a call that go to the same page are neighbours in it, with no
+ * other tokens between them (as those of a sequence are); otherwise what that page holds afterwards is undefined.  A token at a page's first place begins
+ * the page anew: its scales and bounds are those of the call's tokens.  On a page that is not begun the scale grows where the call's tokens need it, and the codes of all other
+ * places are rounded to the new one: exactly, but for those below 2^-6 of it.  The bounds are of elements as stored, and keep those of elements that were rounded again. */
+cf_status cf_kv_append8(const cf_attn_desc *desc, const cf_kv_cache8 *cache, const cf_append *args, void *stream);
+
+/* Pages that the heads attend to: of a context of fewer pages than count the first so many entries are read.  Entries outside of the
+ * context's pages (negative, say) are none; a page that is there twice counts twice. */
+typedef struct {
+    const int32_t *blocks;   /* device [n_seqs][kv_heads][count], dense: entry j of the sequence's row of the table */
+    int32_t count;           /* 1 .. 2^20 */
+} cf_blocks;
+
+/* cf_attn_paged over such a cache; with `blocks` (may be null: all pages) over those pages of the context alone.  A head's weights and
+ * values take part as `desc->dtype` holds them: codes times scales are exact in it, but in fp16 for magnitudes below 2^-21, and for those past
+ * 65504 of a cache that another type filled, which are infinite. */
+cf_status cf_attn_paged8(const cf_attn_desc *desc, const cf_kv_cache8 *cache, const cf_paged *args, const cf_blocks *blocks, void *workspace,
+                         size_t workspace_bytes, void *stream);
+
+typedef struct {
+    int32_t n_seqs;       /* >= 0 */
+    int32_t max_pages;    /* as in cf_paged, and so are the next five */
+    int64_t table_stride;
+    int64_t max_len;
+    const int32_t *table;
+    const int32_t *lens;
+    cf_rows q;            /* [n_seqs][q_heads][head_dim]: one token of every sequence */
+    int32_t count;        /* pages for each head, 1 .. 2^20 */
+    int32_t first, recent;/* so many of a context's first and of its last pages are always among them: >= 0, first + recent <= count */
+    int32_t *blocks;      /* device [n_seqs][kv_heads][count], dense: filled */
+} cf_select;
+
+/* For every sequence and head of keys the `count` pages of the context whose keys may score highest, in the order of the context, then -1.  The score of a page is
+ * sum over the heads that share the keys and over i of max(q_i least_i, q_i largest_i): no sum of a key's scores of these heads is larger.  It is summed in 64 bits, and of
+ * equal ones the earlier page is taken; NaN is the least of scores.  The scale of the scores does not matter.  The workspace (as for the attentions, not null) holds the scores: 8 bytes for each page of each
+ * head of keys; where it does not hold all, the call takes some at a time, and it has to hold those of one head (CF_ERR_WORKSPACE). */
+cf_status cf_attn_select(const cf_attn_desc *desc, const cf_kv_cache8 *cache, const cf_select *args, void *workspace, size_t workspace_bytes, void *stream);
+
+typedef struct {
+    int32_t n_seqs;          /* >= 0 */
+    int32_t page_size;       /* tokens of a page: a power of two, 16 .. 32768 */
+    int32_t max_pages;       /* >= 1: entries of a row of the table */
+    int32_t n_ring;          /* >= 1: entries of the ring, as many as the cache has pages */
+    int64_t table_stride;    /* entries from row to row, at least max_pages; 0 = max_pages */
+    int64_t n_tokens;        /* >= 0: entries of slots and positions; n_tokens at most 2^30 */
+    const int32_t *lens;     /* device [n_seqs]: tokens that each sequence holds */
+    const int32_t *news;     /* device [n_seqs]: tokens that come to it; negative: it has ended, and gives its pages back */
+    int32_t *table;          /* device [n_seqs][max_pages]: the sequences' pages; entries of new pages are written */
+    int32_t *ring;           /* device [n_ring]: free pages are ring[i % n_ring] for state[0] <= i < state[1]; pages that come back are written behind them */
+    const int64_t *state;    /* device [2]: pages taken from the ring and pages put into it, ever; not negative */
+    int64_t *state_out;      /* device [2]: after the call; may be state itself */
+    int32_t *lens_out;       /* device [n_seqs]: after the call, 0 for those that have ended; may be lens itself */
+    int32_t *cu;             /* device [n_seqs + 1]: where each sequence's new tokens begin among all */
+    int64_t *slots;          /* device [n_tokens]: where each token goes in the cache; -1 behind the last one, and for tokens that are not served */
+    int32_t *positions;      /* device [n_tokens]: its position in its sequence; -1 likewise */
+    int32_t *refused;        /* device [1]: sequences whose new tokens are not served */
+} cf_plan;
+
+/* Plans a step: new tokens get positions behind those that their sequences hold, and slots on the sequences' pages, the last one first and then new ones from the ring.
+ * Sequences are served in order, each with all of its new tokens or with none: with none if its row of the table or n_tokens is too short for it, and from the first one
+ * on for which the free pages do not suffice, if it needs any.  Pages that come back are free from the next call on.  A workspace (as for the
+ * attentions, its counters zero; 4 bytes of it are used) lets calls of many tokens run on more than one workgroup; it may be null. */
+cf_status cf_kv_plan(const cf_plan *args, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -34,7 +34,8 @@ CF_FLAG_TEST_NO_WAIT = 0x100
 EXPORTS = ["cf_sizes", "cf_workspace_bytes", "cf_init", "cf_warmup", "cf_set_warm", "cf_compress",
            "cf_decompress", "cf_step_fused", "cf_destroy", "cf_status_string", "cf_last_hip_error",
            "cf_profile_next_call", "cf_profile_launch_count", "cf_profile_kernel_name", "cf_check_device",
-           "cf_step_fused_static", "cf_given_up_items", "cf_kv_append", "cf_attn_prompt", "cf_attn_paged", "cf_attn_join"]
+           "cf_step_fused_static", "cf_given_up_items", "cf_kv_append", "cf_attn_prompt", "cf_attn_paged", "cf_attn_join", "cf_kv_append8",
+           "cf_attn_paged8", "cf_attn_select", "cf_kv_plan"]
 
 
 class cf_tensor_desc(ctypes.Structure):
@@ -80,6 +81,26 @@ class cf_paged(ctypes.Structure):
 class cf_join(ctypes.Structure):
     _fields_ = [("n_parts", _i32), ("part_dtype", _i32), ("n_tokens", _i64), ("parts", ctypes.POINTER(_vp)), ("lses", ctypes.POINTER(_vp)),
                 ("out", cf_rows), ("lse", _vp)]
+
+
+class cf_kv_cache8(ctypes.Structure):
+    _fields_ = [("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp), ("bounds", _vp), ("n_pages", _i64), ("page_stride", _i64),
+                ("page_size", _i32)]
+
+
+class cf_blocks(ctypes.Structure):
+    _fields_ = [("blocks", _vp), ("count", _i32)]
+
+
+class cf_select(ctypes.Structure):
+    _fields_ = [("n_seqs", _i32), ("max_pages", _i32), ("table_stride", _i64), ("max_len", _i64), ("table", _vp), ("lens", _vp),
+                ("q", cf_rows), ("count", _i32), ("first", _i32), ("recent", _i32), ("blocks", _vp)]
+
+
+class cf_plan(ctypes.Structure):
+    _fields_ = [("n_seqs", _i32), ("page_size", _i32), ("max_pages", _i32), ("n_ring", _i32), ("table_stride", _i64), ("n_tokens", _i64),
+                ("lens", _vp), ("news", _vp), ("table", _vp), ("ring", _vp), ("state", _vp), ("state_out", _vp), ("lens_out", _vp), ("cu", _vp),
+                ("slots", _vp), ("positions", _vp), ("refused", _vp)]
 
 
 class CFError(RuntimeError):
@@ -147,6 +168,15 @@ def lib() -> ctypes.CDLL:
         L.cf_attn_paged.argtypes = [desc_p, cache_p, ctypes.POINTER(cf_paged), vp, sz, vp]
         L.cf_attn_join.restype = i32
         L.cf_attn_join.argtypes = [desc_p, ctypes.POINTER(cf_join), vp]
+        cache8_p = ctypes.POINTER(cf_kv_cache8)
+        L.cf_kv_append8.restype = i32
+        L.cf_kv_append8.argtypes = [desc_p, cache8_p, ctypes.POINTER(cf_append), vp]
+        L.cf_attn_paged8.restype = i32
+        L.cf_attn_paged8.argtypes = [desc_p, cache8_p, ctypes.POINTER(cf_paged), ctypes.POINTER(cf_blocks), vp, sz, vp]
+        L.cf_attn_select.restype = i32
+        L.cf_attn_select.argtypes = [desc_p, cache8_p, ctypes.POINTER(cf_select), vp, sz, vp]
+        L.cf_kv_plan.restype = i32
+        L.cf_kv_plan.argtypes = [ctypes.POINTER(cf_plan), vp, sz, vp]
         L.cf_step_fused_static.restype = i32
         L.cf_step_fused_static.argtypes = [dp, i32, op, pp, pp, pp, pp, pp, vp]
         _lib = L
@@ -318,3 +348,22 @@ def cf_attn_paged(desc: cf_attn_desc, cache: cf_kv_cache, args: cf_paged, worksp
 
 def cf_attn_join(desc: cf_attn_desc, args: cf_join, stream=None) -> None:
     _check(lib().cf_attn_join(desc, args, _addr(stream)), "cf_attn_join")
+
+
+# ---------------------------------------------------------------- serving from a cache in 8 bits
+
+def cf_kv_append8(desc: cf_attn_desc, cache: cf_kv_cache8, args: cf_append, stream=None) -> None:
+    _check(lib().cf_kv_append8(desc, cache, args, _addr(stream)), "cf_kv_append8")
+
+
+def cf_attn_paged8(desc: cf_attn_desc, cache: cf_kv_cache8, args: cf_paged, blocks: Optional[cf_blocks] = None, workspace=None, workspace_bytes: int = 0,
+                   stream=None) -> None:
+    _check(lib().cf_attn_paged8(desc, cache, args, blocks, _addr(workspace), workspace_bytes, _addr(stream)), "cf_attn_paged8")
+
+
+def cf_attn_select(desc: cf_attn_desc, cache: cf_kv_cache8, args: cf_select, workspace=None, workspace_bytes: int = 0, stream=None) -> None:
+    _check(lib().cf_attn_select(desc, cache, args, _addr(workspace), workspace_bytes, _addr(stream)), "cf_attn_select")
+
+
+def cf_kv_plan(args: cf_plan, workspace=None, workspace_bytes: int = 0, stream=None) -> None:
+    _check(lib().cf_kv_plan(args, _addr(workspace), workspace_bytes, _addr(stream)), "cf_kv_plan")

@@ -1,0 +1,86 @@
+// Internal interface between the host half of the entry points for the cache in 8 bits (cf_attn8_api.cpp) and their
+// kernels (cf_attn8_paged.hip, cf_attn8_append.hip, cf_attn8_select.hip, cf_kv_plan.hip).  Not installed; not part of the ABI.
+#pragma once
+
+#include "cf_attn.h"
+
+namespace cf {
+namespace attn {
+
+struct Cache8 {
+    char *k, *v;
+    float *k_scale, *v_scale;       // [n_pages][kv_heads]
+    uint16_t *bounds;               // [n_pages][kv_heads][2][head_dim] or null
+    int64_t page_bytes;             // from page to page
+    int32_t n_pages, page_size, page_shift;
+};
+
+struct Paged8Args {
+    PagedArgs p;                    // its cache is not used
+    Cache8 cache;
+    const int32_t *blocks;          // [n_seqs][kv_heads][count], or null: all pages of a context, in order
+    int32_t count;
+};
+
+struct Append8Args {
+    Heads h;
+    Cache8 cache;
+    Rows k, v, q, q_out;            // q.data null: none
+    const int64_t *slots;
+    const int32_t *positions;
+    const float *cos, *sin;
+    int64_t n_tokens;
+    int32_t n_positions, rotary_dim, interleaved;
+    int32_t chunk;                  // tokens whose pages a wave takes
+    int32_t page_groups;            // workgroups that store keys and values; those behind them rotate queries
+};
+
+struct SelectArgs {
+    Heads h;
+    Cache8 cache;
+    Rows q;
+    const int32_t *table, *lens;
+    int64_t table_stride;
+    int32_t n_seqs, max_pages;
+    int32_t count, first, recent;
+    int32_t *blocks;
+    uint64_t *scores;               // [rows of a launch][columns]
+    int64_t first_row, n_rows;      // (sequence, head of keys) rows of a launch
+    int32_t columns;                // pages of the longest context that there may be
+    int32_t groups;                 // workgroups that score a row's pages
+};
+
+struct PlanArgs {
+    const int32_t *lens, *news;
+    int32_t *table, *ring;
+    const int64_t *state;
+    int64_t *state_out;
+    int32_t *lens_out, *cu, *positions, *refused;
+    int64_t *slots;
+    uint32_t *counter;              // zero between calls; of more than one workgroup
+    int64_t table_stride;
+    int32_t n_seqs, page_shift, max_pages, n_ring, n_tokens;
+    int32_t workgroups;
+};
+
+constexpr int kSelectPages = 64;    // that a workgroup of the scores takes
+constexpr int kPlanThreads = 1024;
+
+inline int64_t paged8_workgroups(const Paged8Args &a)
+{
+    const int64_t items = paged_units(a.p) * a.p.n_splits, held = 256 * (a.p.h.head_dim == 256 ? 2 : 3);
+    return a.p.many && held < items ? held : items;
+}
+
+inline int64_t append8_workgroups(const Append8Args &a)
+{
+    return a.page_groups + (a.q.data ? (a.n_tokens * a.h.q_heads * (a.h.head_dim / 16) + 255) / 256 : 0);
+}
+
+hipError_t launch_paged8(const Paged8Args &a, hipStream_t s);
+hipError_t launch_append8(const Append8Args &a, hipStream_t s);
+hipError_t launch_select(const SelectArgs &a, hipStream_t s);
+hipError_t launch_plan(const PlanArgs &a, hipStream_t s);
+
+}  // namespace attn
+}  // namespace cf

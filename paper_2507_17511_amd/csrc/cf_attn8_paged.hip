@@ -1,0 +1,293 @@
+// Attention of one new token per sequence over a paged cache of 8-bit codes: as over the one in 16 bits, every key and value is read once
+// for 16 query heads that share it, straight into registers, and the same matrix instructions of 16-bit numbers take them.  In between a
+// conversion brings two codes, times the scale of their page, into the type of the queries; codes times scales are exact there.
+//
+// A wave takes 64 keys at a time (32 where head_dim is 256), so that as many bytes are on their way to a CU as with 16 bits.  Of K a lane reads 16
+// neighbouring elements, the left operands of two instructions over the head dimension (the queries' lanes lie alike).  Of V it reads 4 (8, 16) elements
+// of 8 neighbouring keys; a byte permute brings the codes of two keys together before they are converted.
+#include "cf_attn_parts.h"
+#include "cf_attn8_device.h"
+
+namespace cf {
+namespace attn {
+namespace {
+
+// MANY: as in the kernel over 16 bits.  LISTED: heads attend to the listed pages of their contexts alone; keys are counted along the list.
+// WHOLE: a step's keys lie on one page.
+template <int DT, int D, bool MANY, bool LISTED, bool WHOLE> __global__ __launch_bounds__(kWaves * 64, D == 256 ? 2 : 3) void k_attn_paged8(Paged8Args b)
+{
+    using E = Elem<DT>;
+    using C = Code<DT>;
+    constexpr int kTiles = D == 256 ? 1 : 2;    // of 32 keys: a wave's step
+    constexpr int kKeys = 32 * kTiles;
+    constexpr int kLoads = D / 64;              // of 16 elements of a key
+    constexpr int kSteps = D / 32;              // matrix instructions over the head dimension
+    constexpr int kPer = D / 16;                // elements of a value row that a lane reads
+    constexpr int kWords = kPer / 4;
+    constexpr int kGroups = WHOLE ? 1 : 2 * kTiles;     // keys of a step that lie on one page for sure: 16 on small ones
+    constexpr int kGroupKeys = kKeys / kGroups;
+    const PagedArgs &a = b.p;
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quarter = lane >> 4;
+    const int head_tiles = (a.h.group + kPagedHeads - 1) / kPagedHeads;
+    const int units = a.h.kv_heads * head_tiles;
+    const int shift = b.cache.page_shift, mask = b.cache.page_size - 1;
+    const int64_t capacity = min((int64_t)a.max_pages << shift, (int64_t)1 << 30);
+    auto context_of = [&](int seq) { return (int)min((int64_t)max(gconst<int32_t>(a.lens)[seq], 0), capacity); };
+    auto keys_of = [&](int len) { return LISTED ? (int)min((int64_t)((len + mask) >> shift), (int64_t)b.count) << shift : len; };
+    auto parts_of = [&](int keys) { return max(min((keys + a.split_keys - 1) / a.split_keys, a.n_splits), 1); };    // a context of no keys has an empty one
+    __shared__ int lds_upto[MANY ? kMostListed : 1];        // parts of the sequences up to each
+    int64_t items = gridDim.x;
+    if constexpr (MANY) {
+        if (wave == 0) {
+            int upto = 0;
+            for (int base = 0; base < a.n_seqs; base += 64) {
+                int here = base + lane < a.n_seqs ? parts_of(keys_of(context_of(base + lane))) : 0;
+#pragma unroll
+                for (int d = 1; d < 64; d <<= 1) {
+                    const int below = __shfl_up(here, d);
+                    if (lane >= d) here += below;
+                }
+                if (base + lane < a.n_seqs) lds_upto[base + lane] = upto + here;
+                upto += __builtin_amdgcn_readlane(here, 63);
+            }
+        }
+        __syncthreads();
+        items = (int64_t)lds_upto[a.n_seqs - 1] * units;
+    }
+    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const int unit = (int)(item % units), rest = (int)(item / units);
+        const int kv_head = unit / head_tiles, head0 = (unit % head_tiles) * kPagedHeads;
+        int seq = rest % a.n_seqs, split = rest / a.n_seqs;
+        if constexpr (MANY) {
+            int most = a.n_seqs - 1;        // the first sequence with more parts up to it than `rest`
+            for (seq = 0; seq < most;) {
+                const int middle = (seq + most) >> 1;
+                if (lds_upto[middle] > rest) most = middle;
+                else seq = middle + 1;
+            }
+            seq = __builtin_amdgcn_readfirstlane(seq);
+            split = __builtin_amdgcn_readfirstlane(rest - (seq > 0 ? lds_upto[seq - 1] : 0));
+            __syncthreads();                // LDS of the part before is free
+        }
+        const int heads = min(a.h.group - head0, kPagedHeads);
+
+        const int len = context_of(seq), keys = keys_of(len);
+        const int begin = (int)min((int64_t)split * a.split_keys, (int64_t)keys);
+        const int end = split == a.n_splits - 1 ? keys : min(keys, begin + a.split_keys);
+        const int parts = parts_of(keys);
+        if (!MANY && split >= parts) return;
+
+        float m = kNoMax, l = 0.0f;
+        f32x4 o[kPer];
+#pragma unroll
+        for (int d = 0; d < kPer; ++d) o[d] = (f32x4){0, 0, 0, 0};
+
+        if (begin < end) {
+            u32x4 q[kSteps];        // in the order of a lane's elements of K: 16 of them for two instructions
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+                    q[2 * i + t] = *gconst<u32x4>(a.q.data + (int64_t)seq * a.q.token + (kv_head * a.h.group + head0 + min(col, heads - 1)) * a.q.head + i * 128 + quarter * 32 + t * 16);
+
+            const float c = a.h.scale_log2;
+            // all of these are read by scalar loads
+            const CF_CONST int32_t *table = (const CF_CONST int32_t *)a.table + seq * a.table_stride;
+            const CF_CONST int32_t *list = LISTED ? (const CF_CONST int32_t *)b.blocks + ((int64_t)seq * a.h.kv_heads + kv_head) * b.count : nullptr;
+            const CF_CONST float *k_scale = (const CF_CONST float *)b.cache.k_scale + kv_head, *v_scale = (const CF_CONST float *)b.cache.v_scale + kv_head;
+            const int64_t head_bytes = (int64_t)kv_head * b.cache.page_size * D;
+            const char *k_head = b.cache.k + head_bytes, *v_head = b.cache.v + head_bytes;
+            const int last = end - 1, held = (len + mask) >> shift;
+
+            // Where a step's groups of keys are, their scales, and how many of the keys are there.  Groups past the end are read on its last page, and not used.
+            struct Step {
+                int64_t at[kGroups];
+                float k[kGroups], v[kGroups];
+                int there[kGroups];
+            };
+            auto find = [&](int key0) {
+                Step s;
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g) {
+                    const int key = key0 + g * kGroupKeys, off = key & mask;
+                    int block = min(key, last) >> shift;
+                    s.there[g] = end - key;
+                    if constexpr (LISTED) {
+                        const int listed = list[block];
+                        block = min(max(listed, 0), held - 1);
+                        s.there[g] = listed == block && key < end ? len - (block << shift) - off : 0;
+                    }
+                    const int64_t page = min(max(table[block], 0), b.cache.n_pages - 1);
+                    s.at[g] = page * b.cache.page_bytes + off * D;
+                    s.k[g] = k_scale[page * a.h.kv_heads];
+                    s.v[g] = v_scale[page * a.h.kv_heads];
+                }
+                return s;
+            };
+            // of the two groups of a tile the second one, if so said; whole tiles have one
+            auto group_at = [](const auto &x, int g, bool second) {
+                const auto low = x[WHOLE ? 0 : 2 * g], high = x[WHOLE ? 0 : 2 * g + 1];
+                return second ? high : low;
+            };
+            u32x4 k[kTiles][2][kLoads];
+            auto load_k = [&](const Step &s) {
+#pragma unroll
+                for (int g = 0; g < kTiles; ++g)
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        const int x = 8 * (col >> 2) + 4 * t + (col & 3);
+                        const char *src = WHOLE ? k_head + s.at[0] + (32 * g + x) * D + quarter * 16 : k_head + group_at(s.at, g, x >= 16) + (x & 15) * D + quarter * 16;
+#pragma unroll
+                        for (int i = 0; i < kLoads; ++i) k[g][t][i] = *gconst<u32x4>(src + i * 64);
+                    }
+            };
+            uint32_t v[kTiles][8][kWords];
+            auto load_v = [&](const Step &s) {
+#pragma unroll
+                for (int g = 0; g < kTiles; ++g)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const int x = 8 * quarter + j;
+                        const char *src = WHOLE ? v_head + s.at[0] + (32 * g + x) * D + col * kPer : v_head + group_at(s.at, g, x >= 16) + (x & 15) * D + col * kPer;
+                        if constexpr (kWords == 1) v[g][j][0] = *gconst<uint32_t>(src);
+                        else if constexpr (kWords == 2) {
+                            const u32x2 y = *gconst<u32x2>(src);
+                            v[g][j][0] = y[0], v[g][j][1] = y[1];
+                        } else {
+                            const u32x4 y = *gconst<u32x4>(src);
+#pragma unroll
+                            for (int w = 0; w < 4; ++w) v[g][j][w] = y[w];
+                        }
+                    }
+            };
+            auto most_of = [&](const Step &s, int g) { return WHOLE ? s.there[0] - 32 * g - 8 * quarter : group_at(s.there, g, quarter >= 2) - 8 * (quarter & 1); };    // of a lane's 8 keys
+
+            // K of the next step is asked for as soon as this one's is used up, V of this one before that.
+            int key0 = begin + wave * kKeys;
+            Step at = find(key0);
+            if (key0 < end) load_k(at);
+            while (key0 < end) {
+                const int next0 = key0 + kWaves * kKeys;
+                const Step next = find(next0);
+                load_v(at);
+                __builtin_amdgcn_sched_barrier(0);
+                f32x4 s[kTiles][2];
+#pragma unroll
+                for (int g = 0; g < kTiles; ++g) {
+                    const float scale = group_at(at.k, g, col >= 8);
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        s[g][t] = (f32x4){0, 0, 0, 0};
+#pragma unroll
+                        for (int i = 0; i < kLoads; ++i) {
+                            const u32x4 x = k[g][t][i];
+                            s[g][t] = E::mfma16((u32x4){C::template pair<false>(x[0], scale), C::template pair<true>(x[0], scale), C::template pair<false>(x[1], scale), C::template pair<true>(x[1], scale)}, q[2 * i], s[g][t]);
+                            s[g][t] = E::mfma16((u32x4){C::template pair<false>(x[2], scale), C::template pair<true>(x[2], scale), C::template pair<false>(x[3], scale), C::template pair<true>(x[3], scale)}, q[2 * i + 1], s[g][t]);
+                        }
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                if (next0 < end) load_k(next);
+                __builtin_amdgcn_sched_barrier(0);
+                float top = -__builtin_inff();
+                bool whole = true;          // whether all of the step's keys are there
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g) whole &= at.there[g] >= kGroupKeys;
+#pragma unroll
+                for (int g = 0; g < kTiles; ++g) {
+                    const int most = most_of(at, g);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        if (!whole && j >= most) s[g][j >> 2][j & 3] = -__builtin_inff();
+                        top = fmaxf(top, s[g][j >> 2][j & 3]);
+                    }
+                }
+                top *= c;
+                bool moves = __any(top > m + E::kMostOver);
+                if constexpr (E::kFollow) {     // a row's four lanes: has one of them a key that is near enough?
+                    uint64_t near = __ballot(!(top < m + kLeastOver));
+                    near |= near >> 32;
+                    near |= near >> 16;
+                    if ((near & 0xffff) != 0xffff) {
+                        const float row_top = max_quarters(max_halves(top));
+                        moves |= __any(row_top < m + kLeastOver && row_top > -__builtin_inff() && max_quarters(max_halves(l)) < kFullTotal);
+                    }
+                }
+                if (moves) {
+                    const float fresh = reference<DT>(m, max_quarters(max_halves(top)), true, E::kFollow ? max_quarters(max_halves(l)) : 0.0f), scale = exp2_fast(m - fresh);
+#pragma unroll
+                    for (int d = 0; d < kPer; ++d)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[d][i] *= scale;
+                    l *= scale;
+                    m = fresh;
+                }
+#pragma unroll
+                for (int g = 0; g < kTiles; ++g) {
+                    if (!whole) {           // what lies in places that are not there may be NaN: 0 times it is not 0
+                        const int most = most_of(at, g);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+#pragma unroll
+                            for (int w = 0; w < kWords; ++w) v[g][j][w] = j < most ? v[g][j][w] : 0u;
+                    }
+                    u32x4 p;        // scaled scores are rounded as their maximum was: of scores of any size the largest has the weight 1
+#pragma unroll
+                    for (int j = 0; j < 8; j += 2) {
+                        const float p0 = exp2_fast(s[g][j >> 2][j & 3] * c - m), p1 = exp2_fast(s[g][j >> 2][(j & 3) + 1] * c - m);
+                        l += p0 + p1;
+                        p[j >> 1] = E::pack(p0, p1);
+                    }
+                    const float scale = group_at(at.v, g, quarter >= 2);
+#pragma unroll
+                    for (int w = 0; w < kWords; ++w) {
+                        u32x4 x[4];         // elements 4w .. 4w + 3 of this lane's 8 keys
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const uint32_t low = __builtin_amdgcn_perm(v[g][2 * j + 1][w], v[g][2 * j][w], 0x05010400), high = __builtin_amdgcn_perm(v[g][2 * j + 1][w], v[g][2 * j][w], 0x07030602);
+                            x[0][j] = C::template pair<false>(low, scale);
+                            x[1][j] = C::template pair<true>(low, scale);
+                            x[2][j] = C::template pair<false>(high, scale);
+                            x[3][j] = C::template pair<true>(high, scale);
+                        }
+#pragma unroll
+                        for (int d = 0; d < 4; ++d) o[4 * w + d] = E::mfma16(x[d], p, o[4 * w + d]);
+                    }
+                }
+                key0 = next0;
+                at = next;
+            }
+            l = sum_quarters(sum_halves(l));
+        }
+
+        join_waves<D>(m, l, o, lane, wave);
+        if (!finish_part<DT, D, MANY>(a, seq, unit, units, kv_head, head0, split, parts, lane, wave, m, l, o)) return;
+    }
+}
+
+template <int DT, int D, bool MANY> hipError_t paged8_over(const Paged8Args &a, hipStream_t s)
+{
+    const int64_t n = paged8_workgroups(a);
+    const bool whole = a.cache.page_size >= (D == 256 ? 32 : 64);
+    if (a.blocks) return whole ? enqueue(k_attn_paged8<DT, D, MANY, true, true>, n, s, a) : enqueue(k_attn_paged8<DT, D, MANY, true, false>, n, s, a);
+    return whole ? enqueue(k_attn_paged8<DT, D, MANY, false, true>, n, s, a) : enqueue(k_attn_paged8<DT, D, MANY, false, false>, n, s, a);
+}
+
+template <int DT, int D> hipError_t paged8_dim(const Paged8Args &a, hipStream_t s) { return a.p.many ? paged8_over<DT, D, true>(a, s) : paged8_over<DT, D, false>(a, s); }
+
+template <int DT> hipError_t paged8_typed(const Paged8Args &a, hipStream_t s)
+{
+    switch (a.p.h.head_dim) {
+    case 64: return paged8_dim<DT, 64>(a, s);
+    case 128: return paged8_dim<DT, 128>(a, s);
+    default: return paged8_dim<DT, 256>(a, s);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_paged8(const Paged8Args &a, hipStream_t s) { return a.p.h.dtype == BF16 ? paged8_typed<BF16>(a, s) : paged8_typed<F16>(a, s); }
+
+}  // namespace attn
+}  // namespace cf
