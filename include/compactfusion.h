@@ -450,7 +450,7 @@ cf_status cf_attn_join(const cf_attn_desc *desc, const cf_join *args, void *stre
  * Codes.  An element is code x scale, rounded once: codes are 8-bit floats of 4 exponent and 3 mantissa bits (OCP e4m3: largest 448,
  * least 2^-9, no infinities), the scale is one for all keys (values) of a head on a page, and a power of two from 2^-100 to 2^119: the least that
  * brings the largest magnitude to 448 at most.  Magnitudes, infinite ones among them, are 448 x 2^119 (bf16) or 240 x 2^8 (fp16) at most, the
- * largest codes that the type holds; NaN stays NaN, and counts as 0 in scales and bounds. */
+ * largest codes that the type holds; NaN stays NaN, and is left out of scales and bounds (those of nothing else are the least scale, and 0). */
 
 /* Codes and scales in pages: code i of head h of slot s is k[(s / page_size) * page_stride + (h * page_size + s % page_size) * head_dim + i],
  * its scale k_scale[(s / page_size) * kv_heads + h]. */

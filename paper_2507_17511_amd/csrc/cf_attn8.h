@@ -31,8 +31,9 @@ struct Append8Args {
     const float *cos, *sin;
     int64_t n_tokens;
     int32_t n_positions, rotary_dim, interleaved;
-    int32_t chunk;                  // tokens whose pages a wave takes
-    int32_t page_groups;            // workgroups that store keys and values; those behind them rotate queries
+    int32_t chunk;                  // tokens whose pages a workgroup takes, 64 at most
+    int32_t chunks_each;            // that an XCD has
+    int32_t page_groups;            // workgroups that store keys and values, a multiple of kXcds; those behind them rotate queries
 };
 
 struct SelectArgs {
@@ -63,7 +64,9 @@ struct PlanArgs {
     int32_t workgroups;
 };
 
+constexpr int kXcds = 8;             // which take the workgroups in turn
 constexpr int kSelectPages = 64;    // that a workgroup of the scores takes
+constexpr int kAppendThreads = 256, kAppendTurns = 2;    // a lane rotates so many queries' parts
 constexpr int kPlanThreads = 1024;
 
 inline int64_t paged8_workgroups(const Paged8Args &a)
@@ -72,10 +75,7 @@ inline int64_t paged8_workgroups(const Paged8Args &a)
     return a.p.many && held < items ? held : items;
 }
 
-inline int64_t append8_workgroups(const Append8Args &a)
-{
-    return a.page_groups + (a.q.data ? (a.n_tokens * a.h.q_heads * (a.h.head_dim / 16) + 255) / 256 : 0);
-}
+inline int64_t append8_workgroups(const Append8Args &a) { return a.page_groups + (a.q.data ? (a.n_tokens * a.h.q_heads * (a.h.head_dim / 16) + kAppendThreads * kAppendTurns - 1) / (kAppendThreads * kAppendTurns) : 0); }
 
 hipError_t launch_paged8(const Paged8Args &a, hipStream_t s);
 hipError_t launch_append8(const Append8Args &a, hipStream_t s);

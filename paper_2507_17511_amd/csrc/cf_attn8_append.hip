@@ -1,310 +1,440 @@
 // Keys and values into the paged cache of 8-bit codes, rotated on the way, and the queries' rotation.
 //
 // What a call's tokens bring to one page is one piece of work for each head of keys and of values: their largest magnitude decides the scale.  Such
-// tokens are neighbours in the call, so that a wave finds where they begin by looking at the slots alone: WAVES waves take the pages that begin among
-// `chunk` tokens, read their rows once (up to kKeep rounds of them stay in registers), agree on the scale, and store the codes.  Everything is read and
-// written once, and the call is bound by HBM, or by its launch where it is small.
+// tokens are neighbours in the call, so that a workgroup finds where they begin by looking at the slots alone.  It takes the pages that begin among `chunk` tokens: lone
+// tokens, one of a page, as a step of generation brings them, for four heads, a wave each, as many at a time as a wave has room for their rows; neighbours on a page for one head, or
+// as many as its four waves have room for.  They read the rows twice, once for the scale and once for the codes, the second time from the caches.  To keep them in registers
+// instead took so many that few waves were there to wait for memory (16384 tokens, 8 heads of 128, no queries: 83 us for 41).
 #include "cf_attn8_device.h"
 
 namespace cf {
 namespace attn {
 namespace {
 
-constexpr int kKeep = 4;        // rounds of rows that wait in registers for their scale
+constexpr int kWaves = kAppendThreads / 64;
 
-// 16 elements of a row: two vectors of 8, which hold the two halves of 8 pairs where pairs lie rotary_dim / 2 apart.
+// 16 elements of a row: two vectors of 8, which hold the two halves of 8 pairs where pairs lie rotary_dim / 2 apart (or, PAIRS, side by side).
 struct Place {
     int first, second;
-    bool apart, rotated;
+    bool rotated;
 };
-__device__ __forceinline__ Place place_of(int lane, int half, bool interleaved)
+template <bool PAIRS> __device__ __forceinline__ Place place_of(int lane, int half)
 {
     Place p;
     const int lanes = half >> 3;
     p.rotated = lane < lanes;
-    p.apart = p.rotated && !interleaved;
-    p.first = p.apart ? lane : 2 * lane;
-    p.second = p.apart ? lane + lanes : p.first + 1;
+    p.first = !PAIRS && p.rotated ? lane : 2 * lane;
+    p.second = !PAIRS && p.rotated ? lane + lanes : p.first + 1;
     return p;
 }
 
-template <int DT> __device__ __forceinline__ void turn(u32x4 x, u32x4 y, const Place &p, const float *cos, const float *sin, float (&r)[16])
+struct Elements {
+    float x[16];
+};
+struct Angles {
+    f32x4 c[2], s[2];
+};
+struct Raw {
+    u32x4 x, y;
+};
+
+// A lane's part of a position's row of cosines and sines.
+__device__ __forceinline__ Angles angles_of(const Append8Args &a, int pos, int half, int lane)
 {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        r[2 * k] = Elem<DT>::lo(x[k]), r[2 * k + 1] = Elem<DT>::hi(x[k]);
-        r[8 + 2 * k] = Elem<DT>::lo(y[k]), r[8 + 2 * k + 1] = Elem<DT>::hi(y[k]);
-    }
-    if (!p.rotated) return;
-    const CF_GLOBAL f32x4 *c = gconst<f32x4>(cos), *s = gconst<f32x4>(sin);
-    const f32x4 cs[2] = {c[0], c[1]}, sn[2] = {s[0], s[1]};
-    if (p.apart) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const float a = r[k], b = r[8 + k], co = cs[k >> 2][k & 3], si = sn[k >> 2][k & 3];
-            r[k] = a * co - b * si;
-            r[8 + k] = b * co + a * si;
-        }
-    } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const float a = r[2 * k], b = r[2 * k + 1], co = cs[k >> 2][k & 3], si = sn[k >> 2][k & 3];
-            r[2 * k] = a * co - b * si;
-            r[2 * k + 1] = b * co + a * si;
-        }
-    }
+    const CF_GLOBAL f32x4 *c = gconst<f32x4>(a.cos + (int64_t)pos * half + lane * 8), *s = gconst<f32x4>(a.sin + (int64_t)pos * half + lane * 8);
+    return {{c[0], c[1]}, {s[0], s[1]}};
 }
 
-template <int DT, int D> __device__ __forceinline__ void rotate_queries(const Append8Args &a, int64_t id)
+template <int DT, bool PAIRS> __device__ __forceinline__ Elements turn(const Raw &in, const Angles &g, bool rotated)
+{
+    Elements r;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        r.x[2 * k] = Elem<DT>::lo(in.x[k]), r.x[2 * k + 1] = Elem<DT>::hi(in.x[k]);
+        r.x[8 + 2 * k] = Elem<DT>::lo(in.y[k]), r.x[8 + 2 * k + 1] = Elem<DT>::hi(in.y[k]);
+    }
+    if (rotated) {
+        if constexpr (!PAIRS) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float a = r.x[k], b = r.x[8 + k], co = g.c[k >> 2][k & 3], si = g.s[k >> 2][k & 3];
+                r.x[k] = a * co - b * si;
+                r.x[8 + k] = b * co + a * si;
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float a = r.x[2 * k], b = r.x[2 * k + 1], co = g.c[k >> 2][k & 3], si = g.s[k >> 2][k & 3];
+                r.x[2 * k] = a * co - b * si;
+                r.x[2 * k + 1] = b * co + a * si;
+            }
+        }
+    }
+    return r;
+}
+
+constexpr int kTurns = kAppendTurns;
+
+template <int DT, int D, bool PAIRS> __device__ __forceinline__ void rotate_queries(const Append8Args &a, uint32_t group)
 {
     constexpr int kLanes = D / 16;
-    const int64_t token = id / (a.h.q_heads * kLanes);
-    if (token >= a.n_tokens) return;
-    const int rest = (int)(id - token * (a.h.q_heads * kLanes)), lane = rest % kLanes, head = rest / kLanes, half = a.rotary_dim >> 1;
-    int pos = 0;
-    if (half) {
-        pos = gconst<int32_t>(a.positions)[token];
-        if (pos < 0 || pos >= a.n_positions) return;
-    }
-    const Place p = place_of(lane, half, a.interleaved);
-    const CF_GLOBAL u32x4 *src = gconst<u32x4>(a.q.data + token * a.q.token + head * a.q.head);
-    float r[16];
-    const int64_t at = (int64_t)pos * half + lane * 8;
-    turn<DT>(src[p.first], src[p.second], p, a.cos + at, a.sin + at, r);
-    CF_GLOBAL u32x4 *dst = gmut<u32x4>(a.q_out.data + token * a.q_out.token + head * a.q_out.head);
-    u32x4 u, w;
+    const uint32_t of_token = a.h.q_heads * kLanes;
+    const int half = a.rotary_dim >> 1;
+    const CF_GLOBAL u32x4 *src[kTurns];
+    CF_GLOBAL u32x4 *dst[kTurns];
+    Raw raw[kTurns];
+    Angles angles[kTurns];
+    Place place[kTurns];
+    bool there[kTurns];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        u[k] = Elem<DT>::pack(r[2 * k], r[2 * k + 1]);
-        w[k] = Elem<DT>::pack(r[8 + 2 * k], r[8 + 2 * k + 1]);
+    for (int i = 0; i < kTurns; ++i) {
+        const uint32_t id = (group * kTurns + i) * (kWaves * 64) + threadIdx.x;       // a launch counts fewer than 2^32 work-items, a half of these
+        const int64_t token = id / of_token;
+        const uint32_t rest = id % of_token, lane = rest % kLanes, head = rest / kLanes;
+        int pos = 0;
+        there[i] = token < a.n_tokens;
+        if (there[i] && half) {
+            pos = gconst<int32_t>(a.positions)[token];
+            there[i] = pos >= 0 && pos < a.n_positions;
+        }
+        place[i] = place_of<PAIRS>(lane, half);
+        src[i] = gconst<u32x4>(a.q.data + token * a.q.token + head * a.q.head);
+        dst[i] = gmut<u32x4>(a.q_out.data + token * a.q_out.token + head * a.q_out.head);
+        if (!there[i]) continue;
+        raw[i] = {src[i][place[i].first], src[i][place[i].second]};
+        if (place[i].rotated) angles[i] = angles_of(a, pos, half, lane);
     }
-    dst[p.first] = u;
-    dst[p.second] = w;
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+        if (!there[i]) continue;
+        const Elements r = turn<DT, PAIRS>(raw[i], angles[i], place[i].rotated);
+        u32x4 u, w;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            u[k] = Elem<DT>::pack(r.x[2 * k], r.x[2 * k + 1]);
+            w[k] = Elem<DT>::pack(r.x[8 + 2 * k], r.x[8 + 2 * k + 1]);
+        }
+        dst[i][place[i].first] = u;
+        dst[i][place[i].second] = w;
+    }
 }
 
-template <int DT, int D, int WAVES> __global__ __launch_bounds__(256) void k_kv_append8(Append8Args a)
+template <bool LARGEST> __device__ __forceinline__ float extreme(float a, float b) { return LARGEST ? fmaxf(a, b) : fminf(a, b); }
+template <int CONTROL> __device__ __forceinline__ float dpp(float x) { return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CONTROL, 0xf, 0xf, false)); }
+
+// Over the lanes of sixteen that hold the same elements, every LANES-th one.  NaN yields to a number.
+template <bool LARGEST, int LANES> __device__ __forceinline__ float over_sixteen(float x)
+{
+    if constexpr (LANES <= 4) x = extreme<LARGEST>(x, dpp<0x124>(x));       // 4 lanes on
+    if constexpr (LANES <= 8) x = extreme<LARGEST>(x, dpp<0x128>(x));       // 8
+    return x;
+}
+// Of x and the lane 32 (16) away in the lower half (the even sixteens), of y in the other.
+template <bool LARGEST> __device__ __forceinline__ float of_halves(float x, float y)
+{
+    const u32x2 r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y), false, false));
+    return extreme<LARGEST>(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+template <bool LARGEST> __device__ __forceinline__ float of_quarters(float x, float y)
+{
+    const u32x2 r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(y), false, false));
+    return extreme<LARGEST>(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+// The largest of LANES neighbouring lanes.
+template <int LANES> __device__ __forceinline__ float over_lanes(float x)
+{
+    x = fmaxf(x, dpp<0xb1>(x));                                 // of pairs
+    x = fmaxf(x, dpp<0x4e>(x));                                 // of fours
+    if constexpr (LANES >= 8) x = fmaxf(x, dpp<0x141>(x));      // eight lanes turned round
+    if constexpr (LANES >= 16) x = fmaxf(x, dpp<0x140>(x));     // sixteen
+    return x;
+}
+
+template <int DT> __device__ __forceinline__ float within(float x) { return x > Code<DT>::kMost ? Code<DT>::kMost : x < -Code<DT>::kMost ? -Code<DT>::kMost : x; }      // NaN stays
+
+// Codes of 8 neighbouring elements.
+__device__ __forceinline__ u32x2 encode8(const float *x, float by)
+{
+    return {encode4(x[0] * by, x[1] * by, x[2] * by, x[3] * by), encode4(x[4] * by, x[5] * by, x[6] * by, x[7] * by)};
+}
+
+// Codes of a head's page go by a new scale, 2^by times as large.  `step` lanes share them; places of this call are written behind them.
+__device__ __forceinline__ void rescale(char *codes, int bytes, int by, int lane, int step)
+{
+    const float f = power_of_two(max(by, -126));
+    for (int i = lane * 16; i < bytes; i += step * 16) {
+        u32x4 w = *gconst<u32x4>(codes + i);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const auto low = __builtin_amdgcn_cvt_pk_f32_fp8(w[k], false), high = __builtin_amdgcn_cvt_pk_f32_fp8(w[k], true);
+            w[k] = encode4(low[0] * f, low[1] * f, high[0] * f, high[1] * f);
+        }
+        *gmut<u32x4>(codes + i) = w;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+}
+
+struct Where {
+    int off, pos;               // off < 0: not there, or left out
+};
+__device__ __forceinline__ Where where_is(const Append8Args &a, int64_t token)
+{
+    Where w = {-1, 0};
+    if (a.rotary_dim) w.pos = gconst<int32_t>(a.positions)[token];
+    const int off = (int)(gconst<int64_t>(a.slots)[token] & (a.cache.page_size - 1));
+    if (!a.rotary_dim || (w.pos >= 0 && w.pos < a.n_positions)) w.off = off;
+    else w.pos = 0;
+    return w;
+}
+
+// What a row of work is about: one head of keys or of values.
+struct Row {
+    const char *data;           // of token 0
+    int64_t token;
+    char *codes;                // of page 0
+    float *scale;               // of page 0
+    uint16_t *bounds;           // of page 0, or null
+    bool rotated;
+};
+template <int D> __device__ __forceinline__ Row row_of(const Append8Args &a, int row)
+{
+    const bool value = row >= a.h.kv_heads;
+    const int head = value ? row - a.h.kv_heads : row;
+    const Rows &in = value ? a.v : a.k;
+    return {in.data + head * in.head, in.token, (value ? a.cache.v : a.cache.k) + (int64_t)head * a.cache.page_size * D, (value ? a.cache.v_scale : a.cache.k_scale) + head,
+            value || !a.cache.bounds ? nullptr : a.cache.bounds + (int64_t)head * 2 * D, !value && a.rotary_dim > 0};
+}
+
+// A token that is the only one of its page, for every LANES lanes: `there` says so.
+template <int DT, int D, bool PAIRS> __device__ __forceinline__ void store_lone(const Append8Args &a, const Row &row, int64_t token, int page, bool there, int lane)
+{
+    constexpr int kLanes = D / 16;
+    const int row_lane = lane % kLanes;
+    if (!there) return;
+    const Where where = where_is(a, token);
+    if (where.off < 0) return;
+    const Place place = place_of<PAIRS>(row_lane, row.rotated ? a.rotary_dim >> 1 : 0);
+    const CF_GLOBAL u32x4 *src = gconst<u32x4>(row.data + token * row.token);
+    const Raw raw = {src[place.first], src[place.second]};
+    Angles angles;
+    if (place.rotated) angles = angles_of(a, where.pos, a.rotary_dim >> 1, row_lane);
+    float *scale_at = row.scale + (int64_t)page * a.h.kv_heads;
+    const float scale_was = *gconst<float>(scale_at);
+    uint16_t *bounds = row.bounds ? row.bounds + (int64_t)page * a.h.kv_heads * 2 * D : nullptr;
+    const bool begins = where.off == 0;
+    u32x4 was[2][2] = {};
+    if (bounds && !begins) {
+#pragma unroll
+        for (int v = 0; v < 2; ++v)
+#pragma unroll
+            for (int high = 0; high < 2; ++high) was[v][high] = gconst<u32x4>(bounds + high * D)[v ? place.second : place.first];
+    }
+    Elements r = turn<DT, PAIRS>(raw, angles, place.rotated);
+    float most = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) most = fmaxf(most, fabsf(r.x[k]));
+    most = over_lanes<kLanes>(most);
+    if (most > Code<DT>::kMost) {
+        most = Code<DT>::kMost;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) r.x[k] = within<DT>(r.x[k]);
+    }
+    const int before = begins ? kLeastExponent : exponent_of(scale_was), e = max(exponent_for(most), before);
+    char *codes = row.codes + page * a.cache.page_bytes;
+    if (!begins && e > before) rescale(codes, a.cache.page_size * D, before - e, row_lane, kLanes);
+    const float by = power_of_two(-e), scale = power_of_two(e);
+    if (row_lane == 0) *gmut<float>(scale_at) = scale;
+#pragma unroll
+    for (int v = 0; v < 2; ++v) {
+        const int at = v ? place.second : place.first;
+        const u32x2 c = encode8(r.x + 8 * v, by);
+        *gmut<u32x2>(codes + where.off * D + at * 8) = c;
+        if (!bounds) continue;
+        u32x4 least, largest;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const auto y = k & 1 ? __builtin_amdgcn_cvt_pk_f32_fp8(c[k >> 1], true) : __builtin_amdgcn_cvt_pk_f32_fp8(c[k >> 1], false);
+            float low[2], high[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                low[j] = high[j] = y[j] == y[j] ? y[j] * scale : 0.0f;
+                if (begins) continue;
+                const float old_low = j ? Elem<BF16>::hi(was[v][0][k]) : Elem<BF16>::lo(was[v][0][k]), old_high = j ? Elem<BF16>::hi(was[v][1][k]) : Elem<BF16>::lo(was[v][1][k]);
+                low[j] = y[j] == y[j] ? fminf(low[j], old_low) : old_low;
+                high[j] = y[j] == y[j] ? fmaxf(high[j], old_high) : old_high;
+            }
+            least[k] = Elem<BF16>::pack(low[0], low[1]);
+            largest[k] = Elem<BF16>::pack(high[0], high[1]);
+        }
+        gmut<u32x4>(bounds)[at] = least;
+        gmut<u32x4>(bounds + D)[at] = largest;
+    }
+}
+
+struct Shared {
+    float most[kWaves];
+    bool begins[kWaves];
+    float bounds[kWaves][512];      // [least, largest][D]
+};
+
+// Tokens first .. first + n - 1, two at least, go to one page: a row of them, by `waves` of the workgroup's from wave0 on.  A wave without a row has no tokens.
+template <int DT, int D, bool PAIRS>
+__device__ __forceinline__ void store_neighbours(const Append8Args &a, Shared &lds, const Row &row, int64_t first, int n, int page, int lane, int wave, int wave0, int waves)
 {
     constexpr int kLanes = D / 16;              // of a row
     constexpr int kTokens = 64 / kLanes;        // of a wave's round
-    constexpr int kRound = kTokens * WAVES;
-    if (blockIdx.x >= (unsigned)a.page_groups) return rotate_queries<DT, D>(a, (int64_t)(blockIdx.x - a.page_groups) * 256 + threadIdx.x);
-    __shared__ float lds_most[WAVES > 1 ? WAVES : 1];
-    __shared__ bool lds_begins[WAVES > 1 ? WAVES : 1];
-    __shared__ float lds_bounds[WAVES > 1 ? WAVES : 1][kLanes][32];
+    const int round = kTokens * waves;
+    const int row_lane = lane % kLanes, half = a.rotary_dim >> 1;
+    const int mine = (wave - wave0) * kTokens + lane / kLanes;        // a lane's row of a round
+    const Place place = place_of<PAIRS>(row_lane, row.rotated ? half : 0);
+    auto elements = [&](int i, const Where &w) {
+        const CF_GLOBAL u32x4 *src = gconst<u32x4>(row.data + (first + i) * row.token);
+        const Raw raw = {src[place.first], src[place.second]};
+        Angles angles;
+        if (place.rotated) angles = angles_of(a, w.pos, half, row_lane);
+        return turn<DT, PAIRS>(raw, angles, place.rotated);
+    };
+    float *scale_at = row.scale + (int64_t)page * a.h.kv_heads;
+    const float scale_was = *gconst<float>(scale_at);
+    float most = -1.0f;                         // of no token
+    bool begins = false;
+#pragma unroll 2
+    for (int i = mine; i < n; i += round) {
+        const Where w = where_is(a, first + i);
+        if (w.off < 0) continue;
+        const Elements r = elements(i, w);
+        most = fmaxf(most, 0.0f);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) most = fmaxf(most, fabsf(r.x[k]));
+        begins |= w.off == 0;
+    }
+    most = max_quarters(max_halves(over_lanes<16>(most)));
+    begins = __any(begins);
+    if (lane == 0) lds.most[wave] = most, lds.begins[wave] = begins;
+    __syncthreads();                            // and every wave has read the scale
+    for (int w = wave0; w < wave0 + waves; ++w) most = fmaxf(most, lds.most[w]), begins |= lds.begins[w];
 
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row_lane = lane % kLanes;
-    const int share = WAVES > 1 ? wave : 0;     // of a page's rows
-    const int64_t item = WAVES > 1 ? blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
-    const int rows = 2 * a.h.kv_heads, head = (int)(item % rows) % a.h.kv_heads;
-    const bool value = (int)(item % rows) >= a.h.kv_heads;
-    const int64_t begin = item / rows * a.chunk;
-    if (begin >= a.n_tokens) return;            // the whole workgroup, where its waves share pages
+    const bool some = most >= 0.0f;             // not all of the page's tokens are left out
+    const bool limited = most > Code<DT>::kMost;
+    const int before = begins ? kLeastExponent : exponent_of(scale_was), e = max(exponent_for(fminf(most, Code<DT>::kMost)), before);
+    char *codes = row.codes + page * a.cache.page_bytes;
+    if (some && !begins && e > before) rescale(codes, a.cache.page_size * D, before - e, (wave - wave0) * 64 + lane, waves * 64);
+    __syncthreads();
 
-    const int half = a.rotary_dim >> 1;
-    const Place place = place_of(row_lane, value ? 0 : half, a.interleaved);
-    const Rows &in = value ? a.v : a.k;
+    // Rounding keeps the order: the bounds are the codes of the least and the largest element.
+    const float by = power_of_two(-e), scale = power_of_two(e);
+    float least[16], largest[16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) least[k] = __builtin_inff(), largest[k] = -__builtin_inff();
+#pragma unroll 2
+    for (int i = mine; i < n; i += round) {
+        const Where w = where_is(a, first + i);
+        if (w.off < 0) continue;
+        Elements r = elements(i, w);
+        if (limited)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) r.x[k] = within<DT>(r.x[k]);
+        if (row.bounds)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) least[k] = fminf(least[k], r.x[k]), largest[k] = fmaxf(largest[k], r.x[k]);
+        *gmut<u32x2>(codes + w.off * D + place.first * 8) = encode8(r.x, by);
+        *gmut<u32x2>(codes + w.off * D + place.second * 8) = encode8(r.x + 8, by);
+    }
+    if (some && wave == wave0 && lane == 0) *gmut<float>(scale_at) = scale;
+
+    if (row.bounds) {           // every exchange halves what a lane has: 8 of the 32, 4 of the least and 4 of the largest ones
+#pragma unroll
+        for (int k = 0; k < 8; ++k) least[k] = of_halves<false>(least[k], least[k + 8]), largest[k] = of_halves<true>(largest[k], largest[k + 8]);
+        f32x4 low, high;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            low[k] = over_sixteen<false, kLanes>(of_quarters<false>(least[k], least[k + 4]));
+            high[k] = over_sixteen<true, kLanes>(of_quarters<true>(largest[k], largest[k + 4]));
+        }
+        const int at = (lane < 32 ? place.first : place.second) * 8 + (lane & 16) / 4;
+        if (lane % 16 < kLanes) *(f32x4 *)&lds.bounds[wave][at] = low, *(f32x4 *)&lds.bounds[wave][D + at] = high;
+    }
+    __syncthreads();
+    if (row.bounds && some) {
+        uint16_t *bounds = row.bounds + (int64_t)page * a.h.kv_heads * 2 * D;
+        for (int i = (wave - wave0) * 64 + lane; i < D; i += waves * 64) {      // two neighbours of the 2 D numbers
+            const bool high = 2 * i >= D;
+            float x[2] = {lds.bounds[wave0][2 * i], lds.bounds[wave0][2 * i + 1]};
+            for (int w = wave0 + 1; w < wave0 + waves; ++w)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) x[k] = high ? fmaxf(x[k], lds.bounds[w][2 * i + k]) : fminf(x[k], lds.bounds[w][2 * i + k]);
+            const bool any[2] = {fabsf(x[0]) < __builtin_inff(), fabsf(x[1]) < __builtin_inff()};       // a channel may be all NaN
+            const auto y = __builtin_amdgcn_cvt_pk_f32_fp8(__builtin_amdgcn_cvt_pk_fp8_f32(any[0] ? x[0] * by : 0.0f, any[1] ? x[1] * by : 0.0f, 0, false), false);
+            float z[2] = {y[0] * scale, y[1] * scale};
+            CF_GLOBAL uint32_t *to = gmut<uint32_t>(bounds) + i;
+            if (!begins) {
+                const uint32_t was = *to;
+                const float old[2] = {Elem<BF16>::lo(was), Elem<BF16>::hi(was)};
+#pragma unroll
+                for (int k = 0; k < 2; ++k) z[k] = !any[k] ? old[k] : high ? fmaxf(z[k], old[k]) : fminf(z[k], old[k]);
+            }
+            *to = Elem<BF16>::pack(z[0], z[1]);
+        }
+    }
+    __syncthreads();                            // LDS is free
+}
+
+template <int DT, int D, bool PAIRS> __global__ __launch_bounds__(kWaves * 64, 5) void k_kv_append8(Append8Args a)
+{
+    constexpr int kLanes = D / 16, kTokens = 64 / kLanes;
+    if (blockIdx.x >= (unsigned)a.page_groups) return rotate_queries<DT, D, PAIRS>(a, blockIdx.x - a.page_groups);
+    __shared__ Shared lds;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // an XCD has neighbouring tokens: where pages begin every so many of them, each XCD has its share
+    const uint32_t xcd = blockIdx.x % kXcds, mine = blockIdx.x / kXcds;
+    const int rows = 2 * a.h.kv_heads, row_here = (int)(mine % (uint32_t)rows);
+    const int64_t begin = ((int64_t)xcd * a.chunks_each + mine / (uint32_t)rows) * a.chunk;
+
     const int64_t slots_end = (int64_t)a.cache.n_pages << a.cache.page_shift;
     auto page_of = [&](int64_t token) {         // -1: none
-        const int64_t slot = gconst<int64_t>(a.slots)[token];
+        const int64_t slot = token >= 0 && token < a.n_tokens ? gconst<int64_t>(a.slots)[token] : -1;
         return slot < 0 || slot >= slots_end ? -1 : (int)(slot >> a.cache.page_shift);
     };
-    uint64_t starts;
+    uint64_t lone, starts;      // of tokens whose page no neighbour shares; of those that begin neighbours on one page
+    int page;
     {
-        const int64_t token = begin + lane;
-        const int page = lane < a.chunk && token < a.n_tokens ? page_of(token) : -1;
-        starts = __ballot(page >= 0 && (token == 0 || page_of(token - 1) != page));
+        const bool there = lane < a.chunk;
+        page = there ? page_of(begin + lane) : -1;
+        const int before = there ? page_of(begin + lane - 1) : -1, behind = there ? page_of(begin + lane + 1) : -1;
+        lone = __ballot(page >= 0 && before != page && behind != page);
+        starts = __ballot(page >= 0 && before != page && behind == page);
+    }
+    if (lone && row_here % kWaves == 0 && row_here + wave < rows) {
+        const Row row = row_of<D>(a, row_here + wave);
+        for (int i = 0; i < a.chunk; i += kTokens) {
+            const int at = i + lane / kLanes;
+            const int mine = __shfl(page, at & 63);
+            store_lone<DT, D, PAIRS>(a, row, begin + at, mine, at < a.chunk && (lone >> at & 1), lane);
+        }
     }
     for (; starts != 0; starts &= starts - 1) {
-        const int64_t first = begin + __builtin_ctzll(starts);
-        const int page = __builtin_amdgcn_readfirstlane(page_of(first));
-        int64_t n = 0;                          // tokens that go to this page
+        const int at = __builtin_ctzll(starts);
+        const int64_t first = begin + at;
+        const int here = __builtin_amdgcn_readlane(page, at);
+        int n = 1;                              // tokens that go to this page
         for (;; n += 64) {
-            const int64_t token = first + n + lane;
-            const uint64_t others = __ballot(token >= a.n_tokens || page_of(token) != page);
+            const uint64_t others = __ballot(page_of(first + n + lane) != here);
             if (others) {
                 n += __builtin_ctzll(others);
                 break;
             }
         }
-
-        // Rows are read as they are, then rotated: all of the kept ones are on their way together.
-        u32x4 raw[kKeep][2];
-        int off[kKeep], pos[kKeep];             // off < 0: not there, or left out
-        auto locate = [&](int64_t i, int &off, int &pos) {
-            const int64_t token = first + i;
-            off = -1, pos = 0;
-            if (i >= n) return;
-            if (half) pos = gconst<int32_t>(a.positions)[token];
-            if (half && (pos < 0 || pos >= a.n_positions)) return;
-            off = (int)(gconst<int64_t>(a.slots)[token] & (a.cache.page_size - 1));
-        };
-        auto fetch_rows = [&](int64_t i, u32x4 (&x)[2]) {
-            const CF_GLOBAL u32x4 *src = gconst<u32x4>(in.data + (first + i) * in.token + head * in.head);
-            x[0] = src[place.first], x[1] = src[place.second];
-        };
-        auto finish_rows = [&](const u32x4 (&x)[2], int pos, float (&r)[16]) {
-            const int64_t at = (int64_t)pos * half + row_lane * 8;
-            turn<DT>(x[0], x[1], place, a.cos + at, a.sin + at, r);
-#pragma unroll
-            for (int k = 0; k < 16; ++k) r[k] = r[k] > Code<DT>::kMost ? Code<DT>::kMost : r[k] < -Code<DT>::kMost ? -Code<DT>::kMost : r[k];      // NaN stays
-        };
-        const int mine = share * kTokens + lane / kLanes;       // a lane's row of a round
-#pragma unroll
-        for (int i = 0; i < kKeep; ++i) {
-            off[i] = -1;
-            if (i * kRound < n) locate(i * kRound + mine, off[i], pos[i]);
-            if (off[i] >= 0) fetch_rows(i * kRound + mine, raw[i]);
-        }
-        float x[kKeep][16], most = -1.0f;
-        bool begins = false;
-#pragma unroll
-        for (int i = 0; i < kKeep; ++i)
-            if (off[i] >= 0) {
-                finish_rows(raw[i], pos[i], x[i]);
-                most = fmaxf(most, 0.0f);
-#pragma unroll
-                for (int k = 0; k < 16; ++k) most = fmaxf(most, fabsf(x[i][k]));
-                begins |= off[i] == 0;
-            }
-        for (int64_t i = kKeep * kRound + mine; i - mine < n; i += kRound) {        // those that are read twice
-            int off, pos;
-            locate(i, off, pos);
-            if (off < 0) continue;
-            u32x4 y[2];
-            float r[16];
-            fetch_rows(i, y);
-            finish_rows(y, pos, r);
-            most = fmaxf(most, 0.0f);
-#pragma unroll
-            for (int k = 0; k < 16; ++k) most = fmaxf(most, fabsf(r[k]));
-            begins |= off == 0;
-        }
-        most = max_quarters(max_halves(most));
-#pragma unroll
-        for (int d = 1; d < 16; d <<= 1) most = fmaxf(most, __shfl_xor(most, d));
-        begins = __any(begins);
-        if constexpr (WAVES > 1) {
-            __syncthreads();                    // what the page before left there has been read
-            if (lane == 0) lds_most[wave] = most, lds_begins[wave] = begins;
-            __syncthreads();
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) most = fmaxf(most, lds_most[w]), begins |= lds_begins[w];
-        }
-        if (most < 0.0f) continue;              // all of the page's tokens are left out
-
-        float *scale_at = (value ? a.cache.v_scale : a.cache.k_scale) + (int64_t)page * a.h.kv_heads + head;
-        const int before = begins ? kLeastExponent : exponent_of(*gconst<float>(scale_at));
-        const int e = max(exponent_for(most), before);
-        char *codes = (value ? a.cache.v : a.cache.k) + page * a.cache.page_bytes + (int64_t)head * a.cache.page_size * D;
-        if (!begins && e > before) {            // the other places' codes go by the new scale; places of this call are written behind them
-            const float by = power_of_two(max(before - e, -126));
-            for (int i = (share * 64 + lane) * 16; i < a.cache.page_size * D; i += 64 * WAVES * 16) {
-                u32x4 w = *gconst<u32x4>(codes + i);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const auto low = __builtin_amdgcn_cvt_pk_f32_fp8(w[k], false), high = __builtin_amdgcn_cvt_pk_f32_fp8(w[k], true);
-                    w[k] = encode4(low[0] * by, low[1] * by, high[0] * by, high[1] * by);
-                }
-                *gmut<u32x4>(codes + i) = w;
-            }
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        }
-        if constexpr (WAVES > 1) __syncthreads();       // and every wave has read the scale
-
-        const float by = power_of_two(-e), scale = power_of_two(e);
-        const bool bounded = a.cache.bounds && !value;
-        float low[16], high[16];                // of codes
-#pragma unroll
-        for (int k = 0; k < 16; ++k) low[k] = __builtin_inff(), high[k] = -__builtin_inff();
-        auto store = [&](const float (&r)[16], int off) {
-#pragma unroll
-            for (int v = 0; v < 2; ++v) {
-                u32x2 w;
-#pragma unroll
-                for (int k = 0; k < 2; ++k) w[k] = encode4(r[8 * v + 4 * k] * by, r[8 * v + 4 * k + 1] * by, r[8 * v + 4 * k + 2] * by, r[8 * v + 4 * k + 3] * by);
-                *gmut<u32x2>(codes + off * D + (v ? place.second : place.first) * 8) = w;
-                if (bounded)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const auto y = k & 1 ? __builtin_amdgcn_cvt_pk_f32_fp8(w[k >> 1], true) : __builtin_amdgcn_cvt_pk_f32_fp8(w[k >> 1], false);
-#pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            const float z = y[j] == y[j] ? y[j] : 0.0f;
-                            low[8 * v + 2 * k + j] = fminf(low[8 * v + 2 * k + j], z);
-                            high[8 * v + 2 * k + j] = fmaxf(high[8 * v + 2 * k + j], z);
-                        }
-                    }
-            }
-        };
-#pragma unroll
-        for (int i = 0; i < kKeep; ++i)
-            if (off[i] >= 0) store(x[i], off[i]);
-        for (int64_t i = kKeep * kRound + mine; i - mine < n; i += kRound) {
-            int off, pos;
-            locate(i, off, pos);
-            if (off < 0) continue;
-            u32x4 y[2];
-            float r[16];
-            fetch_rows(i, y);
-            finish_rows(y, pos, r);
-            store(r, off);
-        }
-        if (share == 0 && lane == 0) *gmut<float>(scale_at) = scale;
-        if (!bounded) continue;
-
-        // the rows' bounds meet in the first row's lanes
-        if (n > 1) {
-#pragma unroll
-            for (int d = kLanes; d < 64; d <<= 1)
-#pragma unroll
-                for (int k = 0; k < 16; ++k) {
-                    low[k] = fminf(low[k], __shfl_xor(low[k], d));
-                    high[k] = fmaxf(high[k], __shfl_xor(high[k], d));
-                }
-        }
-        if constexpr (WAVES > 1) {
-            if (lane < kLanes)
-#pragma unroll
-                for (int k = 0; k < 16; ++k) lds_bounds[wave][lane][k] = low[k], lds_bounds[wave][lane][16 + k] = high[k];
-            __syncthreads();
-            if (wave > 0) continue;             // to the barrier that the next page begins with
-            if (lane < kLanes)
-#pragma unroll
-                for (int w = 1; w < WAVES; ++w)
-#pragma unroll
-                    for (int k = 0; k < 16; ++k) {
-                        low[k] = fminf(low[k], lds_bounds[w][lane][k]);
-                        high[k] = fmaxf(high[k], lds_bounds[w][lane][16 + k]);
-                    }
-        }
-        if (lane < kLanes) {
-            uint16_t *least = a.cache.bounds + ((int64_t)page * a.h.kv_heads + head) * 2 * D;
-#pragma unroll
-            for (int v = 0; v < 2; ++v) {
-                const int at = v ? place.second : place.first;
-                u32x4 lo, hi;
-                const u32x4 lo_was = begins ? (u32x4){0, 0, 0, 0} : gconst<u32x4>(least)[at], hi_was = begins ? (u32x4){0, 0, 0, 0} : gconst<u32x4>(least + D)[at];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    float l0 = low[8 * v + 2 * k] * scale, l1 = low[8 * v + 2 * k + 1] * scale, h0 = high[8 * v + 2 * k] * scale, h1 = high[8 * v + 2 * k + 1] * scale;
-                    if (!begins) {
-                        l0 = fminf(l0, Elem<BF16>::lo(lo_was[k])), l1 = fminf(l1, Elem<BF16>::hi(lo_was[k]));
-                        h0 = fmaxf(h0, Elem<BF16>::lo(hi_was[k])), h1 = fmaxf(h1, Elem<BF16>::hi(hi_was[k]));
-                    }
-                    lo[k] = Elem<BF16>::pack(l0, l1);
-                    hi[k] = Elem<BF16>::pack(h0, h1);
-                }
-                gmut<u32x4>(least)[at] = lo;
-                gmut<u32x4>(least + D)[at] = hi;
-            }
-        }
+        const int waves = n <= kTokens ? 1 : n <= 2 * kTokens ? 2 : kWaves;     // of a row
+        if (row_here % (kWaves / waves) != 0) continue;                          // it is another workgroup's
+        const int row = row_here + wave / waves;
+        store_neighbours<DT, D, PAIRS>(a, lds, row_of<D>(a, min(row, rows - 1)), first, row < rows ? n : 0, here, lane, wave, wave / waves * waves, waves);
     }
 }
 
 template <int DT, int D> hipError_t append8_dim(const Append8Args &a, hipStream_t s)
 {
     const int64_t n = append8_workgroups(a);
-    return a.chunk > 1 ? enqueue(k_kv_append8<DT, D, 4>, n, s, a) : enqueue(k_kv_append8<DT, D, 1>, n, s, a);
+    return a.interleaved ? enqueue_of<kAppendThreads>(k_kv_append8<DT, D, true>, n, s, a) : enqueue_of<kAppendThreads>(k_kv_append8<DT, D, false>, n, s, a);
 }
 
 template <int DT> hipError_t append8_typed(const Append8Args &a, hipStream_t s)

@@ -63,9 +63,10 @@ class Cache:
                 for i, t in enumerate(rows):
                     self.codes[p, h, slots[t] % page] = y[i]
                 if self.bounds is not None:
-                    y = y.nan_to_num(nan=0.0) * 2.0 ** e
-                    low, high = y.min(0)[0], y.max(0)[0]
+                    y, none = y * 2.0 ** e, y.isnan().all(0)
+                    low, high = (torch.where(none, 0.0, f(torch.where(y.isnan(), z, y), 0)) for f, z in ((torch.amin, math.inf), (torch.amax, -math.inf)))
                     if not begun:
+                        low, high = torch.where(none, self.bounds[p, h, 0], low), torch.where(none, self.bounds[p, h, 1], high)
                         low, high = torch.minimum(low, self.bounds[p, h, 0]), torch.maximum(high, self.bounds[p, h, 1])
                     self.bounds[p, h, 0], self.bounds[p, h, 1] = low, high
 
