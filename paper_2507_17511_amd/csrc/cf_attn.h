@@ -72,8 +72,8 @@ struct JoinArgs {
     int32_t part_dtype;             // cf_dtype
     const int32_t *cover;           // if set, only the tokens from cover[0] to cover[n_cover] are joined
     int32_t n_cover;
-    const int32_t *lens;            // if set, token t has max(1, min(ceil(min(lens[t], most_keys) / split_keys), n_parts)) parts, and one of one part is done already
-    int32_t split_keys, most_keys;
+    const int32_t *lens;            // if set, token t has max(1, min(ceil(lens[t] / split_keys), n_parts)) parts, and one of one part is done already
+    int32_t split_keys;
     const void *parts[kMaxParts];
     const float *lses[kMaxParts];
 };

@@ -64,15 +64,18 @@ struct PlanArgs {
     int32_t workgroups;
 };
 
+constexpr int kHeldWorkgroups = 2;  // of the attention's, a CU
 constexpr int kXcds = 8;             // which take the workgroups in turn
 constexpr int kSelectPages = 64;    // that a workgroup of the scores takes
 constexpr int kAppendThreads = 256, kAppendTurns = 2;    // a lane rotates so many queries' parts
 constexpr int kPlanThreads = 1024;
 
+// Where workgroups have shares of all contexts (p.many): as many as the device holds at a time.
 inline int64_t paged8_workgroups(const Paged8Args &a)
 {
-    const int64_t items = paged_units(a.p) * a.p.n_splits, held = 256 * (a.p.h.head_dim == 256 ? 2 : 3);
-    return a.p.many && held < items ? held : items;
+    if (!a.p.many) return paged_units(a.p) * a.p.n_splits;
+    const int64_t units = paged_units(a.p) / a.p.n_seqs, held = 256 * kHeldWorkgroups;
+    return units * (held > units ? held / units : 1);
 }
 
 inline int64_t append8_workgroups(const Append8Args &a) { return a.page_groups + (a.q.data ? (a.n_tokens * a.h.q_heads * (a.h.head_dim / 16) + kAppendThreads * kAppendTurns - 1) / (kAppendThreads * kAppendTurns) : 0); }

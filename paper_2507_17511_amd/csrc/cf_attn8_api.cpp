@@ -66,7 +66,10 @@ cf_status check_table(int32_t n_seqs, int32_t max_pages, int64_t stride, int64_t
 
 constexpr int64_t kMostPartKeys8 = 2048;
 
-// One launch, and another one that joins parts of more than the device holds at a time.
+// A workgroup for each part of a context, two a CU: of 256 to 2048 keys each (us, 1 x 901 keys, 2 heads of 128: parts of 128 / 256 / 512 keys 8.3 / 8.9 / 10.2; 1 x 8192, 8
+// heads: 14.9 / 11.5 / 11.1; 1 x 131072, 128 to 1024: 47.4), or, past four a CU and where contexts that may differ could fill 64 MB, equal shares of all keys for as many workgroups
+// as the device holds: us, parts taken in turn / shares: 96 x 160 to 16000 keys, 8 heads of 128, 149 / 138; 64 x 8192 196 / 187; 2 x 131100 111 / 104, 24 heads of 64 157 / 150; 48 x
+// 160 to 16000, 2 heads of 256, 34 / 39.
 hipError_t paged8_at_once(Paged8Args &b, int64_t longest, void *workspace, size_t workspace_bytes, hipStream_t s)
 {
     PagedArgs &a = b.p;
@@ -86,18 +89,12 @@ hipError_t paged8_at_once(Paged8Args &b, int64_t longest, void *workspace, size_
         a.split_keys = (int32_t)round_up((longest + splits - 1) / splits, 128);
         a.n_splits = (int32_t)((longest + a.split_keys - 1) / a.split_keys);
     }
+    const bool counted = (int64_t)a.n_seqs * (((int64_t)a.max_pages << b.cache.page_shift) / 256 + 2) <= INT32_MAX;      // shares are in 32 bits
+    a.many = counted && a.n_splits > 1 && (units * a.n_splits > 4 * kCUs || (a.n_seqs > 1 && units * longest * a.h.head_dim * 2 >= (int64_t)64 << 20));
+    if (a.many) a.n_splits = (int32_t)(fit < kMaxParts ? fit : kMaxParts);       // at most, of shares that the lengths decide
     if (a.n_splits > 1) place_parts(a.parts, workspace, rows, a.n_splits, a.h.head_dim);
     a.counters = static_cast<uint32_t *>(workspace);
-    a.many = a.n_splits > 1 && (units * a.n_splits > 4 * kCUs || (a.n_seqs > 1 && units * longest * a.h.head_dim * 2 >= (int64_t)64 << 20));
-    hipError_t e = launch_paged8(b, s);
-    if (e == hipSuccess && a.many) {
-        JoinArgs j = parts_to_join(a.h, a.parts, a.n_splits, a.out, a.lse);
-        j.lens = a.lens;
-        j.split_keys = a.split_keys;
-        if (b.blocks) j.most_keys = (int32_t)(((int64_t)b.count << b.cache.page_shift) < kMostRows ? (int64_t)b.count << b.cache.page_shift : kMostRows);
-        e = launch_join(j, s);
-    }
-    return e;
+    return launch_paged8(b, s);
 }
 
 }  // namespace

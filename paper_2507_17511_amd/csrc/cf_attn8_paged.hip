@@ -2,6 +2,10 @@
 // for 16 query heads that share it, straight into registers, and the same matrix instructions of 16-bit numbers take them.  In between a
 // conversion brings two codes, times the scale of their page, into the type of the queries; codes times scales are exact there.
 //
+// Bound by HBM: 96 contexts of 160 to 16000 keys, 32 / 8 heads of 128, 138 us (5.1 TB/s), 64 of 8192 187 us (5.7; sums over rows of 2 GiB, read once, reach 5.9), 2 of 131100, 24 heads of
+// 64, 150 us (5.4); one of 901 keys, 8 / 2 heads, by latency: 8.9 us.  Two workgroups a CU with 64 keys a wave in flight read faster than three, whose registers spill, or
+// four with 32 keys (96 contexts: 149 us for 164 and 157).
+//
 // A wave takes 64 keys at a time (32 where head_dim is 256), so that as many bytes are on their way to a CU as with 16 bits.  Of K a lane reads 16
 // neighbouring elements, the left operands of two instructions over the head dimension (the queries' lanes lie alike).  Of V it reads 4 (8, 16) elements
 // of 8 neighbouring keys; a byte permute brings the codes of two keys together before they are converted.
@@ -12,9 +16,10 @@ namespace cf {
 namespace attn {
 namespace {
 
-// MANY: as in the kernel over 16 bits.  LISTED: heads attend to the listed pages of their contexts alone; keys are counted along the list.
-// WHOLE: a step's keys lie on one page.
-template <int DT, int D, bool MANY, bool LISTED, bool WHOLE> __global__ __launch_bounds__(kWaves * 64, D == 256 ? 2 : 3) void k_attn_paged8(Paged8Args b)
+// SHARED: as many workgroups as the device holds have an equal share of all contexts' keys each, which they find in the lengths: a share may be the end of one context,
+// some short ones and the beginning of another.  Otherwise a workgroup for each part that there may be.  Either way the last workgroup that is done with a context's head
+// joins its parts.  LISTED: heads attend to the listed pages of their contexts alone; keys are counted along the list.  WHOLE: a step's keys lie on one page.
+template <int DT, int D, bool SHARED, bool LISTED, bool WHOLE> __global__ __launch_bounds__(kWaves * 64, kHeldWorkgroups) void k_attn_paged8(Paged8Args b)
 {
     using E = Elem<DT>;
     using C = Code<DT>;
@@ -26,6 +31,7 @@ template <int DT, int D, bool MANY, bool LISTED, bool WHOLE> __global__ __launch
     constexpr int kWords = kPer / 4;
     constexpr int kGroups = WHOLE ? 1 : 2 * kTiles;     // keys of a step that lie on one page for sure: 16 on small ones
     constexpr int kGroupKeys = kKeys / kGroups;
+    constexpr int kGrain = kWaves * 64;         // keys: a step of the workgroup's
     const PagedArgs &a = b.p;
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quarter = lane >> 4;
@@ -35,48 +41,64 @@ template <int DT, int D, bool MANY, bool LISTED, bool WHOLE> __global__ __launch
     const int64_t capacity = min((int64_t)a.max_pages << shift, (int64_t)1 << 30);
     auto context_of = [&](int seq) { return (int)min((int64_t)max(gconst<int32_t>(a.lens)[seq], 0), capacity); };
     auto keys_of = [&](int len) { return LISTED ? (int)min((int64_t)((len + mask) >> shift), (int64_t)b.count) << shift : len; };
-    auto parts_of = [&](int keys) { return max(min((keys + a.split_keys - 1) / a.split_keys, a.n_splits), 1); };    // a context of no keys has an empty one
-    __shared__ int lds_upto[MANY ? kMostListed : 1];        // parts of the sequences up to each
-    int64_t items = gridDim.x;
-    if constexpr (MANY) {
+    const int unit = (int)(blockIdx.x % units), kv_head = unit / head_tiles, head0 = (unit % head_tiles) * kPagedHeads;
+    int seq = (int)(blockIdx.x / units), split = 0, parts = 1, begin = 0, end = 0;
+
+    // A context counts as its keys, kGrain at a time, and one more for its beginning and its end.
+    __shared__ uint32_t lds_upto[SHARED ? kMostListed : 1];     // of the sequences up to each
+    __shared__ uint32_t lds_longest;
+    uint32_t share = 0, at_work = 0, stop = 0;
+    const uint32_t group = blockIdx.x / units;
+    if constexpr (SHARED) {
         if (wave == 0) {
-            int upto = 0;
+            uint32_t upto = 0, longest = 0;
             for (int base = 0; base < a.n_seqs; base += 64) {
-                int here = base + lane < a.n_seqs ? parts_of(keys_of(context_of(base + lane))) : 0;
+                uint32_t here = base + lane < a.n_seqs ? (keys_of(context_of(base + lane)) + kGrain - 1) / kGrain + 1 : 0;
+                longest = max(longest, here);
 #pragma unroll
                 for (int d = 1; d < 64; d <<= 1) {
-                    const int below = __shfl_up(here, d);
+                    const uint32_t below = __shfl_up(here, d);
                     if (lane >= d) here += below;
                 }
                 if (base + lane < a.n_seqs) lds_upto[base + lane] = upto + here;
                 upto += __builtin_amdgcn_readlane(here, 63);
             }
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) longest = max(longest, __shfl_xor(longest, d));
+            if (lane == 0) lds_longest = longest;
         }
         __syncthreads();
-        items = (int64_t)lds_upto[a.n_seqs - 1] * units;
+        const uint32_t total = __builtin_amdgcn_readfirstlane(lds_upto[a.n_seqs - 1]), groups = gridDim.x / units;
+        share = max(max((total + groups - 1) / groups, (__builtin_amdgcn_readfirstlane(lds_longest) + a.n_splits - 2) / (a.n_splits - 1)), D == 256 ? 6u : 1u);       // a context is in n_splits shares at most
+        at_work = (uint32_t)min((uint64_t)group * share, (uint64_t)total), stop = min(total, at_work + share);
+        int most = a.n_seqs - 1;            // the first sequence with more up to it than this share begins with
+        for (seq = 0; seq < most;) {
+            const int middle = (seq + most) >> 1;
+            if (lds_upto[middle] > at_work) most = middle;
+            else seq = middle + 1;
+        }
+        seq = __builtin_amdgcn_readfirstlane(seq);
+    } else {
+        split = seq / a.n_seqs;
+        seq %= a.n_seqs;
     }
-    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-        const int unit = (int)(item % units), rest = (int)(item / units);
-        const int kv_head = unit / head_tiles, head0 = (unit % head_tiles) * kPagedHeads;
-        int seq = rest % a.n_seqs, split = rest / a.n_seqs;
-        if constexpr (MANY) {
-            int most = a.n_seqs - 1;        // the first sequence with more parts up to it than `rest`
-            for (seq = 0; seq < most;) {
-                const int middle = (seq + most) >> 1;
-                if (lds_upto[middle] > rest) most = middle;
-                else seq = middle + 1;
-            }
-            seq = __builtin_amdgcn_readfirstlane(seq);
-            split = __builtin_amdgcn_readfirstlane(rest - (seq > 0 ? lds_upto[seq - 1] : 0));
+    for (; !SHARED || at_work < stop; ++seq) {
+        const int len = context_of(seq), keys = keys_of(len);
+        if constexpr (SHARED) {
+            const uint32_t base = seq > 0 ? __builtin_amdgcn_readfirstlane(lds_upto[seq - 1]) : 0, top = __builtin_amdgcn_readfirstlane(lds_upto[seq]), from = at_work;
+            at_work = min(stop, top);
+            begin = from > base ? (int)(from - base - 1) * kGrain : 0, end = min((int)(at_work - base - 1) * kGrain, keys);
+            if (keys > 0 && begin >= end) continue;             // its beginning alone
+            split = keys > 0 ? (int)(group - (base + 1) / share) : 0;
+            parts = keys > 0 ? (int)((top - 1) / share - (base + 1) / share) + 1 : 1;
             __syncthreads();                // LDS of the part before is free
+        } else {
+            parts = max(min((keys + a.split_keys - 1) / a.split_keys, a.n_splits), 1);      // a context of no keys has an empty one
+            if (split >= parts) return;
+            begin = (int)min((int64_t)split * a.split_keys, (int64_t)keys);
+            end = split == a.n_splits - 1 ? keys : min(keys, begin + a.split_keys);
         }
         const int heads = min(a.h.group - head0, kPagedHeads);
-
-        const int len = context_of(seq), keys = keys_of(len);
-        const int begin = (int)min((int64_t)split * a.split_keys, (int64_t)keys);
-        const int end = split == a.n_splits - 1 ? keys : min(keys, begin + a.split_keys);
-        const int parts = parts_of(keys);
-        if (!MANY && split >= parts) return;
 
         float m = kNoMax, l = 0.0f;
         f32x4 o[kPer];
@@ -262,16 +284,17 @@ template <int DT, int D, bool MANY, bool LISTED, bool WHOLE> __global__ __launch
         }
 
         join_waves<D>(m, l, o, lane, wave);
-        if (!finish_part<DT, D, MANY>(a, seq, unit, units, kv_head, head0, split, parts, lane, wave, m, l, o)) return;
+        finish_part<DT, D, false>(a, seq, unit, units, kv_head, head0, split, parts, lane, wave, m, l, o);
+        if constexpr (!SHARED) return;
     }
 }
 
-template <int DT, int D, bool MANY> hipError_t paged8_over(const Paged8Args &a, hipStream_t s)
+template <int DT, int D, bool SHARED> hipError_t paged8_over(const Paged8Args &a, hipStream_t s)
 {
     const int64_t n = paged8_workgroups(a);
     const bool whole = a.cache.page_size >= (D == 256 ? 32 : 64);
-    if (a.blocks) return whole ? enqueue(k_attn_paged8<DT, D, MANY, true, true>, n, s, a) : enqueue(k_attn_paged8<DT, D, MANY, true, false>, n, s, a);
-    return whole ? enqueue(k_attn_paged8<DT, D, MANY, false, true>, n, s, a) : enqueue(k_attn_paged8<DT, D, MANY, false, false>, n, s, a);
+    if (a.blocks) return whole ? enqueue(k_attn_paged8<DT, D, SHARED, true, true>, n, s, a) : enqueue(k_attn_paged8<DT, D, SHARED, true, false>, n, s, a);
+    return whole ? enqueue(k_attn_paged8<DT, D, SHARED, false, true>, n, s, a) : enqueue(k_attn_paged8<DT, D, SHARED, false, false>, n, s, a);
 }
 
 template <int DT, int D> hipError_t paged8_dim(const Paged8Args &a, hipStream_t s) { return a.p.many ? paged8_over<DT, D, true>(a, s) : paged8_over<DT, D, false>(a, s); }

@@ -130,7 +130,6 @@ inline JoinArgs parts_to_join(const Heads &h, const Parts &p, int n, const Rows 
     j.n_rows = p.n_rows;
     j.n_parts = n;
     j.part_dtype = CF_F32;
-    j.most_keys = INT32_MAX;
     for (int i = 0; i < n; ++i) {
         j.parts[i] = p.o + i * p.n_rows * h.head_dim;
         j.lses[i] = p.lse + i * p.n_rows;

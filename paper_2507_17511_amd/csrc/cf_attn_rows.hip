@@ -92,7 +92,7 @@ template <int DT, int PT, int D, int SPREAD, int EACH> __global__ __launch_bound
     const int row_here = threadIdx.x / (kLanes * SPREAD), share = threadIdx.x / kLanes % SPREAD, lane = threadIdx.x % kLanes;
     const int64_t row = (int64_t)blockIdx.x * kRows + row_here;
     const int64_t token = (row < a.n_rows ? row : 0) / a.h.q_heads;
-    const int n_parts = a.lens ? (int)max(min((min(gconst<int32_t>(a.lens)[token], a.most_keys) + (int64_t)a.split_keys - 1) / a.split_keys, (int64_t)a.n_parts), (int64_t)1) : a.n_parts;
+    const int n_parts = a.lens ? (int)max(min((gconst<int32_t>(a.lens)[token] + (int64_t)a.split_keys - 1) / a.split_keys, (int64_t)a.n_parts), (int64_t)1) : a.n_parts;
     const bool there = row < a.n_rows && !(a.lens && n_parts == 1);
     float lse[EACH], top = -__builtin_inff(), total = 0.0f, o[8] = {};
     f32x4 x[EACH][2];
