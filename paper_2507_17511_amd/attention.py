@@ -129,6 +129,7 @@ class PageTables:
         self.table, self.lens, self.ring, self.state, self.page_size = table, lens, ring, state, page_size
         self.seqs, self.index = table.shape[0], table.get_device()
         self.head = (self.seqs, page_size, table.shape[1], ring.numel(), table.stride(0) if self.seqs > 1 else 0)
+        self.at = (table.data_ptr(), ring.data_ptr(), state.data_ptr())
 
     @classmethod
     def empty(cls, seqs: int, max_pages: int, pages: int, page_size: int = 64, device: str | torch.device = "cuda:0") -> "PageTables":
@@ -381,12 +382,13 @@ class AttentionSession:
         refused = self._new((1,), torch.int32) if refused is None else refused
         lens_out = tables.lens if lens_out is None else lens_out
         state_out = tables.state if state_out is None else state_out
-        args = _PLAN.pack(*tables.head, tokens, tables.lens.data_ptr(), self._list(news, torch.int32, n, "news"), tables.table.data_ptr(), tables.ring.data_ptr(),
-                          tables.state.data_ptr(), self._list(state_out, torch.int64, 2, "state_out"), self._list(lens_out, torch.int32, n, "lens_out"),
+        args = _PLAN.pack(*tables.head, tokens, tables.lens.data_ptr(), self._list(news, torch.int32, n, "news"), *tables.at,
+                          self._list(state_out, torch.int64, 2, "state_out"), self._list(lens_out, torch.int32, n, "lens_out"),
                           self._list(cu, torch.int32, n + 1, "cu"), self._list(slots, torch.int64, tokens, "slots"),
                           self._list(positions, torch.int32, tokens, "positions"), self._list(refused, torch.int32, 1, "refused"))
         with self._one:
             self._call(self._lib.cf_kv_plan, "cf_kv_plan", args, self._ws, self.ws_bytes)
+        _written((tables.table, tables.ring, lens_out, state_out, slots, positions, cu, refused))
         return Plan(slots, positions, cu, refused)
 
     def join(self, parts: Sequence[torch.Tensor], lses: Sequence[torch.Tensor], out: Optional[torch.Tensor] = None,

@@ -62,6 +62,7 @@ struct PlanArgs {
     int64_t table_stride;
     int32_t n_seqs, page_shift, max_pages, n_ring, n_tokens;
     int32_t workgroups;
+    int32_t wide;                   // of kPlanThreads, else of a quarter
 };
 
 constexpr int kHeldWorkgroups = 2;  // of the attention's, a CU

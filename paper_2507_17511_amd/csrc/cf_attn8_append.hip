@@ -120,13 +120,12 @@ template <int DT, int D, bool PAIRS> __device__ __forceinline__ void rotate_quer
 }
 
 template <bool LARGEST> __device__ __forceinline__ float extreme(float a, float b) { return LARGEST ? fmaxf(a, b) : fminf(a, b); }
-template <int CONTROL> __device__ __forceinline__ float dpp(float x) { return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CONTROL, 0xf, 0xf, false)); }
 
 // Over the lanes of sixteen that hold the same elements, every LANES-th one.  NaN yields to a number.
 template <bool LARGEST, int LANES> __device__ __forceinline__ float over_sixteen(float x)
 {
-    if constexpr (LANES <= 4) x = extreme<LARGEST>(x, dpp<0x124>(x));       // 4 lanes on
-    if constexpr (LANES <= 8) x = extreme<LARGEST>(x, dpp<0x128>(x));       // 8
+    if constexpr (LANES <= 4) x = extreme<LARGEST>(x, moved<0x124>(x));       // 4 lanes on
+    if constexpr (LANES <= 8) x = extreme<LARGEST>(x, moved<0x128>(x));       // 8
     return x;
 }
 // Of x and the lane 32 (16) away in the lower half (the even sixteens), of y in the other.
@@ -143,10 +142,10 @@ template <bool LARGEST> __device__ __forceinline__ float of_quarters(float x, fl
 // The largest of LANES neighbouring lanes.
 template <int LANES> __device__ __forceinline__ float over_lanes(float x)
 {
-    x = fmaxf(x, dpp<0xb1>(x));                                 // of pairs
-    x = fmaxf(x, dpp<0x4e>(x));                                 // of fours
-    if constexpr (LANES >= 8) x = fmaxf(x, dpp<0x141>(x));      // eight lanes turned round
-    if constexpr (LANES >= 16) x = fmaxf(x, dpp<0x140>(x));     // sixteen
+    x = fmaxf(x, moved<0xb1>(x));                                 // of pairs
+    x = fmaxf(x, moved<0x4e>(x));                                 // of fours
+    if constexpr (LANES >= 8) x = fmaxf(x, moved<0x141>(x));      // eight lanes turned round
+    if constexpr (LANES >= 16) x = fmaxf(x, moved<0x140>(x));     // sixteen
     return x;
 }
 

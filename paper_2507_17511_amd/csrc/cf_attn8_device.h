@@ -36,5 +36,31 @@ __device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d)
     return __builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
 }
 
+// Moves between lanes.  CONTROL: 0x110 + n from n lanes below, of sixteen; 0x142 (0x143) from the last lane of the sixteen (half) below; 0xb1, 0x4e the other lane of a pair, pair of a
+// four; 0x141 (0x140) eight (sixteen) lanes turned round.  Lanes that nothing comes to have 0.
+template <int CONTROL, int ROWS = 0xf> __device__ __forceinline__ uint32_t moved(uint32_t x) { return __builtin_amdgcn_update_dpp(0, x, CONTROL, ROWS, 0xf, false); }
+template <int CONTROL> __device__ __forceinline__ float moved(float x) { return __uint_as_float(moved<CONTROL>(__float_as_uint(x))); }
+template <int CONTROL> __device__ __forceinline__ double moved(double x)
+{
+    const u32x2 w = __builtin_bit_cast(u32x2, x);
+    return __builtin_bit_cast(double, (u32x2){moved<CONTROL>(w[0]), moved<CONTROL>(w[1])});
+}
+__device__ __forceinline__ uint32_t add(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }     // stays at the largest number
+
+// Sums over sixteen lanes up to each, and over the wave's.
+__device__ __forceinline__ uint32_t sums_of_sixteen(uint32_t x)
+{
+    x = add(x, moved<0x111>(x));
+    x = add(x, moved<0x112>(x));
+    x = add(x, moved<0x114>(x));
+    return add(x, moved<0x118>(x));
+}
+__device__ __forceinline__ uint32_t sums(uint32_t x)
+{
+    x = sums_of_sixteen(x);
+    x = add(x, moved<0x142, 0xa>(x));
+    return add(x, moved<0x143, 0xc>(x));
+}
+
 }  // namespace attn
 }  // namespace cf

@@ -3,7 +3,8 @@
 // sum over heads h and elements i of max(q_hi least_i, q_hi largest_i) = sum_i largest_i P_i + least_i N_i, where P sums the positive q_hi of the heads that share
 // the keys and N the others: one product of 2 D numbers a page, whatever the number of heads.  Sums are of 64 bits, and exact but for numbers that
 // lie more than 2^36 apart, so that ties are ties, whatever the order.  k_select_scores reads every bound once and is bound by HBM, or by its launch;
-// k_select_pages finds the least score that is taken by its bits, 11 at a time, a workgroup a row, and writes the pages in order.
+// k_select_pages finds the least score that is taken by its bits, 11 at a time, a workgroup a row, and writes the pages in order.  A thread has 8 neighbouring pages, whose
+// scores stay in registers, and whose places follow from a sum over the threads.
 #include "cf_attn8_device.h"
 
 namespace cf {
@@ -24,6 +25,20 @@ __device__ __forceinline__ int pages_of(const SelectArgs &a, int64_t seq)
     return (int)min(held, (int64_t)a.max_pages);
 }
 
+// Sums with the lane 32 (16) away: of x in the lower half (the even sixteens), of y in the other.
+__device__ __forceinline__ double of_halves(double x, double y)
+{
+    const u32x2 a = __builtin_bit_cast(u32x2, x), b = __builtin_bit_cast(u32x2, y);
+    const u32x2 low = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(a[0], b[0], false, false)), high = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(a[1], b[1], false, false));
+    return __builtin_bit_cast(double, (u32x2){low[0], high[0]}) + __builtin_bit_cast(double, (u32x2){low[1], high[1]});
+}
+__device__ __forceinline__ double of_quarters(double x, double y)
+{
+    const u32x2 a = __builtin_bit_cast(u32x2, x), b = __builtin_bit_cast(u32x2, y);
+    const u32x2 low = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false)), high = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false));
+    return __builtin_bit_cast(double, (u32x2){low[0], high[0]}) + __builtin_bit_cast(double, (u32x2){low[1], high[1]});
+}
+
 template <int DT, int D> __global__ __launch_bounds__(256) void k_select_scores(SelectArgs a)
 {
     constexpr int kLanes = D / 4;               // of a page: 8 elements each, of the least ones, then of the largest
@@ -38,14 +53,20 @@ template <int DT, int D> __global__ __launch_bounds__(256) void k_select_scores(
     const int element = lane % (kLanes / 2) * 8;
     const bool largest = lane / (kLanes / 2) % 2;
     double q[8] = {};
-    for (int h = 0; h < a.h.group; ++h) {
-        const u32x4 x = *gconst<u32x4>(a.q.data + seq * a.q.token + (int64_t)(head * a.h.group + h) * a.q.head + element * 2);
+    for (int h0 = 0; h0 < a.h.group; h0 += 4) {
+        u32x4 x[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const float lo = Elem<DT>::lo(x[k]), hi = Elem<DT>::hi(x[k]);
-            q[2 * k] += lo > 0.0f == largest || lo != lo ? (double)lo : 0.0;
-            q[2 * k + 1] += hi > 0.0f == largest || hi != hi ? (double)hi : 0.0;
-        }
+        for (int h = 0; h < 4; ++h)
+            if (h0 + h < a.h.group) x[h] = *gconst<u32x4>(a.q.data + seq * a.q.token + (int64_t)(head * a.h.group + h0 + h) * a.q.head + element * 2);
+#pragma unroll
+        for (int h = 0; h < 4; ++h)
+            if (h0 + h < a.h.group)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float lo = Elem<DT>::lo(x[h][k]), hi = Elem<DT>::hi(x[h][k]);
+                    q[2 * k] += lo > 0.0f == largest || lo != lo ? (double)lo : 0.0;
+                    q[2 * k + 1] += hi > 0.0f == largest || hi != hi ? (double)hi : 0.0;
+                }
     }
     for (int64_t first = group * kSelectPages + wave * (kSelectPages / 4); first < held; first += (int64_t)a.groups * kSelectPages) {
         const int entry = gconst<int32_t>(a.table)[seq * a.table_stride + min(first + lane % (kSelectPages / 4), (int64_t)held - 1)];
@@ -56,123 +77,166 @@ template <int DT, int D> __global__ __launch_bounds__(256) void k_select_scores(
             const int64_t here = __shfl(page, i * kPages + lane / kLanes);
             x[i] = gconst<u32x4>(a.cache.bounds + (here * a.h.kv_heads + head) * 2 * D)[lane % kLanes];
         }
+        double sum[kRounds];
 #pragma unroll
         for (int i = 0; i < kRounds; ++i) {
-            double sum = 0.0;
+            sum[i] = 0.0;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                sum = __builtin_fma((double)Elem<BF16>::lo(x[i][k]), q[2 * k], sum);
-                sum = __builtin_fma((double)Elem<BF16>::hi(x[i][k]), q[2 * k + 1], sum);
+                sum[i] = __builtin_fma((double)Elem<BF16>::lo(x[i][k]), q[2 * k], sum[i]);
+                sum[i] = __builtin_fma((double)Elem<BF16>::hi(x[i][k]), q[2 * k + 1], sum[i]);
             }
-#pragma unroll
-            for (int d = 1; d < kLanes; d <<= 1) sum += __shfl_xor(sum, d);
-            const int64_t j = first + i * kPages + lane / kLanes;
-            if (lane % kLanes == 0 && j < held) gmut<uint64_t>(a.scores)[row * a.columns + j] = ordered(sum);
         }
+        // Every exchange halves what a lane has, down to 4 sums of sixteen lanes: of rounds r, r + 4 in the odd sixteens, and r + 8, r + 12 in the upper half.
+        if constexpr (kRounds == 16)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] = of_halves(sum[i], sum[i + 8]);
+        if constexpr (kRounds >= 8)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[i] = of_quarters(sum[i], sum[i + 4]);
+        double mine = 0.0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            double t = sum[i];
+            t += moved<0xb1>(t);
+            t += moved<0x4e>(t);
+            t += moved<0x141>(t);
+            t += moved<0x140>(t);
+            if ((lane & 3) == i) mine = t;
+        }
+        const int sixteen = lane >> 4, r = lane & 3;
+        const int64_t j = first + (kRounds == 4 ? r * 4 + sixteen : kRounds == 8 ? (r + 4 * (sixteen & 1)) * 2 + (sixteen >> 1) : r + 4 * (sixteen & 1) + 8 * (sixteen >> 1));
+        if ((lane & 15) < 4 && j < held) gmut<uint64_t>(a.scores)[row * a.columns + j] = ordered(mine);
     }
 }
 
-constexpr int kPickThreads = 1024, kPickWaves = kPickThreads / 64, kBins = 2048;
+constexpr int kBins = 2048, kEach = 8;      // pages of a thread
 
-__global__ __launch_bounds__(kPickThreads) void k_select_pages(SelectArgs a)
+template <int THREADS> __global__ __launch_bounds__(THREADS) void k_select_pages(SelectArgs a)
 {
+    constexpr int kWavesHere = THREADS / 64, kOwnBins = kBins / THREADS;
     __shared__ uint32_t lds_bins[kBins];
-    __shared__ uint64_t lds_least[kPickWaves], lds_largest[kPickWaves];
-    __shared__ uint32_t lds_sums[kPickWaves], lds_ties[kPickWaves], lds_found[3];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __shared__ uint32_t lds_least[kWavesHere], lds_largest[kWavesHere], lds_sums[2][kWavesHere], lds_found[3];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t row = blockIdx.x, seq = (a.first_row + row) / a.h.kv_heads;
     const int held = pages_of(a, seq);
     CF_GLOBAL int32_t *out = gmut<int32_t>(a.blocks) + (a.first_row + row) * a.count;
     if (held <= a.count) {
-        for (int j = threadIdx.x; j < a.count; j += kPickThreads) out[j] = j < held ? j : -1;
+        for (int j = threadIdx.x; j < a.count; j += THREADS) out[j] = j < held ? j : -1;
         return;
     }
     const CF_GLOBAL uint64_t *scores = gconst<uint64_t>(a.scores + row * a.columns);
     const int behind = held - a.recent;         // pages from `first` to here compete
-    uint32_t rest = (uint32_t)(a.count - a.first - a.recent);
-    uint64_t least = ~(uint64_t)0, largest = 0;
-    if (rest > 0) {
-        for (int j = a.first + threadIdx.x; j < behind; j += kPickThreads) {
-            least = min(least, (uint64_t)scores[j]);
-            largest = max(largest, (uint64_t)scores[j]);
-        }
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            least = min(least, (uint64_t)__shfl_xor((unsigned long long)least, d));
-            largest = max(largest, (uint64_t)__shfl_xor((unsigned long long)largest, d));
-        }
-        if (lane == 0) lds_least[wave] = least, lds_largest[wave] = largest;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < kPickWaves; ++w) {
-            least = min(least, lds_least[w]);
-            largest = max(largest, lds_largest[w]);
-        }
-    }
-
-    // Scores past `least` are taken, and of those that equal it the first `rest`: all, if so many are.  The range that holds the one that decides is narrowed by 2^11 a time.
-    uint64_t from = least;
-    bool all = false;
-    while (rest > 0) {
-        const uint64_t range = largest - from;
-        const int shift = range >> 11 ? 64 - 11 - __builtin_clzll(range) : 0;
-        for (int i = threadIdx.x; i < kBins; i += kPickThreads) lds_bins[i] = 0;
-        __syncthreads();
-        for (int j = a.first + threadIdx.x; j < behind; j += kPickThreads) {
-            const uint64_t x = scores[j];
-            if (x >= from && x <= largest) atomicAdd(&lds_bins[(x - from) >> shift], 1u);
-        }
-        __syncthreads();
-        // scores in this thread's two bins, and in all bins from there on
-        const uint32_t low = lds_bins[2 * threadIdx.x], high = lds_bins[2 * threadIdx.x + 1];
-        uint32_t upto = low + high;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t above = __shfl_down(upto, d);
-            if (lane + d < 64) upto += above;
-        }
-        if (lane == 0) lds_sums[wave] = upto;
-        __syncthreads();
-        for (int w = wave + 1; w < kPickWaves; ++w) upto += lds_sums[w];
-        const uint32_t from_high = upto - low, past = from_high - high;     // scores from the upper bin on, and past it
-        if (past < rest && rest <= from_high) lds_found[0] = 2 * threadIdx.x + 1, lds_found[1] = past, lds_found[2] = high;
-        if (from_high < rest && rest <= upto) lds_found[0] = 2 * threadIdx.x, lds_found[1] = from_high, lds_found[2] = low;
-        __syncthreads();
-        const uint64_t bin = lds_found[0];
-        rest -= lds_found[1];
-        all = lds_found[2] == rest;
-        from += bin << shift;
-        if (all || shift == 0) break;
-        largest = min(largest, from + (((uint64_t)1 << shift) - 1));
-        __syncthreads();
-    }
-    // -> a score is taken if it is past `from`, or if it equals it and is one of the first `rest`, or (all) if it is not less; nothing competes if rest was 0
     const bool some = a.count > a.first + a.recent;
+    uint64_t x[kEach];                          // scores of pages base + kEach * threadIdx.x .., 0 where they do not compete
+    auto read = [&](int base) {
+        const int j = base + kEach * threadIdx.x;
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) x[k] = some && j + k >= a.first && j + k < behind ? scores[j + k] : 0;
+    };
+    auto competes = [&](int base, int k) {
+        const int j = base + kEach * (int)threadIdx.x + k;
+        return some && j >= a.first && j < behind;
+    };
+    constexpr int kTurn = THREADS * kEach;
+    const bool once = held <= kTurn;            // they stay in registers
+    read(0);
+
+    // -> how many of the threads before this one, and in all
+    int turn = 0;
+    auto upto = [&](uint32_t mine, uint32_t &all) {
+        const uint32_t s = sums(mine);
+        if (lane == 63) lds_sums[turn & 1][wave] = s;
+        __syncthreads();
+        const uint32_t w = sums_of_sixteen((lane & 15) < kWavesHere ? lds_sums[turn & 1][min(lane & 15, kWavesHere - 1)] : 0);
+        all = __builtin_amdgcn_readlane(w, 15);
+        ++turn;
+        return s - mine + (wave > 0 ? __builtin_amdgcn_readlane(w, wave - 1) : 0);
+    };
+
+    // Scores past `from` are taken, and of those that equal it the first `rest`: all, if so many are.  The range that holds the one that decides is narrowed by 2^11 a time.
+    uint64_t from = 0;
+    uint32_t rest = (uint32_t)(a.count - a.first - a.recent);
+    bool all = false;
+    if (some) {
+        uint32_t least = ~0u, largest = 0;      // by their upper halves
+        for (int base = 0; base < behind; base += kTurn) {
+            if (base > 0) read(base);
+#pragma unroll
+            for (int k = 0; k < kEach; ++k) {
+                const uint32_t high = (uint32_t)(x[k] >> 32);
+                if (competes(base, k)) least = min(least, high);
+                largest = max(largest, high);
+            }
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) least = min(least, __shfl_xor(least, d)), largest = max(largest, __shfl_xor(largest, d));
+        if (lane == 0) lds_least[wave] = least, lds_largest[wave] = largest;
+        for (int i = threadIdx.x; i < kBins; i += THREADS) lds_bins[i] = 0;
+        __syncthreads();
+        for (int w = 0; w < kWavesHere; ++w) least = min(least, lds_least[w]), largest = max(largest, lds_largest[w]);
+        from = (uint64_t)least << 32;
+        uint64_t end = (uint64_t)largest << 32 | ~0u;
+        for (;;) {
+            const uint64_t range = end - from;
+            const int shift = range >> 11 ? 64 - 11 - __builtin_clzll(range) : 0;
+            for (int base = 0; base < behind; base += kTurn) {
+                if (!once) read(base);
+#pragma unroll
+                for (int k = 0; k < kEach; ++k)
+                    if (competes(base, k) && x[k] >= from && x[k] <= end) atomicAdd(&lds_bins[(x[k] - from) >> shift], 1u);
+            }
+            __syncthreads();
+            // scores in this thread's bins, and in all bins past them
+            uint32_t bin[kOwnBins], mine = 0, total;
+#pragma unroll
+            for (int k = 0; k < kOwnBins; ++k) {
+                bin[k] = lds_bins[kOwnBins * threadIdx.x + k];
+                lds_bins[kOwnBins * threadIdx.x + k] = 0;
+                mine += bin[k];
+            }
+            const uint32_t below = upto(mine, total);
+            uint32_t past = total - below - mine;
+#pragma unroll
+            for (int k = kOwnBins - 1; k >= 0; --k) {
+                if (past < rest && rest <= past + bin[k]) lds_found[0] = kOwnBins * threadIdx.x + k, lds_found[1] = past, lds_found[2] = bin[k];
+                past += bin[k];
+            }
+            __syncthreads();
+            rest -= lds_found[1];
+            all = lds_found[2] == rest;
+            from += (uint64_t)lds_found[0] << shift;
+            if (all || shift == 0) break;
+            end = min(end, from + (((uint64_t)1 << shift) - 1));
+            __syncthreads();
+        }
+    }
+    // -> a page is taken if its score is past `from`, or if it equals it and is one of the first `rest`, or (all) if it is not less; and if it does not compete
     uint32_t taken = 0, ties = 0;
-    for (int base = 0; base < held; base += kPickThreads) {
-        const int j = base + threadIdx.x;
-        const bool there = j < held, always = there && (j < a.first || j >= behind), competes = there && !always && some;
-        const uint64_t x = competes ? (uint64_t)scores[j] : 0;
-        const bool tie = competes && !all && x == from;
-        const uint64_t tie_mask = __ballot(tie), before = ((uint64_t)1 << lane) - 1;
-        __syncthreads();
-        if (lane == 0) lds_ties[wave] = __builtin_popcountll(tie_mask);
-        __syncthreads();
-        uint32_t rank = ties + __builtin_popcountll(tie_mask & before);
-        for (int w = 0; w < kPickWaves; ++w) {
-            if (w < wave) rank += lds_ties[w];
-            ties += lds_ties[w];
+    for (int base = 0; base < held; base += kTurn) {
+        if (!once) read(base);
+        const int j = base + kEach * threadIdx.x;
+        uint32_t tie = 0, take = 0;
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) {
+            if (competes(base, k)) {
+                if (all ? x[k] >= from : x[k] > from) take |= 1u << k;
+                else if (!all && x[k] == from) tie |= 1u << k;
+            } else if (j + k < held && (j + k < a.first || j + k >= behind)) take |= 1u << k;
         }
-        const bool take = always || (competes && (all ? x >= from : x > from || (tie && rank < rest)));
-        const uint64_t mask = __ballot(take);
-        if (lane == 0) lds_sums[wave] = __builtin_popcountll(mask);
-        __syncthreads();
-        uint32_t at = taken + __builtin_popcountll(mask & before);
-        for (int w = 0; w < kPickWaves; ++w) {
-            if (w < wave) at += lds_sums[w];
-            taken += lds_sums[w];
+        if (some && !all) {
+            uint32_t in_all;
+            uint32_t rank = ties + upto(__builtin_popcount(tie), in_all);
+            for (; tie != 0; tie &= tie - 1, ++rank)
+                if (rank < rest) take |= tie & -tie;
+            ties += in_all;
         }
-        if (take) out[at] = j;
+        uint32_t in_all;
+        uint32_t at = taken + upto(__builtin_popcount(take), in_all);
+        taken += in_all;
+#pragma unroll
+        for (int k = 0; k < kEach; ++k)
+            if (take >> k & 1) out[at++] = j + k;
     }
 }
 
@@ -192,7 +256,8 @@ hipError_t launch_select(const SelectArgs &a, hipStream_t s)
 {
     hipError_t e = hipSuccess;
     if (a.max_pages > a.count && a.count > a.first + a.recent) e = a.h.dtype == BF16 ? scores_typed<BF16>(a, s) : scores_typed<F16>(a, s);
-    return e == hipSuccess ? enqueue_of<kPickThreads>(k_select_pages, a.n_rows, s, a) : e;
+    if (e != hipSuccess) return e;
+    return a.max_pages <= 256 * kEach ? enqueue_of<256>(k_select_pages<256>, a.n_rows, s, a) : enqueue_of<1024>(k_select_pages<1024>, a.n_rows, s, a);
 }
 
 }  // namespace attn
