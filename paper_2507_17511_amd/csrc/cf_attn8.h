@@ -68,7 +68,7 @@ struct PlanArgs {
 constexpr int kHeldWorkgroups = 2;  // of the attention's, a CU
 constexpr int kXcds = 8;             // which take the workgroups in turn
 constexpr int kSelectPages = 64;    // that a workgroup of the scores takes
-constexpr int kAppendThreads = 256, kAppendTurns = 2;    // a lane rotates so many queries' parts
+constexpr int kAppendThreads = 256, kAppendTurns = 4;    // a lane rotates its part of so many heads' queries
 constexpr int kPlanThreads = 1024;
 
 // Where workgroups have shares of all contexts (p.many): as many as the device holds at a time.
@@ -79,7 +79,11 @@ inline int64_t paged8_workgroups(const Paged8Args &a)
     return units * (held > units ? held / units : 1);
 }
 
-inline int64_t append8_workgroups(const Append8Args &a) { return a.page_groups + (a.q.data ? (a.n_tokens * a.h.q_heads * (a.h.head_dim / 16) + kAppendThreads * kAppendTurns - 1) / (kAppendThreads * kAppendTurns) : 0); }
+inline int64_t append8_workgroups(const Append8Args &a)
+{
+    const int64_t lanes = a.q.data ? a.n_tokens * ((a.h.q_heads + kAppendTurns - 1) / kAppendTurns) * (a.h.head_dim / 16) : 0;
+    return a.page_groups + (lanes + kAppendThreads - 1) / kAppendThreads;
+}
 
 hipError_t launch_paged8(const Paged8Args &a, hipStream_t s);
 hipError_t launch_append8(const Append8Args &a, hipStream_t s);

@@ -66,8 +66,8 @@ cf_status check_table(int32_t n_seqs, int32_t max_pages, int64_t stride, int64_t
 
 constexpr int64_t kMostPartKeys8 = 2048;
 
-// A workgroup for each part of a context, two a CU: of 256 to 2048 keys each (us, 1 x 901 keys, 2 heads of 128: parts of 128 / 256 / 512 keys 8.3 / 8.9 / 10.2; 1 x 8192, 8
-// heads: 14.9 / 11.5 / 11.1; 1 x 131072, 128 to 1024: 47.4), or, past four a CU and where contexts that may differ could fill 64 MB, equal shares of all keys for as many workgroups
+// A workgroup for each part of a context, two a CU: of 256 to 2048 keys each, or 128 where a context is 1024 at most (us, parts of 128 / 256 / 512 keys: 1 x 901, 2 heads of 128
+// 8.3 / 9.0 / 10.2, of 256 8.7 / 10.1 / 11.9; 1 x 8192, 8 heads 14.8 / 11.5 / 11.0; 2 x 4000, 4 heads of 256 12.6 / 11.3 / 12.5; 1 x 131072 47.4 all three), or, past four a CU and where contexts that may differ could fill 64 MB, equal shares of all keys for as many workgroups
 // as the device holds: us, parts taken in turn / shares: 96 x 160 to 16000 keys, 8 heads of 128, 149 / 138; 64 x 8192 196 / 187; 2 x 131100 111 / 104, 24 heads of 64 157 / 150; 48 x
 // 160 to 16000, 2 heads of 256, 34 / 39.
 hipError_t paged8_at_once(Paged8Args &b, int64_t longest, void *workspace, size_t workspace_bytes, hipStream_t s)
@@ -75,8 +75,9 @@ hipError_t paged8_at_once(Paged8Args &b, int64_t longest, void *workspace, size_
     PagedArgs &a = b.p;
     const int64_t units = paged_units(a);
     const int64_t rows = (int64_t)a.n_seqs * a.h.q_heads;
-    int64_t keys = round_up((longest * units + 2 * kCUs - 1) / (2 * kCUs), 256);
-    if (units * 32 >= kCUs && keys < longest / 32) keys = round_up(longest / 32, 256);
+    const int64_t grain = longest <= 1024 ? 128 : 256;
+    int64_t keys = round_up((longest * units + 2 * kCUs - 1) / (2 * kCUs), grain);
+    if (units * 32 >= kCUs && keys < longest / 32) keys = round_up(longest / 32, grain);
     if (keys > kMostPartKeys8) keys = kMostPartKeys8;
     int64_t splits = (longest + keys - 1) / keys;
     const int64_t fit = parts_that_fit(workspace_bytes, rows, a.h.head_dim);

@@ -75,48 +75,46 @@ template <int DT, bool PAIRS> __device__ __forceinline__ Elements turn(const Raw
 
 constexpr int kTurns = kAppendTurns;
 
+// A lane has its part of the rows of kTurns heads of a token, which turn by the same angles (16384 tokens of 24 heads of 128: 35 us for 42 with angles for each).
 template <int DT, int D, bool PAIRS> __device__ __forceinline__ void rotate_queries(const Append8Args &a, uint32_t group)
 {
     constexpr int kLanes = D / 16;
-    const uint32_t of_token = a.h.q_heads * kLanes;
-    const int half = a.rotary_dim >> 1;
-    const CF_GLOBAL u32x4 *src[kTurns];
-    CF_GLOBAL u32x4 *dst[kTurns];
+    const uint32_t of_token = (a.h.q_heads + kTurns - 1) / kTurns * kLanes;
+    const uint32_t id = group * (kWaves * 64) + threadIdx.x;        // a launch counts fewer than 2^32 work-items
+    const int64_t token = id / of_token;
+    const uint32_t rest = id % of_token, lane = rest % kLanes;
+    const int head0 = rest / kLanes * kTurns, heads = min(a.h.q_heads - head0, kTurns), half = a.rotary_dim >> 1;
+    if (token >= a.n_tokens) return;
+    const Place place = place_of<PAIRS>(lane, half);
+    const char *src = a.q.data + token * a.q.token + head0 * a.q.head;
+    char *dst = a.q_out.data + token * a.q_out.token + head0 * a.q_out.head;
     Raw raw[kTurns];
-    Angles angles[kTurns];
-    Place place[kTurns];
-    bool there[kTurns];
 #pragma unroll
-    for (int i = 0; i < kTurns; ++i) {
-        const uint32_t id = (group * kTurns + i) * (kWaves * 64) + threadIdx.x;       // a launch counts fewer than 2^32 work-items, a half of these
-        const int64_t token = id / of_token;
-        const uint32_t rest = id % of_token, lane = rest % kLanes, head = rest / kLanes;
-        int pos = 0;
-        there[i] = token < a.n_tokens;
-        if (there[i] && half) {
-            pos = gconst<int32_t>(a.positions)[token];
-            there[i] = pos >= 0 && pos < a.n_positions;
+    for (int i = 0; i < kTurns; ++i)
+        if (i < heads) {
+            const CF_GLOBAL u32x4 *at = gconst<u32x4>(src + i * a.q.head);
+            raw[i] = {at[place.first], at[place.second]};
         }
-        place[i] = place_of<PAIRS>(lane, half);
-        src[i] = gconst<u32x4>(a.q.data + token * a.q.token + head * a.q.head);
-        dst[i] = gmut<u32x4>(a.q_out.data + token * a.q_out.token + head * a.q_out.head);
-        if (!there[i]) continue;
-        raw[i] = {src[i][place[i].first], src[i][place[i].second]};
-        if (place[i].rotated) angles[i] = angles_of(a, pos, half, lane);
+    Angles angles;
+    if (half) {
+        const int pos = gconst<int32_t>(a.positions)[token];
+        if (pos < 0 || pos >= a.n_positions) return;
+        if (place.rotated) angles = angles_of(a, pos, half, lane);
     }
 #pragma unroll
-    for (int i = 0; i < kTurns; ++i) {
-        if (!there[i]) continue;
-        const Elements r = turn<DT, PAIRS>(raw[i], angles[i], place[i].rotated);
-        u32x4 u, w;
+    for (int i = 0; i < kTurns; ++i)
+        if (i < heads) {
+            const Elements r = turn<DT, PAIRS>(raw[i], angles, place.rotated);
+            u32x4 u, w;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            u[k] = Elem<DT>::pack(r.x[2 * k], r.x[2 * k + 1]);
-            w[k] = Elem<DT>::pack(r.x[8 + 2 * k], r.x[8 + 2 * k + 1]);
+            for (int k = 0; k < 4; ++k) {
+                u[k] = Elem<DT>::pack(r.x[2 * k], r.x[2 * k + 1]);
+                w[k] = Elem<DT>::pack(r.x[8 + 2 * k], r.x[8 + 2 * k + 1]);
+            }
+            CF_GLOBAL u32x4 *at = gmut<u32x4>(dst + i * a.q_out.head);
+            at[place.first] = u;
+            at[place.second] = w;
         }
-        dst[i][place[i].first] = u;
-        dst[i][place[i].second] = w;
-    }
 }
 
 template <bool LARGEST> __device__ __forceinline__ float extreme(float a, float b) { return LARGEST ? fmaxf(a, b) : fminf(a, b); }

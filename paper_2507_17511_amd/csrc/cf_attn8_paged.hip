@@ -39,7 +39,7 @@ template <int DT, int D, bool SHARED, bool LISTED, bool WHOLE> __global__ __laun
     const int units = a.h.kv_heads * head_tiles;
     const int shift = b.cache.page_shift, mask = b.cache.page_size - 1;
     const int64_t capacity = min((int64_t)a.max_pages << shift, (int64_t)1 << 30);
-    auto context_of = [&](int seq) { return (int)min((int64_t)max(gconst<int32_t>(a.lens)[seq], 0), capacity); };
+    auto context_of = [&](int seq) { return (int)min((int64_t)max(((const CF_CONST int32_t *)a.lens)[seq], 0), capacity); };
     auto keys_of = [&](int len) { return LISTED ? (int)min((int64_t)((len + mask) >> shift), (int64_t)b.count) << shift : len; };
     const int unit = (int)(blockIdx.x % units), kv_head = unit / head_tiles, head0 = (unit % head_tiles) * kPagedHeads;
     int seq = (int)(blockIdx.x / units), split = 0, parts = 1, begin = 0, end = 0;
@@ -55,11 +55,7 @@ template <int DT, int D, bool SHARED, bool LISTED, bool WHOLE> __global__ __laun
             for (int base = 0; base < a.n_seqs; base += 64) {
                 uint32_t here = base + lane < a.n_seqs ? (keys_of(context_of(base + lane)) + kGrain - 1) / kGrain + 1 : 0;
                 longest = max(longest, here);
-#pragma unroll
-                for (int d = 1; d < 64; d <<= 1) {
-                    const uint32_t below = __shfl_up(here, d);
-                    if (lane >= d) here += below;
-                }
+                here = sums(here);
                 if (base + lane < a.n_seqs) lds_upto[base + lane] = upto + here;
                 upto += __builtin_amdgcn_readlane(here, 63);
             }
@@ -71,13 +67,13 @@ template <int DT, int D, bool SHARED, bool LISTED, bool WHOLE> __global__ __laun
         const uint32_t total = __builtin_amdgcn_readfirstlane(lds_upto[a.n_seqs - 1]), groups = gridDim.x / units;
         share = max(max((total + groups - 1) / groups, (__builtin_amdgcn_readfirstlane(lds_longest) + a.n_splits - 2) / (a.n_splits - 1)), D == 256 ? 6u : 1u);       // a context is in n_splits shares at most
         at_work = (uint32_t)min((uint64_t)group * share, (uint64_t)total), stop = min(total, at_work + share);
-        int most = a.n_seqs - 1;            // the first sequence with more up to it than this share begins with
-        for (seq = 0; seq < most;) {
-            const int middle = (seq + most) >> 1;
-            if (lds_upto[middle] > at_work) most = middle;
-            else seq = middle + 1;
+        for (seq = 0; seq < a.n_seqs; seq += 64) {      // the first sequence with more up to it than this share begins with
+            const uint64_t past = __ballot(seq + lane < a.n_seqs && lds_upto[min(seq + lane, a.n_seqs - 1)] > at_work);
+            if (past) {
+                seq += __builtin_ctzll(past);
+                break;
+            }
         }
-        seq = __builtin_amdgcn_readfirstlane(seq);
     } else {
         split = seq / a.n_seqs;
         seq %= a.n_seqs;
