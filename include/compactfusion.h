@@ -463,7 +463,7 @@ typedef struct {
     int32_t page_size;       /* tokens of a page: 16, 32, 64 or 128 */
 } cf_kv_cache8;
 
-/* cf_kv_append into such a cache: rotation in fp32, then codes, with one rounding.  Tokens of a call that go to the same page are neighbours in it, with no
+/* cf_kv_append into such a cache: rotation in fp32, then codes, with one rounding.  Tokens (two in one slot, too) of a call that go to the same page are neighbours in it, with no
  * other tokens between them (as those of a sequence are); otherwise what that page holds afterwards is undefined.  A token at a page's first place begins
  * the page anew: its scales and bounds are those of the call's tokens.  On a page that is not begun the scale grows where the call's tokens need it, and the codes of all other
  * places are rounded to the new one: exactly, but for those below 2^-6 of it.  The bounds are of elements as stored, and keep those of elements that were rounded again. */
@@ -496,7 +496,7 @@ typedef struct {
 } cf_select;
 
 /* For every sequence and head of keys the `count` pages of the context whose keys may score highest, in the order of the context, then -1.  The score of a page is
- * sum over the heads that share the keys and over i of max(q_i least_i, q_i largest_i): no sum of a key's scores of these heads is larger.  It is summed in 64 bits, and of
+ * sum over the heads that share the keys and over i of max(q_i least_i, q_i largest_i): no sum of a key's scores of these heads is larger (but for keys that were rounded again).  It is summed in 64 bits, and of
  * equal ones the earlier page is taken; NaN is the least of scores.  The scale of the scores does not matter.  The workspace (as for the attentions, not null) holds the scores: 8 bytes for each page of each
  * head of keys; where it does not hold all, the call takes some at a time, and it has to hold those of one head (CF_ERR_WORKSPACE). */
 cf_status cf_attn_select(const cf_attn_desc *desc, const cf_kv_cache8 *cache, const cf_select *args, void *workspace, size_t workspace_bytes, void *stream);

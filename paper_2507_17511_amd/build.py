@@ -12,7 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcompactfusion.so")
 SOURCES = ["cf_api.cpp", "cf_kernels.hip", "cf_single_pass.hip", "cf_lowrank.hip", "cf_static.hip",
            "cf_attn_api.cpp", "cf_attn_prompt.hip", "cf_attn_paged.hip", "cf_attn_rows.hip",
-           "cf_attn8_api.cpp", "cf_attn8_append.hip", "cf_attn8_paged.hip", "cf_attn8_select.hip", "cf_kv_plan.hip"]
+           "cf_attn8_api.cpp", "cf_attn8_append.hip", "cf_attn8_paged.hip", "cf_attn8_select.hip", "cf_attn8_plan.hip"]
 HEADERS = [os.path.join(CSRC, "cf_internal.h"), os.path.join(CSRC, "cf_device.h"), os.path.join(CSRC, "cf_attn.h"),
            os.path.join(CSRC, "cf_attn_device.h"), os.path.join(CSRC, "cf_attn_parts.h"), os.path.join(CSRC, "cf_attn_checks.h"),
            os.path.join(CSRC, "cf_attn8.h"), os.path.join(CSRC, "cf_attn8_device.h"), os.path.join(ROOT, "include", "compactfusion.h")]

@@ -1,5 +1,5 @@
 // Internal interface between the host half of the entry points for the cache in 8 bits (cf_attn8_api.cpp) and their
-// kernels (cf_attn8_paged.hip, cf_attn8_append.hip, cf_attn8_select.hip, cf_kv_plan.hip).  Not installed; not part of the ABI.
+// kernels (cf_attn8_paged.hip, cf_attn8_append.hip, cf_attn8_select.hip, cf_attn8_plan.hip).  Not installed; not part of the ABI.
 #pragma once
 
 #include "cf_attn.h"

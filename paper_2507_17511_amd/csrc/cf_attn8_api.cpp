@@ -305,8 +305,8 @@ cf_status cf_kv_plan(const cf_plan *args, void *workspace, size_t workspace_byte
     a.max_pages = args->max_pages;
     a.n_ring = args->n_ring;
     a.n_tokens = (int32_t)args->n_tokens;
-    // Few threads where there is little to do: what all of them compute is most of the time.  A token for each of many: us, 1500 sequences that bring 40000 tokens, one / two / four at a
-    // time for a thread 11.8 / 13.1 / 16.3, 14 prompts of 3000 5.5 / 6.3 / 6.3.
+    // Few threads where there is little to do: what all of them compute is most of the time.  A token for each of many: us, 1500 sequences that bring 36579 tokens, one / two / four at a
+    // time for a thread 11.8 / 13.1 / 16.3, 14 prompts of 2768 5.5 / 6.3 / 6.3.
     a.wide = args->n_seqs > kPlanThreads / 4 || args->n_tokens > kPlanThreads;
     int64_t groups = (args->n_tokens + kPlanThreads - 1) / kPlanThreads;
     if (groups > kPlanWorkgroups) groups = kPlanWorkgroups;

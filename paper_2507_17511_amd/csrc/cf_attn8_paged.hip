@@ -2,8 +2,8 @@
 // for 16 query heads that share it, straight into registers, and the same matrix instructions of 16-bit numbers take them.  In between a
 // conversion brings two codes, times the scale of their page, into the type of the queries; codes times scales are exact there.
 //
-// Bound by HBM: 96 contexts of 160 to 16000 keys, 32 / 8 heads of 128, 138 us (5.1 TB/s), 64 of 8192 187 us (5.7; sums over rows of 2 GiB, read once, reach 5.9), 2 of 131100, 24 heads of
-// 64, 150 us (5.4); one of 901 keys, 8 / 2 heads, by latency: 8.9 us.  Two workgroups a CU with 64 keys a wave in flight read faster than three, whose registers spill, or
+// Bound by HBM: 96 contexts of 160 to 16000 keys, 32 / 8 heads of 128, 137 us (5.1 TB/s), 64 of 8192 187 us (5.7; sums over rows of 2 GiB, read once, reach 5.9), 2 of 131100, 24 heads of
+// 64, 144 us (5.6); one of 901 keys, 8 / 2 heads, by latency: 8.3 us.  Two workgroups a CU with 64 keys a wave in flight read faster than three, whose registers spill, or
 // four with 32 keys (96 contexts: 149 us for 164 and 157).
 //
 // A wave takes 64 keys at a time (32 where head_dim is 256), so that as many bytes are on their way to a CU as with 16 bits.  Of K a lane reads 16

@@ -4,7 +4,8 @@
 // all, as many sequences at a time as it has threads, and then looks up its share of the tokens in them.  Sums are of 32 bits and stay at the largest number: what passes n_tokens or
 // the free pages is not served, by how much it passes them does not matter.  Lengths and the ring's state may be updated in place: the workgroup that
 // is done last writes them, when all others have read them.  Bound by its launch and a chain of latencies (what it reads and writes is some 100 kB), and by the number of
-// instructions, on the few CUs that it runs on: sums by moves between lanes, no 64-bit division.
+// instructions, on the few CUs that it runs on: sums by moves between lanes, no 64-bit division (us in a graph: 48 sequences of a token 4.1, 14 prompts of 2768 tokens 5.4, 1500 sequences
+// of 36579 11.9; with sums of 64 bits through LDS 11.6, 18.4, 34.3).
 #include "cf_attn8_device.h"
 
 namespace cf {
@@ -56,7 +57,7 @@ template <int THREADS> __global__ __launch_bounds__(THREADS) void k_kv_plan(Plan
         if (base + THREADS < a.n_seqs) ask(base + THREADS);
         const bool ended = news < 0, sane = len_given >= 0 && len_given <= capacity;
         const int32_t len = sane ? len_given : 0;
-        const uint32_t n = ended ? 0 : news, held = (uint32_t)(len + mask) >> shift, total = (uint32_t)len + n;
+        const uint32_t n = ended ? 0 : news, held = ((uint32_t)len + mask) >> shift, total = (uint32_t)len + n;
         const bool room = !ended && sane && total <= (uint64_t)capacity;
         const uint32_t need = room ? ((total + mask) >> shift) - held : 0, back = ended ? held : 0;
         const uint32_t s0 = sums(n), s1 = sums(need), s2 = sums(back);
@@ -124,7 +125,7 @@ template <int THREADS> __global__ __launch_bounds__(THREADS) void k_kv_plan(Plan
             int32_t pos = -1;
             if (len >= 0) {
                 pos = len + (int32_t)(row - (i > 0 ? lds_upto[i - 1] : before));
-                const uint32_t index = pos >> shift, held = (uint32_t)(len + mask) >> shift;
+                const uint32_t index = pos >> shift, held = ((uint32_t)len + mask) >> shift;
                 CF_GLOBAL int32_t *entry = gmut<int32_t>(a.table) + (base + i) * a.table_stride + index;
                 const int64_t page = index < held ? *entry : gconst<int32_t>(a.ring)[wrapped(lds_fresh[i] + (index - held))];
                 if (index >= held && (pos & mask) == 0) *entry = (int32_t)page;

