@@ -120,25 +120,31 @@ template <int DT, int D, bool PAIRS> __device__ __forceinline__ void rotate_quer
         }
 }
 
-template <bool LARGEST> __device__ __forceinline__ float extreme(float a, float b) { return LARGEST ? fmaxf(a, b) : fminf(a, b); }
-
-// Over the lanes of sixteen that hold the same elements, every LANES-th one.  NaN yields to a number.
-template <bool LARGEST, int LANES> __device__ __forceinline__ float over_sixteen(float x)
+// Of two fp16 numbers each.  NaN yields to a number; there are no signalling ones among decoded codes.
+template <bool LARGEST> __device__ __forceinline__ uint32_t extreme(uint32_t a, uint32_t b)
 {
-    if constexpr (LANES <= 4) x = extreme<LARGEST>(x, moved<0x124>(x));       // 4 lanes on
-    if constexpr (LANES <= 8) x = extreme<LARGEST>(x, moved<0x128>(x));       // 8
+    uint32_t r;
+    if constexpr (LARGEST) asm("v_pk_max_f16 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    else asm("v_pk_min_f16 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+// Over the lanes of sixteen that hold the same elements, every LANES-th one.
+template <bool LARGEST, int LANES> __device__ __forceinline__ uint32_t over_sixteen(uint32_t x)
+{
+    if constexpr (LANES <= 4) x = extreme<LARGEST>(x, moved<0x124>(x));     // 4 lanes on
+    if constexpr (LANES <= 8) x = extreme<LARGEST>(x, moved<0x128>(x));     // 8
     return x;
 }
 // Of x and the lane 32 (16) away in the lower half (the even sixteens), of y in the other.
-template <bool LARGEST> __device__ __forceinline__ float of_halves(float x, float y)
+template <bool LARGEST> __device__ __forceinline__ uint32_t of_halves(uint32_t x, uint32_t y)
 {
-    const u32x2 r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y), false, false));
-    return extreme<LARGEST>(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    const u32x2 r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(x, y, false, false));
+    return extreme<LARGEST>(r[0], r[1]);
 }
-template <bool LARGEST> __device__ __forceinline__ float of_quarters(float x, float y)
+template <bool LARGEST> __device__ __forceinline__ uint32_t of_quarters(uint32_t x, uint32_t y)
 {
-    const u32x2 r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(y), false, false));
-    return extreme<LARGEST>(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    const u32x2 r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(x, y, false, false));
+    return extreme<LARGEST>(r[0], r[1]);
 }
 // The largest of LANES neighbouring lanes.
 template <int LANES> __device__ __forceinline__ float over_lanes(float x)
@@ -274,7 +280,7 @@ template <int DT, int D, bool PAIRS> __device__ __forceinline__ void store_lone(
 struct Shared {
     float most[kWaves];
     bool begins[kWaves];
-    float bounds[kWaves][512];      // [least, largest][D]
+    _Float16 bounds[kWaves][512];   // [least, largest][D], codes' values
 };
 
 // Tokens first .. first + n - 1, two at least, go to one page: a row of them, by `waves` of the workgroup's from wave0 on.  A wave without a row has no tokens.
@@ -321,12 +327,10 @@ __device__ __forceinline__ void store_neighbours(const Append8Args &a, Shared &l
     if (some && !begins && e > before) rescale(codes, a.cache.page_size * D, before - e, (wave - wave0) * 64 + lane, waves * 64);
     __syncthreads();
 
-    // Rounding keeps the order: the bounds are the codes of the least and the largest element.
     const float by = power_of_two(-e), scale = power_of_two(e);
-    float least[16], largest[16];
+    uint32_t least[8], largest[8];              // of codes' values, in pairs: fp16 holds them
 #pragma unroll
-    for (int k = 0; k < 16; ++k) least[k] = __builtin_inff(), largest[k] = -__builtin_inff();
-#pragma unroll 2
+    for (int k = 0; k < 8; ++k) least[k] = 0x7c007c00u, largest[k] = 0xfc00fc00u;
     for (int i = mine; i < n; i += round) {
         const Where w = where_is(a, first + i);
         if (w.off < 0) continue;
@@ -334,38 +338,46 @@ __device__ __forceinline__ void store_neighbours(const Append8Args &a, Shared &l
         if (limited)
 #pragma unroll
             for (int k = 0; k < 16; ++k) r.x[k] = within<DT>(r.x[k]);
-        if (row.bounds)
 #pragma unroll
-            for (int k = 0; k < 16; ++k) least[k] = fminf(least[k], r.x[k]), largest[k] = fmaxf(largest[k], r.x[k]);
-        *gmut<u32x2>(codes + w.off * D + place.first * 8) = encode8(r.x, by);
-        *gmut<u32x2>(codes + w.off * D + place.second * 8) = encode8(r.x + 8, by);
+        for (int v = 0; v < 2; ++v) {
+            const u32x2 c = encode8(r.x + 8 * v, by);
+            *gmut<u32x2>(codes + w.off * D + (v ? place.second : place.first) * 8) = c;
+            if (!row.bounds) continue;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t pair = k & 1 ? Code<F16>::pair<true>(c[k >> 1], 1.0f) : Code<F16>::pair<false>(c[k >> 1], 1.0f);
+                least[4 * v + k] = extreme<false>(least[4 * v + k], pair);
+                largest[4 * v + k] = extreme<true>(largest[4 * v + k], pair);
+            }
+        }
     }
     if (some && wave == wave0 && lane == 0) *gmut<float>(scale_at) = scale;
 
-    if (row.bounds) {           // every exchange halves what a lane has: 8 of the 32, 4 of the least and 4 of the largest ones
+    if (row.bounds) {           // every exchange halves what a lane has: 4 of the 16 pairs, 2 of the least and 2 of the largest ones
 #pragma unroll
-        for (int k = 0; k < 8; ++k) least[k] = of_halves<false>(least[k], least[k + 8]), largest[k] = of_halves<true>(largest[k], largest[k + 8]);
-        f32x4 low, high;
+        for (int k = 0; k < 4; ++k) least[k] = of_halves<false>(least[k], least[k + 4]), largest[k] = of_halves<true>(largest[k], largest[k + 4]);
+        u32x2 low, high;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            low[k] = over_sixteen<false, kLanes>(of_quarters<false>(least[k], least[k + 4]));
-            high[k] = over_sixteen<true, kLanes>(of_quarters<true>(largest[k], largest[k + 4]));
+        for (int k = 0; k < 2; ++k) {
+            low[k] = over_sixteen<false, kLanes>(of_quarters<false>(least[k], least[k + 2]));
+            high[k] = over_sixteen<true, kLanes>(of_quarters<true>(largest[k], largest[k + 2]));
         }
         const int at = (lane < 32 ? place.first : place.second) * 8 + (lane & 16) / 4;
-        if (lane % 16 < kLanes) *(f32x4 *)&lds.bounds[wave][at] = low, *(f32x4 *)&lds.bounds[wave][D + at] = high;
+        if (lane % 16 < kLanes) *(u32x2 *)&lds.bounds[wave][at] = low, *(u32x2 *)&lds.bounds[wave][D + at] = high;
     }
     __syncthreads();
     if (row.bounds && some) {
         uint16_t *bounds = row.bounds + (int64_t)page * a.h.kv_heads * 2 * D;
         for (int i = (wave - wave0) * 64 + lane; i < D; i += waves * 64) {      // two neighbours of the 2 D numbers
             const bool high = 2 * i >= D;
-            float x[2] = {lds.bounds[wave0][2 * i], lds.bounds[wave0][2 * i + 1]};
-            for (int w = wave0 + 1; w < wave0 + waves; ++w)
-#pragma unroll
-                for (int k = 0; k < 2; ++k) x[k] = high ? fmaxf(x[k], lds.bounds[w][2 * i + k]) : fminf(x[k], lds.bounds[w][2 * i + k]);
-            const bool any[2] = {fabsf(x[0]) < __builtin_inff(), fabsf(x[1]) < __builtin_inff()};       // a channel may be all NaN
-            const auto y = __builtin_amdgcn_cvt_pk_f32_fp8(__builtin_amdgcn_cvt_pk_fp8_f32(any[0] ? x[0] * by : 0.0f, any[1] ? x[1] * by : 0.0f, 0, false), false);
-            float z[2] = {y[0] * scale, y[1] * scale};
+            uint32_t x = *(const uint32_t *)&lds.bounds[wave0][2 * i];
+            for (int w = wave0 + 1; w < wave0 + waves; ++w) {
+                const uint32_t other = *(const uint32_t *)&lds.bounds[w][2 * i];
+                x = high ? extreme<true>(x, other) : extreme<false>(x, other);
+            }
+            const float y[2] = {Elem<F16>::lo(x), Elem<F16>::hi(x)};
+            const bool any[2] = {fabsf(y[0]) < __builtin_inff(), fabsf(y[1]) < __builtin_inff()};       // a channel may be all NaN
+            float z[2] = {any[0] ? y[0] * scale : 0.0f, any[1] ? y[1] * scale : 0.0f};
             CF_GLOBAL uint32_t *to = gmut<uint32_t>(bounds) + i;
             if (!begins) {
                 const uint32_t was = *to;
