@@ -138,11 +138,11 @@ cf_status cf_kv_append8(const cf_attn_desc *desc, const cf_kv_cache8 *cache, con
     a.rotary_dim = args->rotary_dim;
     a.interleaved = args->interleaved ? 1 : 0;
     // Some 2048 workgroups, or what 64 tokens each give: those that find no page's begin, or leave lone tokens to a neighbour, cost their launch.
-    a.chunk = (int32_t)round_up((n * 2 * a.h.kv_heads + 2047) / 2048, 8);
-    if (a.chunk > 64) a.chunk = 64;
+    const int64_t chunk = round_up((n * 2 * a.h.kv_heads + 2047) / 2048, 8);
+    a.chunk = (int32_t)(chunk < 64 ? chunk : 64);
     const int64_t each = ((n + a.chunk - 1) / a.chunk + kXcds - 1) / kXcds, groups = each * kXcds * 2 * a.h.kv_heads;
-    a.chunks_each = (int32_t)each;
     if (groups > kMostWorkgroups) return CF_ERR_SHAPE;
+    a.chunks_each = (int32_t)each;
     a.page_groups = (int32_t)groups;
     if (append8_workgroups(a) > kMostWorkgroups / (kAppendThreads / 256)) return CF_ERR_SHAPE;
     return status_of(launch_append8(a, static_cast<hipStream_t>(stream)));

@@ -98,8 +98,8 @@ int main()
     char *const far = reinterpret_cast<char *>((uintptr_t)1 << 50);
     int done[4] = {}, refused[4] = {};
     for (int i = 0; i < 200000; ++i) {
-        const int kv = (int)pick(1, pick(0, 9) ? 12 : 300), dims[] = {64, 128, 256, 96};
-        cf_attn_desc d = {(int32_t)pick(pick(0, 19) ? 1 : 0, 2), (int32_t)(kv * pick(1, 20)), kv, dims[pick(0, 20) ? pick(0, 2) : 3], pick(0, 3) ? 0.0f : 0.3f};
+        const int kv = (int)pick(1, pick(0, 9) ? 12 : pick(0, 5) ? 300 : 65536), dims[] = {64, 128, 256, 96};
+        cf_attn_desc d = {(int32_t)pick(pick(0, 19) ? 1 : 0, 2), (int32_t)(kv * (kv > 300 ? 1 : pick(1, 20))), kv, dims[pick(0, 20) ? pick(0, 2) : 3], pick(0, 3) ? 0.0f : 0.3f};
         const int pages[] = {16, 32, 64, 128, 48};
         cf_kv_cache8 c = {};
         c.page_size = pages[pick(0, 20) ? pick(0, 3) : 4];
