@@ -120,13 +120,11 @@ template <int DT, int D, bool PAIRS> __device__ __forceinline__ void rotate_quer
         }
 }
 
-// Of two fp16 numbers each.  NaN yields to a number; there are no signalling ones among decoded codes.
+// Of two fp16 numbers each.  NaN yields to a number.
 template <bool LARGEST> __device__ __forceinline__ uint32_t extreme(uint32_t a, uint32_t b)
 {
-    uint32_t r;
-    if constexpr (LARGEST) asm("v_pk_max_f16 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
-    else asm("v_pk_min_f16 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
-    return r;
+    const f16x2 x = __builtin_bit_cast(f16x2, a), y = __builtin_bit_cast(f16x2, b);
+    return __builtin_bit_cast(uint32_t, LARGEST ? __builtin_elementwise_max(x, y) : __builtin_elementwise_min(x, y));
 }
 // Over the lanes of sixteen that hold the same elements, every LANES-th one.
 template <bool LARGEST, int LANES> __device__ __forceinline__ uint32_t over_sixteen(uint32_t x)
