@@ -18,8 +18,9 @@ namespace {
 
 // SHARED: as many workgroups as the device holds have an equal share of all contexts' keys each, which they find in the lengths: a share may be the end of one context,
 // some short ones and the beginning of another.  Otherwise a workgroup for each part that there may be.  Either way the last workgroup that is done with a context's head
-// joins its parts.  LISTED: heads attend to the listed pages of their contexts alone; keys are counted along the list.  WHOLE: a step's keys lie on one page.
-template <int DT, int D, bool SHARED, bool LISTED, bool WHOLE> __global__ __launch_bounds__(kWaves * 64, kHeldWorkgroups) void k_attn_paged8(Paged8Args b)
+// joins its parts.  LISTED: heads attend to the listed pages of their contexts alone; keys are counted along the list.  TOGETHER: as many of a step's keys
+// as lie on one page for sure, 16 at least.
+template <int DT, int D, bool SHARED, bool LISTED, int TOGETHER> __global__ __launch_bounds__(kWaves * 64, kHeldWorkgroups) void k_attn_paged8(Paged8Args b)
 {
     using E = Elem<DT>;
     using C = Code<DT>;
@@ -29,8 +30,9 @@ template <int DT, int D, bool SHARED, bool LISTED, bool WHOLE> __global__ __laun
     constexpr int kSteps = D / 32;              // matrix instructions over the head dimension
     constexpr int kPer = D / 16;                // elements of a value row that a lane reads
     constexpr int kWords = kPer / 4;
-    constexpr int kGroups = WHOLE ? 1 : 2 * kTiles;     // keys of a step that lie on one page for sure: 16 on small ones
-    constexpr int kGroupKeys = kKeys / kGroups;
+    constexpr int kGroups = kKeys / TOGETHER;
+    constexpr int kGroupKeys = TOGETHER;
+    static_assert(TOGETHER >= 16 && TOGETHER <= kKeys, "groups of a step");
     constexpr int kGrain = kWaves * 64;         // keys: a step of the workgroup's
     const PagedArgs &a = b.p;
 
@@ -143,11 +145,12 @@ template <int DT, int D, bool SHARED, bool LISTED, bool WHOLE> __global__ __laun
                 }
                 return s;
             };
-            // of the two groups of a tile the second one, if so said; whole tiles have one
+            // what is said of a tile's group of keys: of its second one, where it has two
             auto group_at = [](const auto &x, int g, bool second) {
-                const auto low = x[WHOLE ? 0 : 2 * g], high = x[WHOLE ? 0 : 2 * g + 1];
+                const auto low = x[32 * g / kGroupKeys], high = x[(32 * g + 16) / kGroupKeys];
                 return second ? high : low;
             };
+            auto key_of = [](int g, int x) { return (32 * g + x) % kGroupKeys; };      // of its group: key x of tile g
             u32x4 k[kTiles][2][kLoads];
             auto load_k = [&](const Step &s) {
 #pragma unroll
@@ -155,7 +158,7 @@ template <int DT, int D, bool SHARED, bool LISTED, bool WHOLE> __global__ __laun
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
                         const int x = 8 * (col >> 2) + 4 * t + (col & 3);
-                        const char *src = WHOLE ? k_head + s.at[0] + (32 * g + x) * D + quarter * 16 : k_head + group_at(s.at, g, x >= 16) + (x & 15) * D + quarter * 16;
+                        const char *src = k_head + group_at(s.at, g, x >= 16) + key_of(g, x) * D + quarter * 16;
 #pragma unroll
                         for (int i = 0; i < kLoads; ++i) k[g][t][i] = *gconst<u32x4>(src + i * 64);
                     }
@@ -167,7 +170,7 @@ template <int DT, int D, bool SHARED, bool LISTED, bool WHOLE> __global__ __laun
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
                         const int x = 8 * quarter + j;
-                        const char *src = WHOLE ? v_head + s.at[0] + (32 * g + x) * D + col * kPer : v_head + group_at(s.at, g, x >= 16) + (x & 15) * D + col * kPer;
+                        const char *src = v_head + group_at(s.at, g, x >= 16) + key_of(g, x) * D + col * kPer;
                         if constexpr (kWords == 1) v[g][j][0] = *gconst<uint32_t>(src);
                         else if constexpr (kWords == 2) {
                             const u32x2 y = *gconst<u32x2>(src);
@@ -179,7 +182,7 @@ template <int DT, int D, bool SHARED, bool LISTED, bool WHOLE> __global__ __laun
                         }
                     }
             };
-            auto most_of = [&](const Step &s, int g) { return WHOLE ? s.there[0] - 32 * g - 8 * quarter : group_at(s.there, g, quarter >= 2) - 8 * (quarter & 1); };    // of a lane's 8 keys
+            auto most_of = [&](const Step &s, int g) { return group_at(s.there, g, quarter >= 2) - key_of(g, 8 * quarter); };    // of a lane's 8 keys
 
             // K of the next step is asked for as soon as this one's is used up, V of this one before that.
             int key0 = begin + wave * kKeys;
@@ -285,12 +288,19 @@ template <int DT, int D, bool SHARED, bool LISTED, bool WHOLE> __global__ __laun
     }
 }
 
+template <int DT, int D, bool SHARED, int TOGETHER> hipError_t paged8_pages(const Paged8Args &a, int64_t n, hipStream_t s)
+{
+    return a.blocks ? enqueue(k_attn_paged8<DT, D, SHARED, true, TOGETHER>, n, s, a) : enqueue(k_attn_paged8<DT, D, SHARED, false, TOGETHER>, n, s, a);
+}
+
 template <int DT, int D, bool SHARED> hipError_t paged8_over(const Paged8Args &a, hipStream_t s)
 {
     const int64_t n = paged8_workgroups(a);
-    const bool whole = a.cache.page_size >= (D == 256 ? 32 : 64);
-    if (a.blocks) return whole ? enqueue(k_attn_paged8<DT, D, SHARED, true, true>, n, s, a) : enqueue(k_attn_paged8<DT, D, SHARED, true, false>, n, s, a);
-    return whole ? enqueue(k_attn_paged8<DT, D, SHARED, false, true>, n, s, a) : enqueue(k_attn_paged8<DT, D, SHARED, false, false>, n, s, a);
+    constexpr int kStep = D == 256 ? 32 : 64;       // keys of a wave's
+    const int together = a.cache.page_size < kStep ? a.cache.page_size : kStep;
+    if (together == 64) return paged8_pages<DT, D, SHARED, kStep>(a, n, s);
+    if (together == 32) return paged8_pages<DT, D, SHARED, 32>(a, n, s);
+    return paged8_pages<DT, D, SHARED, 16>(a, n, s);
 }
 
 template <int DT, int D> hipError_t paged8_dim(const Paged8Args &a, hipStream_t s) { return a.p.many ? paged8_over<DT, D, true>(a, s) : paged8_over<DT, D, false>(a, s); }
