@@ -205,6 +205,22 @@ def test_append_leaves_out_tokens_and_places():
     assert not torch.equal(cache.k[2].view(torch.uint8), before[0][2])
 
 
+@pytest.mark.parametrize("first", [0, 5])
+def test_append_two_tokens_into_one_slot(first):
+    """The place holds elements of either; scales and bounds are of both, and of the neighbour behind them."""
+    g, page, dim = gen(19), 16, 128
+    cache = filled(20, 3, 2, page, dim, True)
+    k = randn(g, 3, 2, dim)
+    want = [ref.Cache(cache.k, cache.k_scale, cache.bounds) for _ in range(2)]
+    AttentionSession(2, 2, dim).append8(cache, k, k, ints([page + first, page + first, page + first + 1], torch.int64))
+    torch.cuda.synchronize()
+    for w, order in zip(want, ([0, 1, 2], [1, 0, 2])):
+        w.append(k.double().cpu()[order], [page + first, page + first, page + first + 1], BF)
+    got = cache.k.float().double().cpu()
+    assert torch.equal(cache.k_scale.double().cpu(), want[0].scale) and torch.equal(cache.bounds.double().cpu(), want[0].bounds)
+    assert bool(((got == want[0].codes) | (got == want[1].codes)).all())
+
+
 def test_append_queries_in_place_without_and_alone():
     g = gen(11)
     q, k = randn(g, 9, 4, 64), randn(g, 9, 2, 64)
