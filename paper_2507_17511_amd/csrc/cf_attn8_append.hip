@@ -1,13 +1,15 @@
 // Keys and values into the paged cache of 8-bit codes, rotated on the way, and the queries' rotation.
 //
 // What a call's tokens bring to one page is one piece of work for each head of keys and of values: their largest magnitude decides the scale.  Such
-// tokens are neighbours in the call, so that a workgroup finds where they begin by looking at the slots alone.  It takes the pages that begin among `chunk` tokens: lone
-// tokens, one of a page, as a step of generation brings them, for four heads, a wave each, as many at a time as a wave has room for their rows; neighbours on a page for one head, or
-// as many as its four waves have room for.  They read the rows twice, once for the scale and once for the codes, the second time from the caches.  To keep them in registers
-// instead took so many that few waves were there to wait for memory (16384 tokens, 8 heads of 128, no queries: 83 us for 38).
+// tokens are neighbours in the call, so that a workgroup finds where they begin by looking at the slots alone.  It takes the pages that begin among `chunk`
+// tokens: lone tokens, one of a page, as a step of generation brings them, for four heads, a wave each, as many at a time as a wave has room for their rows;
+// neighbours on a page for one head, or as many as its four waves have room for.  They read the rows twice, once for the scale and once for the codes, the
+// second time from the caches.  To keep them in registers instead took so many that few waves were there to wait for memory (16384 tokens, 8 heads of 128,
+// no queries: 83 us; as it is 36).
 //
-// 16384 tokens of 24 + 2 x 8 heads of 128 in 69 us (4.5 TB/s): bound by HBM for the queries, by instructions (60 % of the time) and latencies for the pages; 6331 of 16 + 2 x 2 heads of 256 in
-// 26 (4.9 TB/s); 48 in 4.6, by its launch.  Fewer waves for a row leave instructions out and time in (two rows a workgroup 50 us for 38, four 78); eight waves, which read rows once, 55.
+// 16384 tokens of 24 + 2 x 8 heads of 128 in 68 us (4.5 TB/s): bound by HBM for the queries, by instructions (60 % of the time) and latencies for the pages;
+// 6331 of 16 + 2 x 2 heads of 256 in 25 (5.0 TB/s); 48 in 4.7, by its launch.  Fewer waves for a row leave instructions out and time in (no queries,
+// two rows a workgroup 50 us, four 78); eight waves, which read rows once, 55.
 #include "cf_attn8_device.h"
 
 namespace cf {
