@@ -71,6 +71,28 @@ constexpr int kSelectPages = 64;    // that a workgroup of the scores takes
 constexpr int kAppendThreads = 256, kAppendTurns = 4;    // a lane rotates its part of so many heads' queries
 constexpr int kPlanThreads = 1024;
 
+// Scores as whole numbers in the same order; NaN is the least.
+__host__ __device__ inline uint64_t ordered_score(double x)
+{
+    if (x != x) return 0;
+    const uint64_t w = __builtin_bit_cast(uint64_t, x + 0.0);       // -0 is 0
+    return w >> 63 ? ~w : w | (uint64_t)1 << 63;
+}
+
+// The scores from `from` to `end`, both among them, among which the least one that is taken is looked for, in kScoreBins bins of 2^shift.
+constexpr int kScoreBits = 11, kScoreBins = 1 << kScoreBits;
+struct ScoreRange {
+    uint64_t from, end;
+    __host__ __device__ int shift() const { return (end - from) >> kScoreBits ? 64 - kScoreBits - __builtin_clzll(end - from) : 0; }
+    __host__ __device__ bool holds(uint64_t x) const { return x >= from && x <= end; }
+    // One of the bins that hold scores.  The last one is cut off at `end`: it may reach past the largest number there is (infinity lies 2^52 below that, bins are up to 2^53 wide).
+    __host__ __device__ ScoreRange bin(uint32_t i, int shift) const
+    {
+        const uint64_t at = from + ((uint64_t)i << shift), behind = ((uint64_t)1 << shift) - 1;
+        return {at, end - at < behind ? end : at + behind};
+    }
+};
+
 // Where workgroups have shares of all contexts (p.many): as many as the device holds at a time.
 inline int64_t paged8_workgroups(const Paged8Args &a)
 {

@@ -12,14 +12,6 @@ namespace cf {
 namespace attn {
 namespace {
 
-// Scores as whole numbers in the same order; NaN is the least.
-__device__ __forceinline__ uint64_t ordered(double x)
-{
-    if (x != x) return 0;
-    const uint64_t w = __builtin_bit_cast(uint64_t, x + 0.0);       // -0 is 0
-    return w >> 63 ? ~w : w | (uint64_t)1 << 63;
-}
-
 __device__ __forceinline__ int pages_of(const SelectArgs &a, int64_t seq)
 {
     const int64_t held = ((int64_t)max(gconst<int32_t>(a.lens)[seq], 0) + a.cache.page_size - 1) >> a.cache.page_shift;
@@ -107,11 +99,11 @@ template <int DT, int D> __global__ __launch_bounds__(256) void k_select_scores(
         }
         const int sixteen = lane >> 4, r = lane & 3;
         const int64_t j = first + (kRounds == 4 ? r * 4 + sixteen : kRounds == 8 ? (r + 4 * (sixteen & 1)) * 2 + (sixteen >> 1) : r + 4 * (sixteen & 1) + 8 * (sixteen >> 1));
-        if ((lane & 15) < 4 && j < held) gmut<uint64_t>(a.scores)[row * a.columns + j] = ordered(mine);
+        if ((lane & 15) < 4 && j < held) gmut<uint64_t>(a.scores)[row * a.columns + j] = ordered_score(mine);
     }
 }
 
-constexpr int kBins = 2048, kEach = 8;      // pages of a thread
+constexpr int kBins = kScoreBins, kEach = 8;      // pages of a thread
 
 template <int THREADS> __global__ __launch_bounds__(THREADS) void k_select_pages(SelectArgs a)
 {
@@ -155,8 +147,9 @@ template <int THREADS> __global__ __launch_bounds__(THREADS) void k_select_pages
         return s - mine + (wave > 0 ? __builtin_amdgcn_readlane(w, wave - 1) : 0);
     };
 
-    // Scores past `from` are taken, and of those that equal it the first `rest`: all, if so many are.  The range that holds the one that decides is narrowed by 2^11 a time.
-    uint64_t from = 0;
+    // Scores past `from` are taken, and of those that equal it the first `rest`: all, if so many are.  The range that holds the one that decides is narrowed by 2^11 a time; there are
+    // `rest` scores in it at least, and one at least to be taken.
+    ScoreRange range = {};
     uint32_t rest = (uint32_t)(a.count - a.first - a.recent);
     bool all = false;
     if (some) {
@@ -176,16 +169,14 @@ template <int THREADS> __global__ __launch_bounds__(THREADS) void k_select_pages
         for (int i = threadIdx.x; i < kBins; i += THREADS) lds_bins[i] = 0;
         __syncthreads();
         for (int w = 0; w < kWavesHere; ++w) least = min(least, lds_least[w]), largest = max(largest, lds_largest[w]);
-        from = (uint64_t)least << 32;
-        uint64_t end = (uint64_t)largest << 32 | ~0u;
+        range = {(uint64_t)least << 32, (uint64_t)largest << 32 | ~0u};
         for (;;) {
-            const uint64_t range = end - from;
-            const int shift = range >> 11 ? 64 - 11 - __builtin_clzll(range) : 0;
+            const int shift = range.shift();
             for (int base = 0; base < behind; base += kTurn) {
                 if (!once) read(base);
 #pragma unroll
                 for (int k = 0; k < kEach; ++k)
-                    if (competes(base, k) && x[k] >= from && x[k] <= end) atomicAdd(&lds_bins[(x[k] - from) >> shift], 1u);
+                    if (competes(base, k) && range.holds(x[k])) atomicAdd(&lds_bins[(x[k] - range.from) >> shift], 1u);
             }
             __syncthreads();
             // scores in this thread's bins, and in all bins past them
@@ -206,12 +197,12 @@ template <int THREADS> __global__ __launch_bounds__(THREADS) void k_select_pages
             __syncthreads();
             rest -= lds_found[1];
             all = lds_found[2] == rest;
-            from += (uint64_t)lds_found[0] << shift;
+            range = range.bin(lds_found[0], shift);
             if (all || shift == 0) break;
-            end = min(end, from + (((uint64_t)1 << shift) - 1));
             __syncthreads();
         }
     }
+    const uint64_t from = range.from;
     // -> a page is taken if its score is past `from`, or if it equals it and is one of the first `rest`, or (all) if it is not less; and if it does not compete
     uint32_t taken = 0, ties = 0;
     for (int base = 0; base < held; base += kTurn) {
@@ -237,7 +228,10 @@ template <int THREADS> __global__ __launch_bounds__(THREADS) void k_select_pages
         taken += in_all;
 #pragma unroll
         for (int k = 0; k < kEach; ++k)
-            if (take >> k & 1) out[at++] = j + k;
+            if (take >> k & 1) {
+                if (at < (uint32_t)a.count) out[at] = j + k;      // as many as are taken; whatever the scores, nothing goes into another row
+                ++at;
+            }
     }
 }
 
