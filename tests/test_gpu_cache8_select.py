@@ -101,3 +101,43 @@ def test_infinite_scores(change, dtype, count, first, recent):
     run(51, dtype, 4, 2, 64, 16, [1600, 16 * 900, 100, 16 * 60], count, first, recent, change)
     run(52, dtype, 4, 2, 128, 16, [16 * 2500, 1600, 100], count, first, recent, change)
     run(53, dtype, 6, 2, 256, 32, [32 * 700, 3200], count, first, recent, change, pages=60)
+
+
+# Contexts past the 8192 pages whose scores stay in registers: 8 a thread, 1024 threads.
+
+LONG = [16 * 20001 - 3, 16 * 8193, 16 * 8192, 16 * 16384, 1600, 0]
+
+
+@pytest.mark.parametrize("count,first,recent", [(1, 0, 0), (100, 1, 1), (9000, 0, 0), (8200, 8190, 4), (15000, 8193, 3), (15000, 2, 11900), (20000, 0, 0), (12000, 6000, 6000)])
+@pytest.mark.parametrize("pages", [40, None])
+def test_contexts_whose_scores_are_read_again(count, first, recent, pages):
+    """Few physical pages: many equal scores on both sides of a turn's border.  Pages of their own: scores that differ."""
+    run(54, BF, 4, 2, 64, 16, LONG, count, first, recent, pages=pages)
+
+
+def nothing(q, bounds):
+    q.zero_()
+
+
+def nan_here_and_there(q, bounds):
+    bounds[::3, :, 1, 5] = math.nan
+    q[1, 0, 3] = math.nan
+
+
+def two_scores(q, bounds):                 # one of 1 on every seventh page, 0 elsewhere: ties that lie across all turns
+    bounds.zero_()
+    bounds[::7, :, 1, 0] = 1.0
+    q.zero_()
+    q[:, 0, 0] = 1.0
+
+
+@pytest.mark.parametrize("change", [nothing, nan_here_and_there, two_scores, one, both_and_nan])
+@pytest.mark.parametrize("count,first,recent", [(100, 1, 1), (2000, 0, 0), (8192, 0, 1), (8193, 1, 0), (16385, 100, 100)])
+def test_equal_scores_across_turns(change, count, first, recent):
+    run(55, BF, 2, 1, 64, 16, LONG, count, first, recent, change)
+    run(56, HF, 4, 2, 128, 16, LONG[:4], count, first, recent, change, pages=77)
+
+
+def test_long_contexts_some_heads_at_a_time():
+    """A workspace for the scores of three heads of the eight."""
+    run(57, BF, 4, 2, 64, 16, LONG[:4], 100, 1, 1, workspace_bytes=cf.CF_ATTN_COUNTER_BYTES + 3 * 20001 * 8 // 256 * 256 + 256)
