@@ -142,6 +142,7 @@ template <int DT, int D, bool SHARED, bool LISTED, int TOGETHER> __global__ __la
                     s.at[g] = page * b.cache.page_bytes + off * D;
                     s.k[g] = k_scale[page * a.h.kv_heads];
                     s.v[g] = v_scale[page * a.h.kv_heads];
+                    if (LISTED && s.there[g] <= 0) s.v[g] = 1.0f;       // an infinite scale of a page that is not attended to would make NaN of the zeros that stand for its values
                 }
                 return s;
             };
