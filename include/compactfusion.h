@@ -339,7 +339,8 @@ const char *cf_profile_kernel_name(const cf_ctx *ctx, int32_t k);
  * Arithmetic.  Scores, the running maximum and sum of the softmax and all accumulators are fp32; the weights
  * exp(score - maximum) are rounded once to `dtype` for the product with the values on the matrix cores, and outputs are
  * rounded once.  In fp16, whose smallest numbers are 2^-24, what weights are relative to falls with the scores, so that keys that weigh little
- * each and much together, behind a first key that leads them all by far, keep their part; where scores differ so much again and again, it stays.  Results do not depend on timing: the same call on the same data gives the same bits.
+ * each and much together, behind a first key that leads them all by far, keep their part; where scores differ so much again and again, it stays.
+ * Results do not depend on timing: the same call on the same data gives the same bits (but for two tokens that are appended to one slot).
  * Keys that a row does not see (masked, past the end of a sequence, on a page beyond the context) do not
  * reach its output or its log-sum-exp, whatever those places hold, NaN and infinities included.  A row that sees no
  * key, or whose scores are all -infinity, gives zeros and a log-sum-exp of -infinity. */
@@ -374,7 +375,8 @@ typedef struct {
     int64_t n_tokens;         /* >= 0 */
     cf_rows k, v;             /* [n_tokens][kv_heads][head_dim] */
     const int64_t *slots;     /* device [n_tokens]: where token t goes in the cache; a token with a slot outside the cache
-                                 (negative: padding) does not go there.  Two tokens of one call in one slot: elements of either. */
+                                 (negative: padding) does not go there.  Two tokens of one call in one slot: each element is
+                                 that of either, and may be the other's in another call on the same data. */
     cf_rows q, q_out;         /* [n_tokens][q_heads][head_dim]: rotated queries; data null: none.  q_out may be q itself. */
     const int32_t *positions; /* device [n_tokens]; a token whose position is not in [0, n_positions) is left out
                                  altogether.  Not read with rotary_dim 0. */
@@ -463,9 +465,9 @@ typedef struct {
     int32_t page_size;       /* tokens of a page: 16, 32, 64 or 128 */
 } cf_kv_cache8;
 
-/* cf_kv_append into such a cache: rotation in fp32, then codes, with one rounding.  Tokens (two in one slot, too) of a call that go to the same page are neighbours in it, with no
- * other tokens between them (as those of a sequence are); otherwise what that page holds afterwards is undefined.  A token at a page's first place begins
- * the page anew: its scales and bounds are those of the call's tokens.  On a page that is not begun the scale grows where the call's tokens need it, and the codes of all other
+/* cf_kv_append into such a cache: rotation in fp32, then codes, with one rounding.  Tokens of a call that go to the same page are neighbours in it, with no other tokens between them
+ * (as those of a sequence are); otherwise what that page holds afterwards is undefined.  Two of them in one slot: codes are those of either, as there, scales and bounds are of both.
+ * A token at a page's first place begins the page anew: its scales and bounds are those of the call's tokens.  On a page that is not begun the scale grows where the call's tokens need it, and the codes of all other
  * places are rounded to the new one: exactly, but for those below 2^-6 of it.  The bounds are of elements as stored, and keep those of elements that were rounded again. */
 cf_status cf_kv_append8(const cf_attn_desc *desc, const cf_kv_cache8 *cache, const cf_append *args, void *stream);
 

@@ -182,3 +182,27 @@ def test_rotated_pages_among_up_to_64_tokens(dim, rotary, chunk, n, hk):
 def test_a_long_prompt():
     """Every place taken, page after page: 16 sequences of 16384 tokens in all."""
     append_and_compare(63, BF, 16384, 8, 8, 128, 64, 64, 128, left_out=False)
+
+
+# ---------------------------------------------------------------- two tokens of a call in one slot
+
+@pytest.mark.parametrize("dim,page", [(64, 64), (128, 32), (128, 128), (256, 16), (256, 64)])
+@pytest.mark.parametrize("first", [0, 3])
+def test_two_tokens_in_one_slot_that_two_waves_have(dim, page, first):
+    """Runs that all waves of a workgroup share, the same slots twice: elements of either, the first ones and the last ones of a token alike;
+    scales and bounds are those of all tokens."""
+    g, hk = gen(64), 2
+    n = page - first                        # tokens i and n + i go to one slot: another wave's, or another round's
+    cache = filled(65, 3, hk, page, dim, True)
+    k = randn(g, 2 * n, hk, dim, dtype=BF, scale=2.0)
+    slots = (torch.arange(2 * n, device=DEV) % n) + page + first
+    want = [ref.Cache(cache.k, cache.k_scale, cache.bounds) for _ in range(2)]
+    AttentionSession(hk, hk, dim).append8(cache, k, k, slots)
+    torch.cuda.synchronize()
+    for w, order in zip(want, (list(range(2 * n)), list(range(n, 2 * n)) + list(range(n)))):
+        w.append(k.double().cpu()[order], slots.tolist(), BF)
+    got = cache.k.float().double().cpu()
+    assert torch.equal(cache.k_scale.double().cpu(), want[0].scale) and torch.equal(cache.bounds.double().cpu(), want[0].bounds)
+    assert bool(((got == want[0].codes) | (got == want[1].codes)).all())
+    for p in (0, 2):
+        assert torch.equal(got[p], want[0].codes[p])
