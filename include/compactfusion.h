@@ -458,7 +458,7 @@ cf_status cf_attn_join(const cf_attn_desc *desc, const cf_join *args, void *stre
  * its scale k_scale[(s / page_size) * kv_heads + h]. */
 typedef struct {
     void *k, *v;             /* 16-byte aligned; they must not overlap, except that pages of one may lie between pages of the other */
-    float *k_scale, *v_scale;/* [n_pages][kv_heads] each, dense.  Of a number that is no such power of two the exponent counts */
+    float *k_scale, *v_scale;/* [n_pages][kv_heads] each, dense.  Of a number that is no such power of two the exponent counts; an infinite or NaN one makes NaN of what is attended, and counts as 2^119 for an append */
     void *bounds;            /* bf16 [n_pages][kv_heads][2][head_dim], dense, 16-byte aligned: the least and the largest of each channel of a page's keys; may be null (cf_attn_select reads it) */
     int64_t n_pages;         /* 1 .. 2^31 - 1 */
     int64_t page_stride;     /* elements (bytes) from page to page, a multiple of 16; 0 = kv_heads * page_size * head_dim (dense), less is refused, and so is more than 2^60 bytes of pages */

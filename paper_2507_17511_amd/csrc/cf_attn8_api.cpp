@@ -66,10 +66,16 @@ cf_status check_table(int32_t n_seqs, int32_t max_pages, int64_t stride, int64_t
 
 constexpr int64_t kMostPartKeys8 = 2048;
 
-// A workgroup for each part of a context, two a CU: of 256 to 2048 keys each, or 128 where a context is 1024 at most (us, parts of 128 / 256 / 512 keys: 1 x 901, 2 heads of 128
-// 8.3 / 9.0 / 10.2, of 256 8.7 / 10.1 / 11.9; 1 x 8192, 8 heads 14.8 / 11.5 / 11.0; 2 x 4000, 4 heads of 256 12.6 / 11.3 / 12.5; 1 x 131072 47.4 all three), or, past four a CU and where contexts that may differ could fill 64 MB, equal shares of all keys for as many workgroups
-// as the device holds: us, parts taken in turn / shares: 96 x 160 to 16000 keys, 8 heads of 128, 149 / 138; 64 x 8192 196 / 187; 2 x 131100 111 / 104, 24 heads of 64 157 / 150; 48 x
-// 160 to 16000, 2 heads of 256, 34 / 39.
+// A workgroup for each part of a context, two a CU: of 256 to 2048 keys each, or 128 where a context is 1024 at most.  us in a graph, parts of 128 / 256 keys, 2 and 8 heads: 1 x 901 of
+// 128 8.2 / 8.9 and 8.7 / 9.0, of 256 8.6 / 10.0 and 9.0 / 10.1; 1 x 1500 of 128 8.3 / 9.0 and 9.1 / 9.3, of 64 7.5 / 7.6 and 8.5 / 8.0; 1 x 2048 of 128 8.5 / 9.0 and 9.6 / 9.4; 1 x 4000 9.1 / 9.1
+// and 11.4 / 10.1, of 256 10.4 / 10.5 and 12.6 / 11.4: between 1024 and 3000 keys the better one goes by heads and their width, by a tenth.  Where 32 parts of each already give a workgroup a CU
+// there are no more of them, as each adds to the join: 8 heads of 128, 1 x 16384 13.5 for 15.9, 1 x 32768 18.1 for 20.9, 1 x 60000 26.0 for 26.4.
+//
+// Past four workgroups a CU, and where contexts that may differ could fill 64 MB, equal shares of all keys for as many workgroups as the device holds.  The host does not know the lengths: contexts
+// that differ gain, a few that are alike may lose.  us in a graph, a workgroup for each part / shares, heads of 128: 96 x 160 to 16000 keys, 8 heads, 157 / 139; 150 x 90 to 9000, 1 head, 37 / 23;
+// 64 x 8192, 8 heads, 203 / 187; 2 x 131100 104 / 104; 8 x 8192 27 / 30; lists of 64 pages of 64 (with their selection) for 64 contexts of 320 to 32000
+// 95 / 91, for 8 of 131072 40 / 43; 2 x 131100, 24 heads of 64, 157 / 150.
+// Heads of 256: 48 x 160 to 16000, 2 heads, 51 / 36, 8 heads 167 / 136; 16 x 600 to 60000, 2 heads, 89 / 53; 24 x 8192 44 / 51; 4 x 60000 45 / 59.
 hipError_t paged8_at_once(Paged8Args &b, int64_t longest, void *workspace, size_t workspace_bytes, hipStream_t s)
 {
     PagedArgs &a = b.p;

@@ -5,7 +5,7 @@
 // tokens: lone tokens, one of a page, as a step of generation brings them, for four heads, a wave each, as many at a time as a wave has room for their rows;
 // neighbours on a page for one head, or as many as its four waves have room for.  They read the rows twice, once for the scale and once for the codes, the
 // second time from the caches.  To keep them in registers instead took so many that few waves were there to wait for memory (16384 tokens, 8 heads of 128,
-// no queries: 83 us; as it is 36).
+// no queries: 83 us; as it is 35).
 //
 // 16384 tokens of 24 + 2 x 8 heads of 128 in 68 us (4.5 TB/s): bound by HBM for the queries, by instructions (60 % of the time) and latencies for the pages;
 // 6331 of 16 + 2 x 2 heads of 256 in 25 (5.0 TB/s); 48 in 4.7, by its launch.  Fewer waves for a row leave instructions out and time in (no queries,

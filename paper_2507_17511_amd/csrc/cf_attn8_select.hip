@@ -1,8 +1,9 @@
 // Which pages of a context a head attends to: every page has a bound on what its keys may score, and the largest bounds win.
 //
 // sum over heads h and elements i of max(q_hi least_i, q_hi largest_i) = sum_i largest_i P_i + least_i N_i, where P sums the positive q_hi of the heads that share
-// the keys and N the others: one product of 2 D numbers a page, whatever the number of heads.  Sums are of 64 bits, and exact but for numbers that
-// lie more than 2^36 apart, so that ties are ties, whatever the order.  k_select_scores reads every bound once and is bound by HBM, or by its launch;
+// the keys and N the others: one product of 2 D numbers a page, whatever the number of heads.  Sums are of 64 bits, and every page's in the same order, so that
+// equal bounds have equal scores.  They are exact, and equal whatever the order, where what is summed spans 53 bits at most: 9 of 512 terms, 8 of a bound, 8 (fp16: 11) of a
+// query and log2 of the heads that share keys leave 28 (25) powers of two, less that logarithm, between the largest and the least number of the queries and of the bounds together.  k_select_scores reads every bound once and is bound by HBM, or by its launch;
 // k_select_pages finds the least score that is taken by its bits, 11 at a time, a workgroup a row, and writes the pages in order.  A thread has 8 neighbouring pages, whose
 // scores stay in registers, and whose places follow from a sum over the threads.  us in a graph, both and the attention over what they select: 2048 pages for each of 8 heads 4.7 + 5.2 + 9.9,
 // 24 contexts of 1 to 1875 pages 12.0 (3.6 TB/s) + 6.5 + 31.
@@ -252,6 +253,9 @@ hipError_t launch_select(const SelectArgs &a, hipStream_t s)
     hipError_t e = hipSuccess;
     if (a.max_pages > a.count && a.count > a.first + a.recent) e = a.h.dtype == BF16 ? scores_typed<BF16>(a, s) : scores_typed<F16>(a, s);
     if (e != hipSuccess) return e;
+    // By what the scores of a row may be, for which the table's width speaks (the hint of the longest context may be wrong): 256 threads that have all of them in registers, or four times as
+    // many, which read them less often.  us of both kernels in a graph, 8 heads of 128, 256 / 1024 threads: 2048 pages 16.8 / 18.9, 24 contexts of 900 28 / 30, of 200 in a table of 8192
+    // 46 / 48; 4096 pages 29 / 20, 8192 49 / 26.
     return a.max_pages <= 256 * kEach ? enqueue_of<256>(k_select_pages<256>, a.n_rows, s, a) : enqueue_of<1024>(k_select_pages<1024>, a.n_rows, s, a);
 }
 
