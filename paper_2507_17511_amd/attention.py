@@ -56,9 +56,21 @@ def _require(ok: bool, what: str) -> None:
         raise ValueError(what)
 
 
-class PagedCache:
+class _Held:
+    """Tensors that calls know by their addresses.  One that is put in another's place is checked as the first ones were, and is what the next call is given."""
+    _given: tuple = ()
+
+    def __setattr__(self, name, x):
+        if name in self._given:
+            self.__init__(**{**{n: getattr(self, n) for n in self._given}, name: x})
+        else:
+            super().__setattr__(name, x)
+
+
+class PagedCache(_Held):
     """Pages of keys and values: two tensors [pages, kv_heads, page_size, head_dim], dense within a page.  They may be views
     of one tensor, [pages, 2, ...] say, or of one that holds all layers."""
+    _given = ("k", "v")
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor):
         _require(k.dim() == 4 and k.shape == v.shape and k.dtype == v.dtype and k.device == v.device, "k and v are [pages, kv_heads, page_size, head_dim], alike")
@@ -67,7 +79,7 @@ class PagedCache:
             _require(x.numel() > 0 and x[0].is_contiguous() and (pages == 1 or x.stride(0) == k.stride(0) >= heads * page * dim),
                      "pages are dense, do not overlap, and are as far apart in k as in v")
         _require(not ((k.requires_grad or v.requires_grad) and torch.is_grad_enabled()), f"a cache {_NO_GRADIENT}")
-        self.k, self.v = k, v
+        vars(self).update(k=k, v=v)
         self.heads, self.page_size, self.head_dim, self.dtype, self.index = heads, page, dim, k.dtype, k.get_device()
         self.struct = cf.cf_kv_cache(k.data_ptr(), v.data_ptr(), pages, k.stride(0) if pages > 1 else 0, page)
         self.ref = ctypes.byref(self.struct)
@@ -79,10 +91,11 @@ class PagedCache:
         return cls(kv[0], kv[1])
 
 
-class PagedCache8:
+class PagedCache8(_Held):
     """Pages of 8-bit codes: two tensors [pages, kv_heads, page_size, head_dim] of torch.float8_e4m3fn, dense within a page, and their scales, two of
     torch.float32 [pages, kv_heads], powers of two.  bounds: torch.bfloat16 [pages, kv_heads, 2, head_dim], the least and the largest of each
     channel of a page's keys, which AttentionSession.select reads."""
+    _given = ("k", "v", "k_scale", "v_scale", "bounds")
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, bounds: Optional[torch.Tensor] = None):
         _require(k.dim() == 4 and k.shape == v.shape and k.dtype is v.dtype is torch.float8_e4m3fn and k.device == v.device,
@@ -95,9 +108,9 @@ class PagedCache8:
             _require(x.shape == (pages, heads) and x.dtype is torch.float32 and x.device == k.device and x.is_contiguous(), "scales are dense [pages, kv_heads] of torch.float32")
         _require(bounds is None or (bounds.shape == (pages, heads, 2, dim) and bounds.dtype is torch.bfloat16 and bounds.device == k.device and bounds.is_contiguous()),
                  "bounds are dense [pages, kv_heads, 2, head_dim] of torch.bfloat16")
-        self.written = [x for x in (k, v, k_scale, v_scale, bounds) if x is not None]
-        _require(not (any(x.requires_grad for x in self.written) and torch.is_grad_enabled()), f"a cache {_NO_GRADIENT}")
-        self.k, self.v, self.k_scale, self.v_scale, self.bounds = k, v, k_scale, v_scale, bounds
+        written = [x for x in (k, v, k_scale, v_scale, bounds) if x is not None]
+        _require(not (any(x.requires_grad for x in written) and torch.is_grad_enabled()), f"a cache {_NO_GRADIENT}")
+        vars(self).update(k=k, v=v, k_scale=k_scale, v_scale=v_scale, bounds=bounds, written=written)
         self.heads, self.page_size, self.head_dim, self.index = heads, page, dim, k.get_device()
         self.struct = cf.cf_kv_cache8(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), None if bounds is None else bounds.data_ptr(),
                                       pages, k.stride(0) if pages > 1 else 0, page)
@@ -117,16 +130,17 @@ class Plan(NamedTuple):
     refused: torch.Tensor       # int32 [1]: sequences whose tokens are not served
 
 
-class PageTables:
+class PageTables(_Held):
     """Which pages the sequences of a batch hold, table [sequences, max_pages] int32 and lens [sequences] int32, and which are free: pages ring[i % len(ring)] (int32),
     state[0] <= i < state[1] (int64 [2]: taken and put, ever).  All of it stays on the device; AttentionSession.plan updates it."""
+    _given = ("table", "lens", "ring", "state", "page_size")
 
     def __init__(self, table: torch.Tensor, lens: torch.Tensor, ring: torch.Tensor, state: torch.Tensor, page_size: int):
         _require(table.dim() == 2 and table.dtype is torch.int32 and table.shape[1] > 0 and (table.shape[1] == 1 or table.stride(1) == 1) and
                  (table.shape[0] < 2 or table.stride(0) >= table.shape[1]), "table is [sequences, pages] int32, its rows dense")
         for x, dtype, n, name in ((lens, torch.int32, table.shape[0], "lens"), (ring, torch.int32, ring.numel(), "ring"), (state, torch.int64, 2, "state")):
             _require(x.shape == (n,) and x.dtype is dtype and x.device == table.device and x.is_contiguous(), f"{name} is {n} dense values of {dtype} on {table.device}")
-        self.table, self.lens, self.ring, self.state, self.page_size = table, lens, ring, state, page_size
+        vars(self).update(table=table, lens=lens, ring=ring, state=state, page_size=page_size)
         self.seqs, self.index = table.shape[0], table.get_device()
         self.head = (self.seqs, page_size, table.shape[1], ring.numel(), table.stride(0) if self.seqs > 1 else 0)
         self.at = (table.data_ptr(), ring.data_ptr(), state.data_ptr())
