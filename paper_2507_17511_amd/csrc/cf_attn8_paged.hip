@@ -257,7 +257,7 @@ template <int DT, int D, bool SHARED, bool LISTED, int TOGETHER> __global__ __la
                             for (int w = 0; w < kWords; ++w) v[g][j][w] = j < most ? v[g][j][w] : 0u;
                     }
                     // Scaled scores are rounded as their maximum was: of scores of any size the largest has the weight 1.  Weights are rounded once, to the type that the matrix instructions
-                    // take; their sum is of those that were not.  An output's error is that of its own rounding and 1 to 7 % more (96 contexts, bf16: 1.59e-3 of it, 1.56e-3 with fp32 weights).
+                    // take; their sum is of those that were not.  An output's error is that of its own rounding and up to 7 % more (96 contexts, bf16: 1.59e-3 of it, 1.56e-3 with fp32 weights).
                     u32x4 p;
 #pragma unroll
                     for (int j = 0; j < 8; j += 2) {
